@@ -420,6 +420,179 @@ int hbf_cache_get_chunk(hbf_cache_t cache, uint32_t *accesses);
 int hbf_cache_sweep(const uint32_t *host_frames, const uint32_t *host_prefetch, int n_cfg, uint64_t range_pages,
                     const uint64_t *dev_pages, int64_t n, int64_t *dev_counts, void *stream);
 
+/* ---- Operators of a decode layer: what reads the weights and the KV pages
+ * whose traffic the calls above time.  They need no model.  16-bit values are
+ * bfloat16 or IEEE half (HBF_BF16, HBF_FP16; one type per call).  Products
+ * accumulate, and softmax statistics and sums are held, in 32 bits.
+ * Host-detectable errors return before any launch. */
+#define HBF_BF16 0u
+#define HBF_FP16 1u
+
+/* A cache of pages: token t of a sequence lies in page row[t / page_tokens],
+ * at token t % page_tokens of it.  A page id stands for the same page in
+ * every plane (a plane is one layer's K or V), so that one table row serves
+ * all of them.  The caller owns everything, the arrays' first values
+ * included; the calls below keep them consistent:
+ *  - slot s holds dev_lens[s] tokens and the first
+ *    ceil(dev_lens[s] / page_tokens) entries of row s of dev_tables; other
+ *    entries are not read;
+ *  - dev_refs[p] counts those entries that name page p, and whatever else
+ *    the caller holds it for (a prefix that outlives its sequences); 0 is
+ *    free;
+ *  - a page that is part full belongs to one slot: sharing is of full pages.
+ * Calls on one cache must be ordered on one stream.  Errors found on the
+ * device set a sticky status (hbf_kv_get_status). */
+typedef struct {
+  void *dev_pool;         /* page 0 of plane 0, 16-byte aligned */
+  uint64_t plane_stride;  /* bytes from a page of one plane to the same page of the next */
+  uint64_t page_stride;   /* bytes from page to page of a plane, at least page_tokens * token_bytes */
+  uint64_t token_bytes;   /* bytes of a token in a plane (tokens of a page follow each other);
+                             this and the strides are multiples of 16 */
+  int32_t planes;         /* 1 .. 65535 */
+  int32_t pages;          /* 1 .. 2^20 */
+  int32_t page_tokens;    /* 1 .. 65536 */
+  int32_t slots;          /* 1 .. 2^18 */
+  int32_t table_cols;     /* entries of a row, 1 .. 2^24, table_cols * page_tokens < 2^31 */
+  int64_t table_stride;   /* entries from row to row, >= table_cols */
+  int32_t *dev_refs;      /* [pages] */
+  int32_t *dev_tables;    /* [slots][table_stride] */
+  int32_t *dev_lens;      /* [slots] */
+  void *dev_ws;           /* hbf_kv_workspace_bytes of device memory, 256-byte aligned; its first 256
+                             bytes zero before the first call, kept by the calls from then on */
+} hbf_kv;
+
+/* Bytes of dev_ws for calls of up to max_list list entries (only the sizes in `kv` are looked at). */
+int hbf_kv_workspace_bytes(const hbf_kv *kv, int max_list, size_t *bytes);
+
+/* The lists below are device arrays of n entries, 0 <= n <= 65535 and at most
+ * the workspace's max_list (HBF_ENOWORKSPACE from ws_list < n); ws_list is the
+ * max_list that dev_ws was sized for.  extend, fork, copy and compact check
+ * all their work first: with an entry out of range (HBF_EINVAL) or too few
+ * free pages (HBF_ENOMEM) nothing changes.  Free pages are taken lowest
+ * first, in the list's order.
+ *
+ * extend: slot dev_slots[i] grows by dev_add[i] >= 0 tokens, and gets the
+ *   pages they need.  Refused (HBF_EINVAL): a slot listed twice, a row too
+ *   short, a part-full last page that others hold too.
+ * fork: the empty slot dev_children[i] gets the tokens of dev_parents[i].
+ *   Full pages are shared; the tokens of a part-full last page are copied,
+ *   in every plane, to a page of the child's own.  Refused: a child listed
+ *   twice, not empty, or listed as a parent too.
+ * free: slot dev_slots[i] becomes empty: its entries become -1 and each of
+ *   its pages loses one count.  A slot listed twice is freed once.  Entries
+ *   out of range are left out (HBF_EINVAL), the others are freed.
+ * copy: page dev_dst[i] becomes a copy of page dev_src[i] in every plane;
+ *   counts and tables do not change.  Refused: a destination listed twice or
+ *   that is also a source.
+ * compact: with m pages in use, those numbered m and above move, in order,
+ *   to the free pages below m, in order: the fewest moves that leave [0, m)
+ *   in use.  dev_remap[pages] receives each page's new number, -1 for a free
+ *   one.  Tables and counts are written to dev_tables_out (as dev_tables, same
+ *   stride; entries not in use as they were) and dev_refs_out; NULL: in place.
+ *   Page moves are always in place; a vacated page keeps its bytes. */
+int hbf_kv_extend(const hbf_kv *kv, const int32_t *dev_slots, const int32_t *dev_add, int n, int ws_list, void *stream);
+int hbf_kv_fork(const hbf_kv *kv, const int32_t *dev_parents, const int32_t *dev_children, int n, int ws_list,
+                void *stream);
+int hbf_kv_free(const hbf_kv *kv, const int32_t *dev_slots, int n, void *stream);
+int hbf_kv_copy(const hbf_kv *kv, const int32_t *dev_src, const int32_t *dev_dst, int n, void *stream);
+int hbf_kv_compact(const hbf_kv *kv, int32_t *dev_remap, int32_t *dev_tables_out, int32_t *dev_refs_out,
+                   void *stream);
+
+/* Write tokens' K and V: entry i is token dev_pos[i] of slot dev_slots[i], in
+ * layers first_layer .. first_layer + layers - 1, where layer l's K is plane
+ * 2l and its V plane 2l + 1.  dev_k, dev_v: [layers][n][token_bytes], 16-byte
+ * aligned.  An entry whose slot, position (0 <= pos < length) or page is out
+ * of range is left out (HBF_EINVAL).  Two entries of one token: undefined. */
+int hbf_kv_write(const hbf_kv *kv, int first_layer, int layers, const void *dev_k, const void *dev_v,
+                 const int32_t *dev_slots, const int32_t *dev_pos, int n, void *stream);
+
+/* Synchronise `stream`, then return and clear the cache's sticky status:
+ * HBF_OK, HBF_EINVAL or HBF_ENOMEM (in that order of precedence). */
+int hbf_kv_get_status(const hbf_kv *kv, void *stream);
+
+/* Attention of a batch of rows, one query token each, over cache pages of one
+ * layer.  All rows share one prefix, read once for all of them; each also
+ * sees own tokens:
+ *   s[i] = scale * q . k[i] over the prefix's tokens and the row's own,
+ *   out = sum_i exp(s[i] - lse) v[i],  lse = log sum_i exp(s[i]).
+ * Query head j reads KV head j / (heads / kv_heads).  A row without any token
+ * has out 0 and lse -infinity.  What lies behind a length is not looked at.
+ * The probabilities are rounded to the call's 16-bit type before they meet V
+ * (as fractions of the largest one met so far); nothing else is rounded
+ * before the result. */
+typedef struct {
+  const void *dev_k, *dev_v;  /* page 0, token 0, head 0; 16-byte aligned */
+  int64_t page_stride, token_stride, head_stride;  /* of both, in elements, multiples of 8, >= 0 */
+  int32_t pages, page_tokens; /* as in hbf_kv */
+  int32_t kv_heads;           /* 1 .. 1024 */
+  int32_t head_dim;           /* 64 or 128 */
+  uint32_t dtype;             /* HBF_BF16 or HBF_FP16 */
+} hbf_kv_layer;
+
+typedef struct {
+  const void *dev_q;          /* [rows][heads][head_dim], 16-byte aligned, strides below in elements, multiples of 8 */
+  int64_t q_row_stride, q_head_stride;
+  int32_t rows, heads;        /* 0 .. 65535; a multiple of kv_heads, up to 1024; rows * heads <= 2^22 */
+  float scale;                /* finite */
+  const int32_t *dev_prefix_pages; /* the prefix's pages, ceil(prefix_len / page_tokens) of them; NULL without prefix */
+  int64_t prefix_len;         /* tokens, 0 .. 2^31 - 1 */
+  const int32_t *dev_tables;  /* own pages of row r at r * table_stride; NULL where no row has own tokens */
+  int64_t table_stride;
+  const int32_t *dev_own_len; /* [rows] own tokens, 0 .. max_own; may be NULL if max_own is 0 */
+  int32_t max_own;            /* 0 without own tokens; rows of the table hold that many */
+  void *dev_out;              /* [rows][heads][head_dim], strides as q's, 16-byte aligned */
+  int64_t out_row_stride, out_head_stride;
+  float *dev_lse;             /* [rows][heads], or NULL */
+} hbf_attention;
+
+/* Device scratch of a call, in bytes (only sizes and strides are looked at). */
+int hbf_kv_attention_workspace_bytes(const hbf_kv_layer *kv, const hbf_attention *at, size_t *bytes);
+
+/* dev_status (device, nullable): HBF_EINVAL is stored there if an own length
+ * is outside [0, max_own] or a page id that is read is outside [0, pages);
+ * that row's out and lse (every row's, for a prefix page) are NaN.  Left as it
+ * was otherwise.  dev_ws: 256-byte aligned; a call's contents need not be
+ * kept. */
+int hbf_kv_attention(const hbf_kv_layer *kv, const hbf_attention *at, int32_t *dev_status, void *dev_ws,
+                     size_t ws_bytes, void *stream);
+
+/* A mixture-of-experts layer for a few tokens, all of it:
+ *   logits = x . router[e]  (fp32), the topk largest (ties: the lowest index),
+ *   their weights: the softmax over all experts, with HBF_MOE_RENORM divided
+ *   by the chosen ones' sum;
+ *   h = silu(gate_e x) * (up_e x),  y = sum_j weight_j down_ej h.
+ * h is held as the sum of two 16-bit words (in HBF_FP16 its magnitude is
+ * limited to 65504 as an activation of that type is: beyond, infinity).
+ * Without a router the caller gives the choices: ids[t][j] an expert or -1
+ * (none), and their weights; one expert may be named twice.  A logit that is
+ * NaN counts as the lowest. */
+#define HBF_MOE_RENORM 1u
+typedef struct {
+  int32_t experts;            /* E, 1 .. 1024 */
+  int32_t topk;               /* k, 1 .. min(E, 32) (1 .. 32 without a router) */
+  int32_t hidden, ffn;        /* H, F: multiples of 8, 8 .. 16384 */
+  uint32_t dtype, flags;      /* HBF_BF16 / HBF_FP16; HBF_MOE_* */
+  const void *dev_router;     /* [E][H], or NULL */
+  const void *dev_gate_up;    /* expert e at e * gate_up_stride elements: [2F][H], gate rows then up rows */
+  const void *dev_down;       /* expert e at e * down_stride elements: [H][F] */
+  int64_t gate_up_stride, down_stride; /* multiples of 8; all three 16-byte aligned */
+} hbf_moe;
+
+/* Device scratch of a call of `tokens` tokens, in bytes: 0 .. 128 tokens with
+ * tokens * topk <= 2048 (HBF_EINVAL beyond). */
+int hbf_moe_workspace_bytes(const hbf_moe *moe, int tokens, size_t *bytes);
+
+/* dev_x: [tokens][H], dev_y: [tokens][H], rows x_stride / y_stride elements
+ * apart (multiples of 8), 16-byte aligned.  dev_ids, dev_weights: int32 /
+ * float [tokens][topk], written, or read without a router (an id outside
+ * [-1, E) counts as -1 and stores HBF_EINVAL to dev_status, nullable).
+ * More tokens than above are refused (HBF_EINVAL).  dev_ws: 256-byte aligned,
+ * its first 256 bytes zero before the first call, kept by the calls from
+ * then on; calls that share it must be ordered on one stream. */
+int hbf_moe_layer(const hbf_moe *moe, const void *dev_x, int64_t x_stride, int tokens, int32_t *dev_ids,
+                  float *dev_weights, void *dev_y, int64_t y_stride, int32_t *dev_status, void *dev_ws,
+                  size_t ws_bytes, void *stream);
+
 /* Wall-clock tick of the delay injection, in picoseconds (10,000 for a
  * 100 MHz counter).  Needs the GPU. */
 int hbf_wall_clock_tick_ps(hbf_model_t model, int64_t *tick_ps);

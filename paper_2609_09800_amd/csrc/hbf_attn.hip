@@ -1,0 +1,564 @@
+// Decode attention of a batch whose rows share one prefix, over cache pages.
+//
+// o = sum_i p_i v_i / sum_i p_i with p_i = exp(s_i - m), s_i = scale q.k_i, m a
+// running maximum: one pass over the tokens, and parts of the token axis
+// joined afterwards by their maxima and sums.
+//
+// A KV head's G query heads of all rows meet the same prefix tokens, so the
+// prefix is one product of rows * G queries with its K and V: read once for the
+// batch.  Own tokens are met by one row's G queries.  Both run in one launch,
+// each workgroup taking a part of the token axis for some queries:
+//  - few queries (own tokens; a prefix with at most 32 of them): bound by
+//    memory.  Each of four waves takes 32 tokens at a time, K straight from
+//    memory into the matrix operand, V through LDS for its transpose, the next
+//    tokens' loads in flight meanwhile; the waves meet once, at the end.
+//  - many queries: bound by the matrix cores and the LDS.  64 tokens are staged
+//    for four waves of 32 queries each.
+// Scores are computed transposed, S^T = K Q^T: a lane then holds one query's
+// scores of four consecutive tokens per tile of 16, which, rounded, are
+// already the operand of O^T = V^T P^T (the order of the tokens within a step
+// is free as long as V's are read in the same one), so P never leaves its lane.
+#include <math.h>
+
+#include <algorithm>
+
+#include "hbf_half.h"
+#include "hbf_ops.h"
+
+namespace hbf {
+namespace {
+
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int FEW_TILE = 32;    // tokens of a wave's step where queries are few
+constexpr int MANY_TILE = 64;   // tokens staged where they are many
+constexpr int MANY_Q = 128;     // queries per workgroup there
+constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
+
+struct Args {
+  hbf_kv_layer kv;
+  hbf_attention at;
+  int group;            // query heads per KV head
+  float c;              // scale * log2(e)
+  int few_q;            // the prefix's queries per workgroup if they are few (16 or 32), else 0
+  int m_tiles;          // workgroups across the prefix's queries
+  int prefix_splits;
+  int prefix_chunk;     // tokens per part
+  int prefix_blocks;    // workgroups of the prefix, before the own ones
+  int own_splits, own_chunk, own_tiles;  // own_tiles: workgroups across a row's query heads of one KV head
+  float *part;          // [splits][rows][heads][head_dim] sums of p v
+  float2 *part_ml;      // [splits][rows][heads] maximum (of s log2 e) and sum
+  int32_t *status;
+};
+
+template <int D>
+__device__ __forceinline__ int swizzle(int token) {  // spreads a column of 16-byte pieces over the banks
+  return D == 128 ? token & 15 : (token >> 1) & 7;
+}
+// Byte offset of 16-byte piece `piece` of a token in a staged tile.
+template <int D>
+__device__ __forceinline__ int tile_at(int token, int piece) {
+  return token * (D * 2) + ((piece ^ swizzle<D>(token)) << 4);
+}
+// The lane's operand of V^T: dimensions 16 dt .. + 15, tokens t0 .. + 3 and t1 .. + 3.
+template <int D>
+__device__ __forceinline__ u32x4 v_operand(const char *v, int t0, int t1, int dt, int lane) {
+  const int i = lane & 15, piece = dt * 2 + ((i & 3) >> 1), half = (i & 1) << 3;
+  const u32x2 a = read_transposed(v + tile_at<D>(t0 + (i >> 2), piece) + half);
+  const u32x2 b = read_transposed(v + tile_at<D>(t1 + (i >> 2), piece) + half);
+  return u32x4{a[0], a[1], b[0], b[1]};
+}
+
+__device__ __forceinline__ float max_of_groups(float x) {  // over the four lanes of a query
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float sum_of_groups(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// One step of the running softmax for one query (column): U tiles of 16 tokens'
+// scores s (already times c, masked with -infinity) become probabilities.
+// Returns the factor for what was summed before.
+template <int U>
+__device__ __forceinline__ float softmax_step(f32x4 *s, float &m, float &l) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; u++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) mx = fmaxf(mx, s[u][i]);
+  mx = fmaxf(m, max_of_groups(mx));
+  const float ref = mx == -INFINITY ? 0.f : mx;  // nothing seen yet: every p is 0
+  const float alpha = __builtin_amdgcn_exp2f(m - ref);
+  m = mx;
+  l *= alpha;
+#pragma unroll
+  for (int u = 0; u < U; u++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      s[u][i] = __builtin_amdgcn_exp2f(s[u][i] - ref);
+      l += s[u][i];
+    }
+  return alpha;
+}
+
+template <typename T>
+__device__ __forceinline__ u32x4 p_operand(f32x4 a, f32x4 b) {
+  return u32x4{pack2<T>(a[0], a[1]), pack2<T>(a[2], a[3]), pack2<T>(b[0], b[1]), pack2<T>(b[2], b[3])};
+}
+
+// Page of a token, with a page id out of range noted and page 0 read instead.
+__device__ __forceinline__ int page_of(const Args &a, const int32_t *pages, uint32_t token, bool *bad) {
+  const int p = pages[token / (uint32_t)a.kv.page_tokens];
+  if (p >= 0 && p < a.kv.pages) return p;
+  *bad = true;
+  return 0;
+}
+__device__ __forceinline__ int64_t token_at(const Args &a, int page, uint32_t token, int head) {
+  return (int64_t)page * a.kv.page_stride + (int64_t)(token % (uint32_t)a.kv.page_tokens) * a.kv.token_stride +
+         (int64_t)head * a.kv.head_stride;
+}
+
+struct Query {
+  int row, head;  // row < 0: none
+};
+__device__ __forceinline__ int64_t part_slot(const Args &a, int split, Query q) {
+  return ((int64_t)split * a.at.rows + q.row) * a.at.heads + q.head;
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void load_query(const Args &a, Query q, int kgroup, u32x4 *out) {
+  const char *p = (const char *)a.at.dev_q +
+                  2 * ((q.row < 0 ? 0 : q.row) * a.at.q_row_stride + (q.row < 0 ? 0 : q.head) * a.at.q_head_stride);
+#pragma unroll
+  for (int k = 0; k < D / 32; k++) {
+    const u32x4 v = *(const u32x4 *)(p + (k * 32 + kgroup * 8) * 2);
+    out[k] = q.row < 0 ? u32x4{0, 0, 0, 0} : v;
+  }
+}
+
+// ------------------------------------------------------------ few queries
+
+// Tokens [t0, t1) (t0 < t1) of a page list for 16 QT queries, one per column;
+// query(col) names them.
+template <typename T, int D, int QT, typename Q>
+__device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t1, int head, int split, Q query,
+                    char *lds) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
+  constexpr int KS = D / 32, DT = D / 16;
+  u32x4 qv[QT][KS];
+#pragma unroll
+  for (int q = 0; q < QT; q++) load_query<T, D>(a, query(q * 16 + col), kg, qv[q]);
+  f32x4 o[QT][DT];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int q = 0; q < QT; q++) {
+    m[q] = -INFINITY;
+    l[q] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  char *vt = lds + w * FEW_TILE * D * 2;
+  bool bad = false;
+  uint32_t base = t0 + w * FEW_TILE;
+  u32x4 kv[2][KS], vv[2][KS];
+  int page[2];
+  auto find = [&](uint32_t b) {
+#pragma unroll
+    for (int u = 0; u < 2; u++) page[u] = page_of(a, pages, min(b + u * 16 + col, t1 - 1), &bad);
+  };
+  auto load = [&](uint32_t b) {
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      const int64_t at = 2 * (token_at(a, page[u], min(b + u * 16 + col, t1 - 1), head) + kg * 8);
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+        kv[u][k] = *(const u32x4 *)((const char *)a.kv.dev_k + at + k * 64);
+        vv[u][k] = *(const u32x4 *)((const char *)a.kv.dev_v + at + k * 64);
+      }
+    }
+  };
+  constexpr uint32_t STEP = WAVES * FEW_TILE;
+  if (base < t1) {
+    find(base);
+    load(base);
+    if (t1 - base > STEP) find(base + STEP);
+    while (true) {
+      const bool more = t1 - base > STEP;
+      f32x4 s[QT][2];
+#pragma unroll
+      for (int q = 0; q < QT; q++)
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+          s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < KS; k++) s[q][u] = T::mfma(kv[u][k], qv[q][k], s[q][u]);
+        }
+      const bool tail = t1 - base < FEW_TILE;
+#pragma unroll
+      for (int u = 0; u < 2; u++) {
+        // what lies behind the last token may be anything: 0 * NaN must not reach the sums
+        const bool on = !tail || base + u * 16 + col < t1;
+#pragma unroll
+        for (int k = 0; k < KS; k++)
+          *(u32x4 *)(vt + tile_at<D>(u * 16 + col, k * 4 + kg)) = on ? vv[u][k] : u32x4{0, 0, 0, 0};
+      }
+      wave_lds_fence();
+      if (more) {
+        load(base + STEP);
+        if (t1 - base > 2 * STEP) find(base + 2 * STEP);
+      }
+      u32x4 p[QT];
+      float alpha[QT];
+#pragma unroll
+      for (int q = 0; q < QT; q++) {
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            const float x = s[q][u][i] * a.c;
+            s[q][u][i] = !tail || base + u * 16 + kg * 4 + i < t1 ? x : -INFINITY;
+          }
+        alpha[q] = softmax_step<2>(s[q], m[q], l[q]);
+        p[q] = p_operand<T>(s[q][0], s[q][1]);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; d++) {
+        const u32x4 v = v_operand<D>(vt, kg * 4, 16 + kg * 4, d, lane);
+#pragma unroll
+        for (int q = 0; q < QT; q++) {
+          o[q][d] *= alpha[q];
+          o[q][d] = T::mfma(v, p[q], o[q][d]);
+        }
+      }
+      wave_lds_fence();
+      if (!more) break;
+      base += STEP;
+    }
+  }
+  // the waves' parts become one: 16 queries at a time through LDS
+  constexpr int RS = D + 4;  // a query's row, padded against bank conflicts
+  float *ro = (float *)lds;  // [WAVES][16][RS], then the maxima and sums
+  float2 *rml = (float2 *)(lds + WAVES * 16 * RS * 4);
+  const bool any_bad = __syncthreads_or(bad);
+  if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
+#pragma unroll
+  for (int q = 0; q < QT; q++) {
+    const float lq = sum_of_groups(l[q]);
+    if (kg == 0) rml[w * 16 + col] = make_float2(m[q], lq);
+#pragma unroll
+    for (int d = 0; d < DT; d++) *(f32x4 *)(ro + (w * 16 + col) * RS + d * 16 + kg * 4) = o[q][d];
+    __syncthreads();
+    const int n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 4;
+    const Query qq = query(q * 16 + n);
+    if (qq.row >= 0) {
+      float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < WAVES; i++) mx = fmaxf(mx, rml[i * 16 + n].x);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      float f[WAVES];
+#pragma unroll
+      for (int i = 0; i < WAVES; i++) {
+        f[i] = __builtin_amdgcn_exp2f(rml[i * 16 + n].x - ref);
+        sum += f[i] * rml[i * 16 + n].y;
+      }
+      const int64_t slot = part_slot(a, split, qq);
+#pragma unroll
+      for (int d = d0; d < D; d += 64) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < WAVES; i++) x += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
+        *(f32x4 *)(a.part + slot * D + d) = x;
+      }
+      if (d0 == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum);
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------ many queries
+
+// Tokens [t0, t1) (t0 < t1) of the prefix for MANY_Q queries from m0 on.
+template <typename T, int D>
+__device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int split, int m0, char *lds) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
+  constexpr int KS = D / 32, DT = D / 16, QT = 2, U = MANY_TILE / 16;
+  constexpr int TILE_BYTES = MANY_TILE * D * 2;
+  auto query = [&](int n) {
+    const int mm = m0 + n;
+    const int row = mm / a.group;
+    return row < a.at.rows ? Query{row, head * a.group + mm - row * a.group} : Query{-1, 0};
+  };
+  u32x4 qv[QT][KS];
+#pragma unroll
+  for (int q = 0; q < QT; q++) load_query<T, D>(a, query(w * 32 + q * 16 + col), kg, qv[q]);
+  f32x4 o[QT][DT];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int q = 0; q < QT; q++) {
+    m[q] = -INFINITY;
+    l[q] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // staging: four threads per token, each every fourth 16-byte piece
+  const int st = threadIdx.x >> 2, sp = threadIdx.x & 3;
+  constexpr int SP = D / 32;
+  u32x4 kv[SP], vv[SP];
+  bool bad = false;
+  int page = 0;
+  auto find = [&](uint32_t b) { page = page_of(a, a.at.dev_prefix_pages, min(b + st, t1 - 1), &bad); };
+  auto load = [&](uint32_t b) {
+    const int64_t at = 2 * (token_at(a, page, min(b + st, t1 - 1), head) + sp * 8);
+#pragma unroll
+    for (int k = 0; k < SP; k++) {
+      kv[k] = *(const u32x4 *)((const char *)a.kv.dev_k + at + k * 64);
+      vv[k] = *(const u32x4 *)((const char *)a.kv.dev_v + at + k * 64);
+    }
+  };
+  auto store = [&](uint32_t b, char *buf) {
+    const bool on = b + st < t1;  // behind the last token: zero, whatever lies there
+#pragma unroll
+    for (int k = 0; k < SP; k++) {
+      *(u32x4 *)(buf + tile_at<D>(st, k * 4 + sp)) = kv[k];
+      *(u32x4 *)(buf + TILE_BYTES + tile_at<D>(st, k * 4 + sp)) = on ? vv[k] : u32x4{0, 0, 0, 0};
+    }
+  };
+  find(t0);
+  load(t0);
+  store(t0, lds);
+  if (t1 - t0 > MANY_TILE) {
+    find(t0 + MANY_TILE);
+    load(t0 + MANY_TILE);
+    if (t1 - t0 > 2 * MANY_TILE) find(t0 + 2 * MANY_TILE);
+  }
+  __syncthreads();
+  int cur = 0;
+  for (uint32_t base = t0;; base += MANY_TILE) {
+    const char *kt = lds + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+    f32x4 s[QT][U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+#pragma unroll
+      for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; k++) {
+        const u32x4 kk = *(const u32x4 *)(kt + tile_at<D>(u * 16 + col, k * 4 + kg));
+#pragma unroll
+        for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
+      }
+    }
+    const bool tail = t1 - base < MANY_TILE;
+    float alpha[QT];
+    u32x4 p[QT][U / 2];
+#pragma unroll
+    for (int q = 0; q < QT; q++) {
+#pragma unroll
+      for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const float x = s[q][u][i] * a.c;
+          s[q][u][i] = !tail || base + u * 16 + kg * 4 + i < t1 ? x : -INFINITY;
+        }
+      alpha[q] = softmax_step<U>(s[q], m[q], l[q]);
+#pragma unroll
+      for (int u = 0; u < U / 2; u++) p[q][u] = p_operand<T>(s[q][2 * u], s[q][2 * u + 1]);
+    }
+#pragma unroll
+    for (int d = 0; d < DT; d++) {
+#pragma unroll
+      for (int q = 0; q < QT; q++) o[q][d] *= alpha[q];
+#pragma unroll
+      for (int u = 0; u < U / 2; u++) {
+        const u32x4 v = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
+#pragma unroll
+        for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][u], o[q][d]);
+      }
+    }
+    if (t1 - base <= MANY_TILE) break;
+    const uint32_t next = base + MANY_TILE;
+    store(next, lds + (cur ^ 1) * 2 * TILE_BYTES);
+    if (t1 - next > MANY_TILE) {
+      load(next + MANY_TILE);
+      if (t1 - next > 2 * MANY_TILE) find(next + 2 * MANY_TILE);
+    }
+    __syncthreads();
+    cur ^= 1;
+  }
+  const bool any_bad = __syncthreads_or(bad);
+  if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
+#pragma unroll
+  for (int q = 0; q < QT; q++) {
+    const Query qq = query(w * 32 + q * 16 + col);
+    const float lq = sum_of_groups(l[q]);
+    if (qq.row < 0) continue;
+    const int64_t slot = part_slot(a, split, qq);
+#pragma unroll
+    for (int d = 0; d < DT; d++) *(f32x4 *)(a.part + slot * D + d * 16 + kg * 4) = o[q][d];
+    if (kg == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(m[q], lq);
+  }
+}
+
+template <int D>
+constexpr int lds_bytes() {
+  const int many_b = 4 * MANY_TILE * D * 2, few_b = WAVES * FEW_TILE * D * 2;
+  const int join_b = WAVES * 16 * (D + 4) * 4 + WAVES * 16 * 8;
+  return many_b > few_b ? (many_b > join_b ? many_b : join_b) : (few_b > join_b ? few_b : join_b);
+}
+
+// Workgroups [0, prefix_blocks): the prefix, those of one part and KV head on
+// one XCD (block numbers equal modulo 8) so that they share its L2.  Then the
+// own tokens'.
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
+  __shared__ __align__(16) char lds[lds_bytes<D>()];
+  int b = blockIdx.x;
+  if (b < a.prefix_blocks) {
+    const int sh = b / (8 * a.m_tiles) * 8 + b % 8, mt = b / 8 % a.m_tiles;
+    if (sh >= a.prefix_splits * a.kv.kv_heads) return;
+    const int head = sh % a.kv.kv_heads, split = sh / a.kv.kv_heads;
+    const uint32_t t0 = (uint32_t)split * (uint32_t)a.prefix_chunk;
+    const uint32_t t1 = min(t0 + (uint32_t)a.prefix_chunk, (uint32_t)a.at.prefix_len);
+    if (a.few_q == 0) {
+      many<T, D>(a, t0, t1, head, split, mt * MANY_Q, lds);
+      return;
+    }
+    const int m0 = mt * a.few_q;
+    auto query = [&](int n) {
+      const int mm = m0 + n, row = mm / a.group;
+      return row < a.at.rows ? Query{row, head * a.group + mm - row * a.group} : Query{-1, 0};
+    };
+    if (a.few_q == 16)
+      few<T, D, 1>(a, a.at.dev_prefix_pages, t0, t1, head, split, query, lds);
+    else
+      few<T, D, 2>(a, a.at.dev_prefix_pages, t0, t1, head, split, query, lds);
+    return;
+  }
+  b -= a.prefix_blocks;
+  const int tile = b % a.own_tiles;
+  b /= a.own_tiles;
+  const int head = b % a.kv.kv_heads;
+  b /= a.kv.kv_heads;
+  const int row = b % a.at.rows, split = b / a.at.rows;
+  const int len = a.at.dev_own_len[row];
+  if (len < 0 || len > a.at.max_own) {
+    if (threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
+    return;
+  }
+  const uint32_t t0 = (uint32_t)split * (uint32_t)a.own_chunk;
+  if (t0 >= (uint32_t)len) return;
+  auto query = [&](int n) {
+    const int g = tile * 16 + n;
+    return g < a.group ? Query{row, head * a.group + g} : Query{-1, 0};
+  };
+  few<T, D, 1>(a, a.at.dev_tables + (int64_t)row * a.at.table_stride, t0,
+               min(t0 + (uint32_t)a.own_chunk, (uint32_t)len), head, a.prefix_splits + split, query, lds);
+}
+
+// Join a query's parts, a wave each.
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS) void k_attn_join(Args a) {
+  const int64_t qi = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
+  if (qi >= (int64_t)a.at.rows * a.at.heads) return;
+  const int lane = threadIdx.x & 63;
+  const int row = (int)(qi / a.at.heads), head = (int)(qi - (int64_t)row * a.at.heads);
+  int own = 0;
+  bool bad = false;
+  if (a.at.dev_own_len) {
+    const int len = a.at.dev_own_len[row];
+    bad = len < 0 || len > a.at.max_own;
+    if (!bad && len > 0) own = (int)(((uint32_t)len + (uint32_t)a.own_chunk - 1) / (uint32_t)a.own_chunk);
+  }
+  const int n = a.prefix_splits + own;
+  const int64_t stride = (int64_t)a.at.rows * a.at.heads;
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 64) {
+    const float x = a.part_ml[i * stride + qi].x;
+    bad |= isnan(x);
+    m = fmaxf(m, x);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  bad = __any(bad);
+  if (bad && a.status && lane == 0) *a.status = HBF_EINVAL;
+  const float ref = m == -INFINITY ? 0.f : m;
+  constexpr int V = D / 64;
+  float o[V], l = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; v++) o[v] = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < n; i++) {
+    const float2 ml = a.part_ml[i * stride + qi];
+    const float *p = a.part + (i * stride + qi) * D + lane * V;
+    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+    l += f * ml.y;
+#pragma unroll
+    for (int v = 0; v < V; v++) o[v] += f * p[v];
+  }
+  if (bad) l = NAN;
+  const float inv = n == 0 ? 0.f : 1.f / l;
+  typename T::elem *out =
+      (typename T::elem *)a.at.dev_out + row * a.at.out_row_stride + head * a.at.out_head_stride + lane * V;
+#pragma unroll
+  for (int v = 0; v < V; v++) out[v] = (typename T::elem)(bad ? NAN : o[v] * inv);
+  if (a.at.dev_lse && lane == 0)
+    a.at.dev_lse[qi] = bad ? NAN : n == 0 ? -INFINITY : m * LN2 + logf(l);
+}
+
+// Sizes of a call: how the token axes are cut.
+Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
+  Args a{};
+  a.kv = kv;
+  a.at = at;
+  a.group = at.heads / kv.kv_heads;
+  a.c = at.scale * LOG2E;
+  const int64_t m = (int64_t)at.rows * a.group;
+  a.few_q = m <= 16 ? 16 : m <= 32 ? 32 : 0;
+  a.m_tiles = (int)(a.few_q ? 1 : (m + MANY_Q - 1) / MANY_Q);
+  a.own_tiles = (a.group + 15) / 16;
+  // parts so that the chip's 256 CUs have two workgroups each, no shorter than a step of the waves
+  constexpr int64_t WANT = 512;
+  auto cut = [](int64_t tokens, int64_t others, int64_t step, int *chunk) {
+    if (tokens <= 0 || others <= 0) return 0;
+    int64_t n = (WANT + others - 1) / others;
+    n = std::max<int64_t>(1, std::min(n, (tokens + step - 1) / step));
+    int64_t c = (tokens + n - 1) / n;
+    c = (c + step - 1) / step * step;
+    *chunk = (int)std::min<int64_t>(c, INT32_MAX / 2 / step * step);
+    return (int)((tokens + *chunk - 1) / *chunk);
+  };
+  a.prefix_splits = cut(at.prefix_len, (int64_t)kv.kv_heads * a.m_tiles, a.few_q ? 4 * FEW_TILE : MANY_TILE,
+                        &a.prefix_chunk);
+  a.own_splits = cut(at.max_own, (int64_t)at.rows * kv.kv_heads * a.own_tiles, 4 * FEW_TILE, &a.own_chunk);
+  a.prefix_blocks = (a.prefix_splits * kv.kv_heads + 7) / 8 * 8 * a.m_tiles;
+  return a;
+}
+
+template <typename T, int D>
+hipError_t run(const Args &a, hipStream_t s) {
+  const int64_t blocks =
+      a.prefix_blocks + (int64_t)a.own_splits * a.at.rows * a.kv.kv_heads * a.own_tiles;
+  if (blocks > 0) k_attn<T, D><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+  k_attn_join<T, D><<<(uint32_t)(((int64_t)a.at.rows * a.at.heads + WAVES - 1) / WAVES), THREADS, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_ws_bytes(const hbf_kv_layer &kv, const hbf_attention &at) {
+  const Args a = plan(kv, at);
+  const size_t slots = (size_t)(a.prefix_splits + a.own_splits) * at.rows * at.heads;
+  return slots * ((size_t)kv.head_dim * 4 + 8) + 256;
+}
+
+hipError_t launch_attn(const hbf_kv_layer &kv, const hbf_attention &at, int32_t *status, void *ws, hipStream_t s) {
+  Args a = plan(kv, at);
+  const size_t slots = (size_t)(a.prefix_splits + a.own_splits) * at.rows * at.heads;
+  a.part = (float *)ws;
+  a.part_ml = (float2 *)((char *)ws + slots * kv.head_dim * 4);
+  a.status = status;
+  if (kv.dtype == HBF_BF16) return kv.head_dim == 64 ? run<Bf16, 64>(a, s) : run<Bf16, 128>(a, s);
+  return kv.head_dim == 64 ? run<Fp16, 64>(a, s) : run<Fp16, 128>(a, s);
+}
+
+}  // namespace hbf

@@ -1,0 +1,58 @@
+// The two 16-bit types of the decode-layer operators: conversions, the matrix
+// instruction and the transposing LDS read.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace hbf {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+struct Bf16 {
+  typedef __bf16 elem;
+  typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+  // D[16 x 16] += A[16 x 32] B[32 x 16]: lane l holds A's row l % 16 and B's
+  // column l % 16 at k = 8 (l / 16) .. + 7, and D's column l % 16 at rows
+  // 4 (l / 16) .. + 3.
+  static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+};
+struct Fp16 {
+  typedef _Float16 elem;
+  typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+};
+
+// Two values rounded to nearest even, the first in the low half.
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typename T::x2 v;
+  v[0] = (typename T::elem)lo;
+  v[1] = (typename T::elem)hi;
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// A 16-lane group reads a 4 x 16 block of 16-bit values, lane i the 8 bytes at
+// `at` (row i / 4, columns 4 (i % 4) .. + 3), and lane i receives column i.
+__device__ __forceinline__ u32x2 read_transposed(const void *at) {
+  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)at));
+}
+
+// What the lanes of one wave have written to LDS is read by others of it: the
+// LDS serves a wave's accesses in order, so only the compiler is held.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+}  // namespace hbf

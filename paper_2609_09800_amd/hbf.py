@@ -35,9 +35,15 @@ EXPORTED = [
     "hbf_cache_create", "hbf_cache_destroy", "hbf_cache_reset", "hbf_cache_access", "hbf_cache_sweep",
     "hbf_cache_set_chunk", "hbf_cache_get_chunk",
     "hbf_time_requests_noalloc", "hbf_vmem_configure",
+    "hbf_kv_workspace_bytes", "hbf_kv_extend", "hbf_kv_fork", "hbf_kv_free", "hbf_kv_copy", "hbf_kv_compact",
+    "hbf_kv_write", "hbf_kv_get_status", "hbf_kv_attention_workspace_bytes", "hbf_kv_attention",
+    "hbf_moe_workspace_bytes", "hbf_moe_layer",
 ]
 HBF_NOALLOC_SCRATCH_BYTES = 64 << 20
 REFRESH_PENDING = -1
+HBF_BF16 = 0
+HBF_FP16 = 1
+HBF_MOE_RENORM = 1
 
 
 class hbf_params(ctypes.Structure):
@@ -50,6 +56,38 @@ class hbf_params(ctypes.Structure):
 class hbf_refresh_block(ctypes.Structure):
     _fields_ = [("epoch", ctypes.c_uint32), ("zone", ctypes.c_uint32), ("channel", ctypes.c_uint32),
                 ("die", ctypes.c_uint32), ("plane", ctypes.c_uint32), ("block", ctypes.c_uint32)]
+
+
+class hbf_kv(ctypes.Structure):
+    _fields_ = [("dev_pool", ctypes.c_void_p), ("plane_stride", ctypes.c_uint64), ("page_stride", ctypes.c_uint64),
+                ("token_bytes", ctypes.c_uint64), ("planes", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("slots", ctypes.c_int32), ("table_cols", ctypes.c_int32),
+                ("table_stride", ctypes.c_int64), ("dev_refs", ctypes.c_void_p), ("dev_tables", ctypes.c_void_p),
+                ("dev_lens", ctypes.c_void_p), ("dev_ws", ctypes.c_void_p)]
+
+
+class hbf_kv_layer(ctypes.Structure):
+    _fields_ = [("dev_k", ctypes.c_void_p), ("dev_v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("pages", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_uint32)]
+
+
+class hbf_attention(ctypes.Structure):
+    _fields_ = [("dev_q", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("rows", ctypes.c_int32), ("heads", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("dev_prefix_pages", ctypes.c_void_p), ("prefix_len", ctypes.c_int64),
+                ("dev_tables", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("dev_own_len", ctypes.c_void_p), ("max_own", ctypes.c_int32), ("dev_out", ctypes.c_void_p),
+                ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("dev_lse", ctypes.c_void_p)]
+
+
+class hbf_moe(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("topk", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("ffn", ctypes.c_int32), ("dtype", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+                ("dev_router", ctypes.c_void_p), ("dev_gate_up", ctypes.c_void_p), ("dev_down", ctypes.c_void_p),
+                ("gate_up_stride", ctypes.c_int64), ("down_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -98,6 +136,21 @@ def load_library(path=LIB_PATH):
         "hbf_cache_sweep": ([vp, vp, i32, u64, vp, i64, vp, vp], i32),
         "hbf_cache_set_chunk": ([vp, u32], i32),
         "hbf_cache_get_chunk": ([vp, ctypes.POINTER(u32)], i32),
+        "hbf_kv_workspace_bytes": ([ctypes.POINTER(hbf_kv), i32, ctypes.POINTER(ctypes.c_size_t)], i32),
+        "hbf_kv_extend": ([ctypes.POINTER(hbf_kv), vp, vp, i32, i32, vp], i32),
+        "hbf_kv_fork": ([ctypes.POINTER(hbf_kv), vp, vp, i32, i32, vp], i32),
+        "hbf_kv_free": ([ctypes.POINTER(hbf_kv), vp, i32, vp], i32),
+        "hbf_kv_copy": ([ctypes.POINTER(hbf_kv), vp, vp, i32, vp], i32),
+        "hbf_kv_compact": ([ctypes.POINTER(hbf_kv), vp, vp, vp, vp], i32),
+        "hbf_kv_write": ([ctypes.POINTER(hbf_kv), i32, i32, vp, vp, vp, vp, i32, vp], i32),
+        "hbf_kv_get_status": ([ctypes.POINTER(hbf_kv), vp], i32),
+        "hbf_kv_attention_workspace_bytes": ([ctypes.POINTER(hbf_kv_layer), ctypes.POINTER(hbf_attention),
+                                              ctypes.POINTER(ctypes.c_size_t)], i32),
+        "hbf_kv_attention": ([ctypes.POINTER(hbf_kv_layer), ctypes.POINTER(hbf_attention), vp, vp, ctypes.c_size_t,
+                              vp], i32),
+        "hbf_moe_workspace_bytes": ([ctypes.POINTER(hbf_moe), i32, ctypes.POINTER(ctypes.c_size_t)], i32),
+        "hbf_moe_layer": ([ctypes.POINTER(hbf_moe), vp, i64, i32, vp, vp, vp, i64, vp, vp, ctypes.c_size_t, vp],
+                          i32),
     }
     for name, (args, res) in sig.items():
         f = getattr(lib, name)
@@ -420,6 +473,314 @@ def cache_sweep(frames, prefetch, range_pages, pages, counts, stream=None):
     _dev(counts, "counts", _I64, numel=5 * f.size, at_least=True)
     return lib.hbf_cache_sweep(f.ctypes.data_as(ctypes.c_void_p), d.ctypes.data_as(ctypes.c_void_p), f.size,
                                range_pages, _dp(pages), pages.numel(), _dp(counts), _sp(stream))
+
+
+_I32 = ("int32",)
+_HALF = ("bfloat16", "float16")
+
+
+def _strided(t, what, dtypes, dim, inner=1):
+    """As _dev, for a tensor of `dim` dimensions whose last `inner` are
+    contiguous and whose others may be strided (by 16-byte multiples)."""
+    import torch
+    bad = None
+    if not isinstance(t, torch.Tensor):
+        bad = f"not a tensor ({type(t).__name__})"
+    elif not t.is_cuda:
+        bad = "not in GPU memory"
+    elif str(t.dtype).replace("torch.", "") not in dtypes:
+        bad = f"dtype {t.dtype}, expected {'/'.join(dtypes)}"
+    elif t.dim() != dim:
+        bad = f"{t.dim()} dimensions, expected {dim}"
+    elif t.numel():
+        want = 1
+        for d in range(dim - 1, dim - 1 - inner, -1):
+            if t.shape[d] != 1 and t.stride(d) != want:
+                bad = f"strides {tuple(t.stride())}: the last {inner} dimension(s) must be contiguous"
+            want *= t.shape[d]
+        if any(t.stride(d) * t.element_size() % 16 for d in range(dim - inner) if t.shape[d] > 1):
+            bad = f"strides {tuple(t.stride())}: not multiples of 16 bytes"
+    if bad is not None:
+        raise HbfError(HBF_EINVAL, f"{what}: {bad}")
+    return t
+
+
+def _writable(t, what):
+    """An output whose elements must not share memory (an expanded tensor's do)."""
+    if any(t.stride(d) == 0 and t.shape[d] > 1 for d in range(t.dim())):
+        raise HbfError(HBF_EINVAL, f"{what}: an expanded tensor cannot be written")
+    return t
+
+
+class _Scratch:
+    """Device scratch that grows with the calls' needs."""
+
+    def __init__(self):
+        self._t = None
+
+    def get(self, nbytes, device, stream):
+        import torch
+        s = stream if stream is not None else torch.cuda.current_stream(device)
+        if self._t is None or self._t.numel() < nbytes or self._t.device != device:
+            # (the allocator takes the old block back once the streams it was used on are through with it)
+            self._t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+        self._t.record_stream(s)
+        return self._t
+
+
+def _stride(t, d):
+    """Stride of a dimension in elements; of one of a single entry, which is never taken, 0."""
+    return t.stride(d) if t.shape[d] > 1 else 0
+
+
+def _zeroed(nbytes, device):
+    """Device bytes, the first 256 zero and seen so by every stream."""
+    import torch
+    t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    t[:256].zero_()
+    torch.cuda.current_stream(device).synchronize()
+    return t
+
+
+def _dtype_code(t):
+    import torch
+    return HBF_BF16 if t.dtype == torch.bfloat16 else HBF_FP16
+
+
+class KvPages:
+    """A KV cache of pages on the current GPU (reading in include/hbf.h).
+
+    pool: bfloat16 or float16 [layers, 2, pages, page_tokens, kv_heads,
+    head_dim], contiguous; index 0 of the second dimension is K, 1 is V.
+    refs: int32 [pages]; tables: int32 [slots, entries] (rows may be strided);
+    lens: int32 [slots].  All stay the caller's; a cache that only
+    prefix_attention reads needs the pool alone.  max_list: the longest list
+    that extend and fork will be given.  Calls on one object must be ordered
+    on one stream."""
+
+    def __init__(self, pool, refs=None, tables=None, lens=None, max_list=1024):
+        import torch
+        self._lib = load_library()
+        _dev(pool, "pool", _HALF)
+        if pool.dim() != 6 or pool.shape[1] != 2 or 0 in pool.shape:
+            raise HbfError(HBF_EINVAL, f"pool: shape {tuple(pool.shape)}, expected "
+                                       "[layers, 2, pages, page_tokens, kv_heads, head_dim]")
+        self.pool, self.refs, self.tables, self.lens = pool, refs, tables, lens
+        self.layers, _, self.pages, self.page_tokens, self.kv_heads, self.head_dim = pool.shape
+        self._attn_ws = _Scratch()
+        self._attn_status = _zeroed(256, pool.device)[:4].view(torch.int32)
+        self._kv = None
+        if refs is None and tables is None and lens is None:
+            return
+        _dev(refs, "refs", _I32, shape=(self.pages,))
+        if not isinstance(tables, torch.Tensor) or not tables.is_cuda or tables.dtype != torch.int32 \
+                or tables.dim() != 2 or 0 in tables.shape or (tables.shape[1] > 1 and tables.stride(1) != 1) \
+                or (tables.shape[0] > 1 and tables.stride(0) < tables.shape[1]):
+            raise HbfError(HBF_EINVAL, "tables: expected int32 [slots, entries] in GPU memory, rows contiguous")
+        _dev(lens, "lens", _I32, shape=(tables.shape[0],))
+        tok = self.kv_heads * self.head_dim * 2
+        self.max_list = int(max_list)
+        self._kv = hbf_kv(pool.data_ptr(), tok * self.page_tokens * self.pages, tok * self.page_tokens, tok,
+                          self.layers * 2, self.pages, self.page_tokens, tables.shape[0], tables.shape[1],
+                          max(tables.stride(0), tables.shape[1]), refs.data_ptr(), tables.data_ptr(),
+                          lens.data_ptr(), None)
+        b = ctypes.c_size_t()
+        _check(self._lib.hbf_kv_workspace_bytes(ctypes.byref(self._kv), self.max_list, ctypes.byref(b)),
+               "hbf_kv_workspace_bytes")
+        self._ws = _zeroed(b.value, pool.device)
+        self._kv.dev_ws = self._ws.data_ptr()
+
+    def _desc(self):
+        if self._kv is None:
+            raise HbfError(HBF_EINVAL, "this KvPages was made without refs, tables and lens")
+        return ctypes.byref(self._kv)
+
+    def extend(self, slots, add, stream=None):
+        """Slot slots[i] grows by add[i] tokens (int32 device tensors [n])."""
+        d = self._desc()
+        n = _dev(slots, "slots", _I32).numel()
+        _dev(add, "add", _I32, numel=n)
+        return self._lib.hbf_kv_extend(d, _dp(slots), _dp(add), n, self.max_list, _sp(stream))
+
+    def fork(self, parents, children, stream=None):
+        """The empty slot children[i] gets parents[i]'s tokens (int32 [n])."""
+        d = self._desc()
+        n = _dev(parents, "parents", _I32).numel()
+        _dev(children, "children", _I32, numel=n)
+        return self._lib.hbf_kv_fork(d, _dp(parents), _dp(children), n, self.max_list, _sp(stream))
+
+    def free(self, slots, stream=None):
+        """Slots (int32 [n]) become empty and give their pages back."""
+        d = self._desc()
+        n = _dev(slots, "slots", _I32).numel()
+        return self._lib.hbf_kv_free(d, _dp(slots), n, _sp(stream))
+
+    def copy(self, src, dst, stream=None):
+        """Pages dst[i] become copies of pages src[i] (int32 [n])."""
+        d = self._desc()
+        n = _dev(src, "src", _I32).numel()
+        _dev(dst, "dst", _I32, numel=n)
+        return self._lib.hbf_kv_copy(d, _dp(src), _dp(dst), n, _sp(stream))
+
+    def compact(self, remap, tables_out=None, refs_out=None, stream=None):
+        """Pages in use move to the front.  remap: int32 [pages]; tables_out
+        (shaped and strided as tables) and refs_out: None for in place."""
+        d = self._desc()
+        _dev(remap, "remap", _I32, numel=self.pages)
+        if refs_out is not None:
+            _dev(refs_out, "refs_out", _I32, numel=self.pages)
+        if tables_out is not None and (not getattr(tables_out, "is_cuda", False)
+                                       or tables_out.dtype != self.tables.dtype
+                                       or tables_out.shape != self.tables.shape
+                                       or tables_out.stride() != self.tables.stride()):
+            raise HbfError(HBF_EINVAL, "tables_out: expected the shape, strides and type of tables")
+        return self._lib.hbf_kv_compact(d, _dp(remap), _dp(tables_out), _dp(refs_out), _sp(stream))
+
+    def write(self, k, v, slots, pos, first_layer=0, stream=None):
+        """Token pos[i] of slot slots[i] (int32 [n]) gets k[:, i] and v[:, i]:
+        [layers, n, kv_heads, head_dim] of the pool's type, for the layers from
+        first_layer on (or [n, kv_heads, head_dim] for that layer alone)."""
+        d = self._desc()
+        n = _dev(slots, "slots", _I32).numel()
+        _dev(pos, "pos", _I32, numel=n)
+        for t, what in ((k, "k"), (v, "v")):
+            _dev(t, what, (str(self.pool.dtype).replace("torch.", ""),))
+        shape = (n, self.kv_heads, self.head_dim)
+        layers = k.shape[0] if k.dim() == 4 else 1
+        if tuple(k.shape[-3:]) != shape or k.dim() not in (3, 4) or k.shape != v.shape:
+            raise HbfError(HBF_EINVAL, f"k, v: shapes {tuple(k.shape)}, {tuple(v.shape)}, expected "
+                                       f"[layers, {n}, {self.kv_heads}, {self.head_dim}]")
+        return self._lib.hbf_kv_write(d, int(first_layer), layers, _dp(k), _dp(v), _dp(slots), _dp(pos), n,
+                                      _sp(stream))
+
+    def get_status(self, stream=None):
+        """Synchronises; HBF_OK, HBF_EINVAL or HBF_ENOMEM since the last call
+        (the attention's status counts too)."""
+        rc = HBF_OK
+        if self._kv is not None:
+            rc = self._lib.hbf_kv_get_status(self._desc(), _sp(stream))
+        if rc == HBF_OK:
+            if stream is not None:
+                stream.synchronize()
+            rc = int(self._attn_status.item())
+            if rc != HBF_OK:
+                self._attn_status.zero_()
+        return rc
+
+    def prefix_attention(self, layer, q, out, prefix_pages, prefix_len, tables=None, own_lens=None, lse=None,
+                         scale=None, stream=None):
+        """Attention of q [rows, heads, head_dim] (one token per row) over the
+        first prefix_len tokens of the pages prefix_pages (int32; None without
+        prefix), shared by all rows, and each row's own_lens[r] tokens of the
+        pages tables[r] (int32 [rows, entries], rows may be strided; e.g. the
+        columns behind the prefix of a cache's table).  out: as q; lse: float32
+        [rows, heads] or None; scale: 1 / sqrt(head_dim) if None."""
+        import torch
+        name = (str(self.pool.dtype).replace("torch.", ""),)
+        if not 0 <= layer < self.layers:
+            raise HbfError(HBF_EINVAL, f"layer {layer}, the pool has {self.layers}")
+        _strided(q, "q", name, 3)
+        _writable(_strided(out, "out", name, 3), "out")
+        rows, heads, dim = q.shape
+        if dim != self.head_dim or out.shape != q.shape:
+            raise HbfError(HBF_EINVAL, f"q, out: shapes {tuple(q.shape)}, {tuple(out.shape)}, expected "
+                                       f"[rows, heads, {self.head_dim}]")
+        if lse is not None:
+            _dev(lse, "lse", ("float32",), shape=(rows, heads))
+        prefix_len = int(prefix_len)
+        if prefix_len > 0:
+            _dev(prefix_pages, "prefix_pages", _I32, numel=-(-prefix_len // self.page_tokens), at_least=True)
+        if (tables is None) != (own_lens is None):
+            raise HbfError(HBF_EINVAL, "tables and own_lens: both or neither")
+        max_own = stride = 0
+        if tables is not None:
+            if not isinstance(tables, torch.Tensor) or not tables.is_cuda or tables.dtype != torch.int32 \
+                    or tables.dim() != 2 or tables.shape[0] != rows \
+                    or (tables.shape[1] > 1 and tables.stride(1) != 1):
+                raise HbfError(HBF_EINVAL, f"tables: expected int32 [{rows}, entries] in GPU memory, rows contiguous")
+            _dev(own_lens, "own_lens", _I32, shape=(rows,))
+            max_own, stride = min(tables.shape[1] * self.page_tokens, (1 << 31) - 1), _stride(tables, 0)
+        plane = self.pages * self.page_tokens * self.kv_heads * dim * self.pool.element_size()
+        base = self.pool.data_ptr() + 2 * layer * plane
+        kv = hbf_kv_layer(base, base + plane, self.page_tokens * self.kv_heads * dim, self.kv_heads * dim, dim,
+                          self.pages, self.page_tokens, self.kv_heads, dim, _dtype_code(self.pool))
+        at = hbf_attention(q.data_ptr(), _stride(q, 0), _stride(q, 1), rows, heads,
+                           1.0 / dim ** 0.5 if scale is None else scale,
+                           prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len,
+                           tables.data_ptr() if max_own else None, stride,
+                           own_lens.data_ptr() if own_lens is not None else None, max_own, out.data_ptr(), _stride(out, 0),
+                           _stride(out, 1), None if lse is None else lse.data_ptr())
+        b = ctypes.c_size_t()
+        rc = self._lib.hbf_kv_attention_workspace_bytes(ctypes.byref(kv), ctypes.byref(at), ctypes.byref(b))
+        if rc != HBF_OK:
+            return rc
+        ws = self._attn_ws.get(b.value, self.pool.device, stream)
+        return self._lib.hbf_kv_attention(ctypes.byref(kv), ctypes.byref(at), _dp(self._attn_status), _dp(ws),
+                                          ws.numel(), _sp(stream))
+
+
+class MoeLayer:
+    """A mixture-of-experts layer for a few tokens (reading in include/hbf.h).
+
+    gate_up: [experts, 2 * ffn, hidden], gate rows then up rows; down:
+    [experts, hidden, ffn]; the experts may be strided (both may be views of
+    one buffer that holds expert after expert).  router: [experts, hidden], or
+    None where the caller chooses.  max_tokens: the most tokens of a call (its
+    scratch is allocated here; HBF_ENOWORKSPACE beyond).  All bfloat16 or all float16.  renormalize:
+    the chosen experts' weights sum to 1.  Calls on one object must be
+    ordered on one stream."""
+
+    def __init__(self, gate_up, down, topk, router=None, renormalize=True, max_tokens=64):
+        import torch
+        self._lib = load_library()
+        _strided(gate_up, "gate_up", _HALF, 3, 2)
+        name = (str(gate_up.dtype).replace("torch.", ""),)
+        _strided(down, "down", name, 3, 2)
+        E, F2, H = gate_up.shape
+        if F2 % 2 or tuple(down.shape) != (E, H, F2 // 2):
+            raise HbfError(HBF_EINVAL, f"gate_up, down: shapes {tuple(gate_up.shape)}, {tuple(down.shape)}, expected "
+                                       "[experts, 2 * ffn, hidden], [experts, hidden, ffn]")
+        if router is not None:
+            _dev(router, "router", name, shape=(E, H))
+        self._keep = (gate_up, down, router)
+        self._name, self.topk, self.hidden, self.device = name, int(topk), H, gate_up.device
+        self._m = hbf_moe(E, self.topk, H, F2 // 2, _dtype_code(gate_up), HBF_MOE_RENORM if renormalize else 0,
+                          None if router is None else router.data_ptr(), gate_up.data_ptr(), down.data_ptr(),
+                          _stride(gate_up, 0), _stride(down, 0))
+        self._ws = _zeroed(self._bytes(max_tokens), gate_up.device)
+        self._status = _zeroed(256, gate_up.device)[:4].view(torch.int32)
+
+    def _bytes(self, tokens):
+        b = ctypes.c_size_t()
+        _check(self._lib.hbf_moe_workspace_bytes(ctypes.byref(self._m), int(tokens), ctypes.byref(b)),
+               "hbf_moe_workspace_bytes")
+        return b.value
+
+    def forward(self, x, y, ids, weights, stream=None):
+        """x, y: [tokens, hidden] (rows may be strided); ids: int32 [tokens,
+        topk], weights: float32 [tokens, topk]: outputs, or the caller's
+        choices where the layer has no router (-1: none)."""
+        _strided(x, "x", self._name, 2)
+        _writable(_strided(y, "y", self._name, 2), "y")
+        T = x.shape[0]
+        if x.shape[1] != self.hidden or y.shape != x.shape:
+            raise HbfError(HBF_EINVAL, f"x, y: shapes {tuple(x.shape)}, {tuple(y.shape)}, expected "
+                                       f"[tokens, {self.hidden}]")
+        _dev(ids, "ids", _I32, shape=(T, self.topk))
+        _dev(weights, "weights", ("float32",), shape=(T, self.topk))
+        return self._lib.hbf_moe_layer(ctypes.byref(self._m), _dp(x), _stride(x, 0), T, _dp(ids), _dp(weights),
+                                       _dp(y), _stride(y, 0), _dp(self._status), _dp(self._ws), self._ws.numel(),
+                                       _sp(stream))
+
+    def get_status(self, stream=None):
+        """Synchronises; HBF_OK, or HBF_EINVAL if an id was out of range since
+        the last call."""
+        if stream is not None:
+            stream.synchronize()
+        rc = int(self._status.item())
+        if rc != HBF_OK:
+            self._status.zero_()
+        return rc
 
 
 def refresh_plan(params, blocks, pages_per_block):
