@@ -48,6 +48,17 @@ __device__ __forceinline__ u32x2 read_transposed(const void *at) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)at));
 }
 
+// op over the four lanes that hold the same column of a tile (l % 16), in each of them.
+template <typename F>
+__device__ __forceinline__ float across_rows(float x, F op) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const float y = op(__builtin_bit_cast(float, a[0]), __builtin_bit_cast(float, a[1]));
+  const uint32_t v = __builtin_bit_cast(uint32_t, y);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return op(__builtin_bit_cast(float, b[0]), __builtin_bit_cast(float, b[1]));
+}
+
 // What the lanes of one wave have written to LDS is read by others of it: the
 // LDS serves a wave's accesses in order, so only the compiler is held.
 __device__ __forceinline__ void wave_lds_fence() {

@@ -8,14 +8,21 @@
 // are gathered by expert, a tile of 16 of them being the narrow side of the
 // matrix instruction, and the weights are its wide side, loaded straight from
 // memory into the operand (16 rows of 64 bytes at a time; a row's next 64 follow
-// at once).  Three launches, each a pass over one kind of weights:
-//  - route: logits by tiles of 16 experts; the last workgroup chooses, and sorts
-//    the (token, choice) pairs by expert;
-//  - up: 8 gate rows and the 8 up rows of the same channels per tile, so that
-//    one tile's products give 8 channels of h;
-//  - down: 16 rows of y per workgroup, its waves dealing the experts out among
-//    them; each pair's product has a place of its own in LDS, and a token's are
-//    summed in the order of its choices, whoever computed them.
+// at once).  Four launches, each a pass over one kind of weights:
+//  - route: logits by tiles of 16 experts and 16 tokens; a token tile's last
+//    workgroup chooses, and the last of these sorts the (token, choice) pairs
+//    by expert, in tiles of up to 16 (an expert with more is read once per
+//    tile, by workgroups that run beside each other);
+//  - up: 8 gate rows and the 8 up rows of the same channels per tile of weights,
+//    so that its products give 8 channels of h;
+//  - down: 32 rows of y per tile and unit, each pair's product to a place of its
+//    own;
+//  - sum: a token's products in the order of its choices, so that the result
+//    does not depend on who computed them.
+// Up and down are one scheme: a workgroup goes through consecutive units (a
+// token tile's rows, then the next tile's) with the tile's tokens kept in
+// registers, so that only weights are loaded, the next unit's while this one
+// ends; its four waves split the inner axis and meet in LDS once per unit.
 #include <math.h>
 
 #include <algorithm>
@@ -26,21 +33,27 @@
 namespace hbf {
 namespace {
 
-constexpr int UP_THREADS = 256, UP_WAVES = UP_THREADS / 64;
-constexpr int UP_GROUPS = 768;          // three workgroups of 4 waves per CU
-constexpr int ROUTE_THREADS = 512, ROUTE_WAVES = ROUTE_THREADS / 64;
-constexpr int DOWN_THREADS = 512, DOWN_WAVES = DOWN_THREADS / 64;
+constexpr int THREADS = 256, WAVES = THREADS / 64;  // up and down
+constexpr int GROUPS = 768;             // three workgroups per CU
+constexpr int ROUTE_THREADS = 1024, ROUTE_WAVES = ROUTE_THREADS / 64;
+constexpr int SUM_THREADS = 256;
 constexpr int MAX_PAIRS = MOE_MAX_PAIRS;
+constexpr int MAX_TILES = MOE_MAX_EXPERTS + MAX_PAIRS / 16;
+constexpr int TOKEN_TILES = MOE_MAX_TOKENS / 16;
 
+struct Tile {                           // up to 16 pairs of one expert
+  int32_t expert;
+  uint16_t start, count;                // start: first entry of Lists::pair
+};
 struct Lists {                          // what the route leaves for the others
-  uint32_t n_active;
+  uint32_t n_tiles;
   uint32_t pad[63];
-  int32_t expert[MOE_MAX_EXPERTS];      // of the n_active experts with tokens, ascending
-  int32_t start[MOE_MAX_EXPERTS + 1];   // their first entry of `pair`
+  Tile tile[MAX_TILES];
   int32_t pair[MAX_PAIRS];              // token * topk + choice, by expert
 };
-struct Ctl {
-  uint32_t arrived;                     // 0 between calls
+struct Ctl {                            // 0 between calls
+  uint32_t arrived[TOKEN_TILES];        // a token tile's workgroups that are done
+  uint32_t chosen;                      // token tiles whose choices are made
 };
 
 struct Args {
@@ -58,6 +71,7 @@ struct Args {
   float *logits;                        // [tokens][e_pad]
   int e_pad;
   char *h_hi, *h_lo;                    // [pairs][F], in the order of `pair`
+  float *part;                          // [pairs][H] products, by token and choice
 };
 
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
@@ -75,6 +89,7 @@ size_t carve(const hbf_moe &m, int tokens, char *base, Args *a) {
   a->logits = (float *)take((size_t)tokens * a->e_pad * 4);
   a->h_hi = take((size_t)tokens * m.topk * m.ffn * 2);
   a->h_lo = take((size_t)tokens * m.topk * m.ffn * 2);
+  a->part = (float *)take((size_t)tokens * m.topk * m.hidden * 4);
   return o;
 }
 
@@ -91,13 +106,15 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   HBF_DPP_MAX(0x141);  // row_half_mirror
   HBF_DPP_MAX(0x140);  // row_mirror
 #undef HBF_DPP_MAX
-  v = max(v, (uint32_t)__shfl_xor((int)v, 16));
-  return max(v, (uint32_t)__shfl_xor((int)v, 32));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(b[0], b[1]);
 }
 
 // The topk choices of token t by one wave; lane l holds experts l EPL .. + EPL-1.
 template <int EPL>
-__device__ void choose(const Args &a, int t, int32_t *ids_lds) {
+__device__ void choose(const Args &a, int t) {
   const int lane = threadIdx.x & 63, E = a.m.experts, k = a.m.topk;
   float v[EPL];
   uint32_t key[EPL];
@@ -153,10 +170,26 @@ __device__ void choose(const Args &a, int t, int32_t *ids_lds) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
   if (lane < k) {
-    ids_lds[t * k + lane] = chosen;
     a.ids[t * k + lane] = chosen;
     a.weights[t * k + lane] = w / sum;
   }
+}
+
+// This workgroup's part is written.  True in every thread of the last of n
+// workgroups to get here, which then sees what all of them wrote; the counter
+// is 0 again.
+__device__ bool last_of(uint32_t *counter, uint32_t n) {
+  __shared__ uint32_t last;
+  __syncthreads();
+  if (n == 1) return true;
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = atomicAdd(counter, 1) + 1 == n;
+    if (last) *counter = 0;
+    __threadfence();
+  }
+  __syncthreads();
+  return last != 0;
 }
 
 template <typename T>
@@ -165,7 +198,6 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
   __shared__ int32_t ids[MAX_PAIRS];
   __shared__ int32_t cnt[MOE_MAX_EXPERTS];
   __shared__ uint32_t wsum[ROUTE_WAVES], asum[ROUTE_WAVES];
-  __shared__ uint32_t last;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   const int E = a.m.experts, H = a.m.hidden, pairs = a.tokens * a.m.topk;
   if (a.m.dev_router) {
@@ -196,21 +228,16 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
       for (int i = 1; i < ROUTE_WAVES; i++) acc += red[i][lane];
       if (t0 + col < a.tokens) *(f32x4 *)(a.logits + (int64_t)(t0 + col) * a.e_pad + e0 + kg * 4) = acc;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      __threadfence();
-      last = atomicAdd(&a.ctl->arrived, 1) + 1 == gridDim.x;
-      __threadfence();
+    const int tile = blockIdx.x / e_tiles;
+    if (!last_of(&a.ctl->arrived[tile], e_tiles)) return;
+    for (int tt = t0 + w; tt < min(t0 + 16, a.tokens); tt += ROUTE_WAVES) {
+      if (E <= 64) choose<1>(a, tt);
+      else if (E <= 128) choose<2>(a, tt);
+      else if (E <= 256) choose<4>(a, tt);
+      else choose<16>(a, tt);
     }
-    __syncthreads();
-    if (!last) return;
-    if (threadIdx.x == 0) a.ctl->arrived = 0;
-    for (int tt = w; tt < a.tokens; tt += ROUTE_WAVES) {
-      if (E <= 64) choose<1>(a, tt, ids);
-      else if (E <= 128) choose<2>(a, tt, ids);
-      else if (E <= 256) choose<4>(a, tt, ids);
-      else choose<16>(a, tt, ids);
-    }
+    if (!last_of(&a.ctl->chosen, gridDim.x / e_tiles)) return;
+    for (int p = threadIdx.x; p < pairs; p += ROUTE_THREADS) ids[p] = a.ids[p];
   } else {
     for (int p = threadIdx.x; p < pairs; p += ROUTE_THREADS) {
       const int e = a.ids[p];
@@ -232,7 +259,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
   for (int i = 0; i < PER; i++) {
     c[i] = cnt[threadIdx.x * PER + i];
     sum += c[i];
-    act += c[i] > 0;
+    act += (c[i] + 15) / 16;
   }
   uint32_t xs = sum, xa = act;
   for (int d = 1; d < 64; d <<= 1) {
@@ -247,24 +274,19 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
     asum[w] = xa;
   }
   __syncthreads();
-  uint32_t at = xs - sum, ai = xa - act;
+  uint32_t at = xs - sum, ti = xa - act;
   for (int i = 0; i < w; i++) {
     at += wsum[i];
-    ai += asum[i];
+    ti += asum[i];
   }
 #pragma unroll
   for (int i = 0; i < PER; i++) {
-    if (c[i] > 0) {
-      a.lists->expert[ai] = threadIdx.x * PER + i;
-      a.lists->start[ai++] = at;
-    }
+    for (int j = 0; j < c[i]; j += 16)
+      a.lists->tile[ti++] = Tile{(int)threadIdx.x * PER + i, (uint16_t)(at + j), (uint16_t)min(c[i] - j, 16)};
     cnt[threadIdx.x * PER + i] = at;
     at += c[i];
   }
-  if (threadIdx.x == ROUTE_THREADS - 1) {
-    a.lists->n_active = ai;
-    a.lists->start[ai] = at;
-  }
+  if (threadIdx.x == ROUTE_THREADS - 1) a.lists->n_tiles = ti;
   __syncthreads();
   // (an expert's pairs in any order: they are columns of its product, which do not meet)
   for (int p = threadIdx.x; p < pairs; p += ROUTE_THREADS)
@@ -275,158 +297,220 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
 
 // KS steps of 32 per wave and pass; EXACT: the hidden size is one pass of them.
 template <typename T, int KS, bool EXACT>
-__global__ __launch_bounds__(UP_THREADS) void k_moe_up(Args a) {
-  __shared__ f32x4 red[2][UP_WAVES][64];
+__global__ __launch_bounds__(THREADS) void k_moe_up(Args a) {
+  __shared__ f32x4 red[2][WAVES][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   const int H = a.m.hidden, F = a.m.ffn, blocks = F / 8;
-  const int64_t units = (int64_t)a.lists->n_active * blocks;
+  const int64_t units = (int64_t)a.lists->n_tiles * blocks;
   const int u0 = (int)(units * blockIdx.x / gridDim.x), u1 = (int)(units * (blockIdx.x + 1) / gridDim.x);
-  const int passes = EXACT ? 1 : (H + UP_WAVES * KS * 32 - 1) / (UP_WAVES * KS * 32);
+  if (u0 >= u1) return;
+  const int passes = EXACT ? 1 : (H + WAVES * KS * 32 - 1) / (WAVES * KS * 32);
   u32x4 av[KS], bv[KS];
-  auto k_of = [&](int pass, int s) { return ((pass * UP_WAVES + w) * KS + s) * 32 + kg * 8; };
-  auto load_w = [&](int u, int pass) {
-    const int e = a.lists->expert[u / blocks], r = u % blocks * 8 + (col & 7) + (col & 8 ? F : 0);
-    const char *p = (const char *)a.m.dev_gate_up + 2 * ((int64_t)e * a.m.gate_up_stride + (int64_t)r * H);
+  auto k_of = [&](int pass, int s) { return ((pass * WAVES + w) * KS + s) * 32 + kg * 8; };
+  auto load_w = [&](int expert, int block, int pass) {
+    const int r = block * 8 + (col & 7) + (col & 8 ? F : 0);
+    const char *p = (const char *)a.m.dev_gate_up + 2 * ((int64_t)expert * a.m.gate_up_stride + (int64_t)r * H);
 #pragma unroll
     for (int s = 0; s < KS; s++) {
       const int k = k_of(pass, s);
       av[s] = EXACT || k < H ? load16(p + 2 * k) : ZERO4;
     }
   };
-  auto load_x = [&](int pair, int pass) {
-    const char *p = a.x + 2 * ((int64_t)(a.lists->pair[pair] / a.m.topk) * a.xs);
+  auto load_x = [&](int token, int pass) {
+    const char *p = a.x + 2 * (token * a.xs);
 #pragma unroll
     for (int s = 0; s < KS; s++) {
       const int k = k_of(pass, s);
       bv[s] = EXACT || k < H ? load16(p + 2 * k) : ZERO4;
     }
   };
-  int held = -1, buf = 0;  // the active expert whose (only) tile of tokens bv holds
-  if (u0 < u1) load_w(u0, 0);
+  int ti = u0 / blocks, block = u0 - ti * blocks, buf = 0;
+  Tile tile = a.lists->tile[ti];
+  load_w(tile.expert, block, 0);
+  // columns past the tokens repeat the last
+  int token = a.lists->pair[tile.start + min(col, (int)tile.count - 1)] / a.m.topk;
+  if (passes == 1) load_x(token, 0);  // kept for all of the tile's units
   for (int u = u0; u < u1; u++) {
-    const int act = u / blocks, p0 = a.lists->start[act], p1 = a.lists->start[act + 1];
-    for (int p = p0; p < p1; p += 16) {
-      const int mine = min(p + col, p1 - 1);  // columns past the tokens repeat the last
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      for (int pass = 0; pass < passes; pass++) {
-        if (passes > 1 && (pass || p > p0)) load_w(u, pass);
-        if (passes > 1 || p1 - p0 > 16 || held != act) load_x(mine, pass);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int pass = 0; pass < passes; pass++) {
+      if (pass) load_w(tile.expert, block, pass);
+      if (passes > 1) load_x(token, pass);
 #pragma unroll
-        for (int s = 0; s < KS; s++) acc = T::mfma(av[s], bv[s], acc);
-      }
-      held = p1 - p0 > 16 ? -1 : act;
-      if (p + 16 >= p1 && u + 1 < u1) load_w(u + 1, 0);  // in flight while this tile ends
-      red[buf][w][lane] = acc;
-      __syncthreads();
-      const int n = threadIdx.x >> 3, r = threadIdx.x & 7;
-      if (threadIdx.x < 128 && p + n < p1) {
-        float g = 0.f, up = 0.f;
-#pragma unroll
-        for (int i = 0; i < UP_WAVES; i++) {
-          g += red[buf][i][(r >> 2) * 16 + n][r & 3];
-          up += red[buf][i][(2 + (r >> 2)) * 16 + n][r & 3];
-        }
-        const float h = g / (1.f + expf(-g)) * up;
-        // two words: what rounding h to one would lose shows in y as much as y's own rounding
-        const typename T::elem hi = (typename T::elem)h;
-        const float rest = h - (float)hi;
-        const int64_t at = (int64_t)(p + n) * F + u % blocks * 8 + r;
-        ((typename T::elem *)a.h_hi)[at] = hi;
-        ((typename T::elem *)a.h_lo)[at] = (typename T::elem)(isfinite(rest) ? rest : 0.f);
-      }
-      buf ^= 1;  // (the next tile writes the other half; one barrier per tile)
+      for (int s = 0; s < KS; s++) acc = T::mfma(av[s], bv[s], acc);
     }
+    const Tile done = tile;
+    const int b8 = block * 8;
+    if (u + 1 < u1) {  // the next loads are in flight while this unit ends
+      if (++block == blocks) {
+        block = 0;
+        tile = a.lists->tile[++ti];
+        token = a.lists->pair[tile.start + min(col, (int)tile.count - 1)] / a.m.topk;
+        if (passes == 1) load_x(token, 0);
+      }
+      load_w(tile.expert, block, 0);
+    }
+    red[buf][w][lane] = acc;
+    __syncthreads();
+    const int n = threadIdx.x >> 3, r = threadIdx.x & 7;
+    if (n < done.count) {
+      float g = 0.f, up = 0.f;
+#pragma unroll
+      for (int i = 0; i < WAVES; i++) {
+        g += red[buf][i][(r >> 2) * 16 + n][r & 3];
+        up += red[buf][i][(2 + (r >> 2)) * 16 + n][r & 3];
+      }
+      const float h = g / (1.f + expf(-g)) * up;
+      // two words: what rounding h to one would lose shows in y as much as y's own rounding
+      const typename T::elem hi = (typename T::elem)h;
+      const float rest = h - (float)hi;
+      const int64_t at = (int64_t)(done.start + n) * F + b8 + r;
+      ((typename T::elem *)a.h_hi)[at] = hi;
+      ((typename T::elem *)a.h_lo)[at] = (typename T::elem)(isfinite(rest) ? rest : 0.f);
+    }
+    buf ^= 1;  // (the next unit writes the other half: one barrier per unit)
   }
 }
 
 // ------------------------------------------------------------ down
 
-template <typename T>
-__global__ __launch_bounds__(DOWN_THREADS) void k_moe_down(Args a) {
-  extern __shared__ __align__(16) float part[];  // [pairs][16] products of this workgroup's rows
+// KS steps of 32 per wave and pass, RB tiles of 16 rows per unit; EXACT: F is one
+// pass and H whole units.
+template <typename T, int KS, int RB, bool EXACT>
+__global__ __launch_bounds__(THREADS) void k_moe_down(Args a) {
+  __shared__ f32x4 red[2][WAVES][RB][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
-  const int H = a.m.hidden, F = a.m.ffn, k = a.m.topk, r0 = blockIdx.x * 16;
-  constexpr int KS = 8;
-  const int chunks = (F + KS * 32 - 1) / (KS * 32), n_act = a.lists->n_active;
-  for (int i = threadIdx.x; i < a.tokens * k * 4; i += DOWN_THREADS) ((f32x4 *)part)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  __syncthreads();
-  const char *wp = (const char *)a.m.dev_down + 2 * ((int64_t)min(r0 + col, H - 1) * F + kg * 8);
-  u32x4 next[KS], av[KS];
-  auto load_w = [&](int act, int c) {
-    const char *p = wp + 2 * (int64_t)a.lists->expert[act] * a.m.down_stride;
+  const int H = a.m.hidden, F = a.m.ffn, blocks = (H + 16 * RB - 1) / (16 * RB);
+  const int64_t units = (int64_t)a.lists->n_tiles * blocks;
+  const int u0 = (int)(units * blockIdx.x / gridDim.x), u1 = (int)(units * (blockIdx.x + 1) / gridDim.x);
+  if (u0 >= u1) return;
+  const int passes = EXACT ? 1 : (F + WAVES * KS * 32 - 1) / (WAVES * KS * 32);
+  u32x4 av[RB][KS], hi[KS], lo[KS];
+  auto k_of = [&](int pass, int s) { return ((pass * WAVES + w) * KS + s) * 32 + kg * 8; };
+  auto load_w = [&](int expert, int block, int pass) {
 #pragma unroll
-    for (int s = 0; s < KS; s++) {
-      const int kk = (c * KS + s) * 32;
-      next[s] = kk + kg * 8 < F ? load16(p + 2 * kk) : ZERO4;
-    }
-  };
-  if (w < n_act) load_w(w, 0);
-  for (int act = w; act < n_act; act += DOWN_WAVES) {
-    const int p0 = a.lists->start[act], p1 = a.lists->start[act + 1];
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < chunks; c++) {
+    for (int b = 0; b < RB; b++) {
+      const int r = (block * RB + b) * 16 + col;
+      const char *p = (const char *)a.m.dev_down +
+                      2 * ((int64_t)expert * a.m.down_stride + (int64_t)(EXACT ? r : min(r, H - 1)) * F);
 #pragma unroll
-      for (int s = 0; s < KS; s++) av[s] = next[s];
-      if (c + 1 < chunks)
-        load_w(act, c + 1);
-      else if (act + DOWN_WAVES < n_act)
-        load_w(act + DOWN_WAVES, 0);
-      for (int p = p0; p < p1; p += 16) {
-        const int64_t row = (int64_t)min(p + col, p1 - 1) * F + c * KS * 32 + kg * 8;
-        if (p1 - p0 > 16) acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < KS; s++) {
-          const bool on = (c * KS + s) * 32 + kg * 8 < F;
-          const u32x4 hi = on ? load16(a.h_hi + 2 * (row + s * 32)) : ZERO4;
-          const u32x4 lo = on ? load16(a.h_lo + 2 * (row + s * 32)) : ZERO4;
-          acc = T::mfma(av[s], hi, acc);
-          acc = T::mfma(av[s], lo, acc);
-        }
-        if ((p1 - p0 > 16 || c + 1 == chunks) && p + col < p1) {
-          f32x4 *to = (f32x4 *)(part + a.lists->pair[p + col] * 16 + kg * 4);
-          *to = p1 - p0 > 16 ? *to + acc : acc;
-        }
+      for (int s = 0; s < KS; s++) {
+        const int k = k_of(pass, s);
+        av[b][s] = EXACT || k < F ? load16(p + 2 * k) : ZERO4;
       }
     }
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.tokens * 16; i += DOWN_THREADS) {
-    const int t = i >> 4, r = i & 15;
-    float y = 0.f;
-    for (int j = 0; j < k; j++) {
-      const int p = t * k + j;
-      if (a.m.dev_router || (uint32_t)a.ids[p] < (uint32_t)a.m.experts) y += a.weights[p] * part[p * 16 + r];
+  };
+  auto load_h = [&](int entry, int pass) {
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+      const int k = k_of(pass, s);
+      const int64_t at = 2 * ((int64_t)entry * F + k);
+      hi[s] = EXACT || k < F ? load16(a.h_hi + at) : ZERO4;
+      lo[s] = EXACT || k < F ? load16(a.h_lo + at) : ZERO4;
     }
-    if (r0 + r < H) ((typename T::elem *)a.y)[t * a.ys + r0 + r] = (typename T::elem)y;
+  };
+  int ti = u0 / blocks, block = u0 - ti * blocks, buf = 0;
+  Tile tile = a.lists->tile[ti];
+  load_w(tile.expert, block, 0);
+  int entry = tile.start + min(col, (int)tile.count - 1);  // columns past the tokens repeat the last
+  if (passes == 1) load_h(entry, 0);
+  for (int u = u0; u < u1; u++) {
+    f32x4 acc[RB];
+#pragma unroll
+    for (int b = 0; b < RB; b++) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int pass = 0; pass < passes; pass++) {
+      if (pass) load_w(tile.expert, block, pass);
+      if (passes > 1) load_h(entry, pass);
+#pragma unroll
+      for (int s = 0; s < KS; s++)
+#pragma unroll
+        for (int b = 0; b < RB; b++) {
+          acc[b] = T::mfma(av[b][s], hi[s], acc[b]);
+          acc[b] = T::mfma(av[b][s], lo[s], acc[b]);
+        }
+    }
+    const Tile done = tile;
+    const int row0 = block * RB * 16;
+    if (u + 1 < u1) {
+      if (++block == blocks) {
+        block = 0;
+        tile = a.lists->tile[++ti];
+        entry = tile.start + min(col, (int)tile.count - 1);
+        if (passes == 1) load_h(entry, 0);
+      }
+      load_w(tile.expert, block, 0);
+    }
+#pragma unroll
+    for (int b = 0; b < RB; b++) red[buf][w][b][lane] = acc[b];
+    __syncthreads();
+    const int n = threadIdx.x >> 4, r = threadIdx.x & 15;
+    if (n < done.count) {
+      const int64_t to = (int64_t)a.lists->pair[done.start + n] * H + row0 + r;
+#pragma unroll
+      for (int b = 0; b < RB; b++) {
+        float o = 0.f;
+#pragma unroll
+        for (int i = 0; i < WAVES; i++) o += red[buf][i][b][(r >> 2) * 16 + n][r & 3];
+        if (EXACT || row0 + b * 16 + r < H) a.part[to + b * 16] = o;
+      }
+    }
+    buf ^= 1;
   }
+}
+
+// ------------------------------------------------------------ sum
+
+// Four channels of one token per thread.
+template <typename T>
+__global__ __launch_bounds__(SUM_THREADS) void k_moe_sum(Args a) {
+  const int quads = a.m.hidden / 4, k = a.m.topk;
+  const int i = blockIdx.x * SUM_THREADS + threadIdx.x, t = i / quads, r = (i - t * quads) * 4;
+  if (t >= a.tokens) return;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int j = 0; j < k; j++) {
+    const int p = t * k + j;
+    if (a.m.dev_router || (uint32_t)a.ids[p] < (uint32_t)a.m.experts)
+      y += a.weights[p] * *(const f32x4 *)(a.part + (int64_t)p * a.m.hidden + r);
+  }
+  *(u32x2 *)(a.y + 2 * (t * a.ys + r)) = u32x2{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
 }
 
 template <typename T, int KS>
 void up(const Args &a, int groups, hipStream_t s) {
-  if (a.m.hidden == UP_WAVES * KS * 32)
-    k_moe_up<T, KS, true><<<groups, UP_THREADS, 0, s>>>(a);
+  if (a.m.hidden == WAVES * KS * 32)
+    k_moe_up<T, KS, true><<<groups, THREADS, 0, s>>>(a);
   else
-    k_moe_up<T, KS, false><<<groups, UP_THREADS, 0, s>>>(a);
+    k_moe_up<T, KS, false><<<groups, THREADS, 0, s>>>(a);
+}
+template <typename T, int KS, int RB>
+void down(const Args &a, int tiles, hipStream_t s) {
+  const int64_t units = (int64_t)tiles * ((a.m.hidden + 16 * RB - 1) / (16 * RB));
+  const int groups = (int)std::min<int64_t>(units, GROUPS);
+  if (a.m.ffn == WAVES * KS * 32 && a.m.hidden % (16 * RB) == 0)
+    k_moe_down<T, KS, RB, true><<<groups, THREADS, 0, s>>>(a);
+  else
+    k_moe_down<T, KS, RB, false><<<groups, THREADS, 0, s>>>(a);
 }
 
 template <typename T>
 hipError_t run(const Args &a, hipStream_t s) {
+  const int pairs = a.tokens * a.m.topk;
   const int route = a.m.dev_router ? a.e_pad / 16 * ((a.tokens + 15) / 16) : 1;
   k_moe_route<T><<<route, ROUTE_THREADS, 0, s>>>(a);
-  const int64_t units = (int64_t)std::min(a.m.experts, a.tokens * a.m.topk) * (a.m.ffn / 8);
-  const int groups = (int)std::min<int64_t>(units, UP_GROUPS);
-  const int per = ((a.m.hidden + 31) / 32 + UP_WAVES - 1) / UP_WAVES;  // steps per wave
-  if (per <= 2) up<T, 2>(a, groups, s);
-  else if (per <= 4) up<T, 4>(a, groups, s);
-  else if (per <= 8) up<T, 8>(a, groups, s);
+  const int tiles = std::min(pairs, a.m.experts + pairs / 16);  // at most
+  const int groups = (int)std::min<int64_t>((int64_t)tiles * (a.m.ffn / 8), GROUPS);
+  // steps per wave
+  const int up_steps = ((a.m.hidden + 31) / 32 + WAVES - 1) / WAVES;
+  if (up_steps <= 2) up<T, 2>(a, groups, s);
+  else if (up_steps <= 4) up<T, 4>(a, groups, s);
+  else if (up_steps <= 8) up<T, 8>(a, groups, s);
   else up<T, 16>(a, groups, s);
-  const int lds = a.tokens * a.m.topk * 64;
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute((const void *)k_moe_down<T>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             MAX_PAIRS * 64);
-    if (e != hipSuccess) return e;
-  }
-  k_moe_down<T><<<(a.m.hidden + 15) / 16, DOWN_THREADS, lds, s>>>(a);
+  const int down_steps = ((a.m.ffn + 31) / 32 + WAVES - 1) / WAVES;
+  if (down_steps <= 2) down<T, 2, 2>(a, tiles, s);
+  else if (down_steps <= 4) down<T, 4, 2>(a, tiles, s);
+  else if (down_steps <= 6) down<T, 6, 2>(a, tiles, s);
+  else down<T, 8, 2>(a, tiles, s);
+  k_moe_sum<T><<<(a.tokens * (a.m.hidden / 4) + SUM_THREADS - 1) / SUM_THREADS, SUM_THREADS, 0, s>>>(a);
   return hipGetLastError();
 }
 

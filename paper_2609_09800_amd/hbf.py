@@ -479,6 +479,22 @@ _I32 = ("int32",)
 _HALF = ("bfloat16", "float16")
 
 
+def _raw(stream):
+    """hipStream_t of a torch stream (None -> current stream), as a number.
+    (torch.cuda.current_stream() builds an object: 2.8 us of a call that lasts 10.)"""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+
+
+def _ints(t, what, numel=None):
+    """_dev for an int32 tensor, its checks in the order that passes soonest."""
+    import torch
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.int32 and t.is_contiguous()
+            and (numel is None or t.numel() == numel)):
+        _dev(t, what, _I32, numel=numel)
+    return t.numel()
+
+
 def _strided(t, what, dtypes, dim, inner=1):
     """As _dev, for a tensor of `dim` dimensions whose last `inner` are
     contiguous and whose others may be strided (by 16-byte multiples)."""
@@ -488,11 +504,11 @@ def _strided(t, what, dtypes, dim, inner=1):
         bad = f"not a tensor ({type(t).__name__})"
     elif not t.is_cuda:
         bad = "not in GPU memory"
-    elif str(t.dtype).replace("torch.", "") not in dtypes:
-        bad = f"dtype {t.dtype}, expected {'/'.join(dtypes)}"
+    elif t.dtype not in dtypes:
+        bad = f"dtype {t.dtype}, expected {'/'.join(map(str, dtypes))}"
     elif t.dim() != dim:
         bad = f"{t.dim()} dimensions, expected {dim}"
-    elif t.numel():
+    elif not t.is_contiguous() or dim > inner and t.shape[-1] * t.element_size() % 16:
         want = 1
         for d in range(dim - 1, dim - 1 - inner, -1):
             if t.shape[d] != 1 and t.stride(d) != want:
@@ -507,7 +523,7 @@ def _strided(t, what, dtypes, dim, inner=1):
 
 def _writable(t, what):
     """An output whose elements must not share memory (an expanded tensor's do)."""
-    if any(t.stride(d) == 0 and t.shape[d] > 1 for d in range(t.dim())):
+    if not t.is_contiguous() and any(t.stride(d) == 0 and t.shape[d] > 1 for d in range(t.dim())):
         raise HbfError(HBF_EINVAL, f"{what}: an expanded tensor cannot be written")
     return t
 
@@ -517,14 +533,16 @@ class _Scratch:
 
     def __init__(self):
         self._t = None
+        self._stream = None   # the one that the block was made on
 
     def get(self, nbytes, device, stream):
         import torch
-        s = stream if stream is not None else torch.cuda.current_stream(device)
-        if self._t is None or self._t.numel() < nbytes or self._t.device != device:
+        if self._t is None or self._t.numel() < nbytes:
             # (the allocator takes the old block back once the streams it was used on are through with it)
             self._t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-        self._t.record_stream(s)
+            self._stream = torch.cuda.current_stream(device).cuda_stream
+        if _raw(stream) != self._stream:
+            self._t.record_stream(stream if stream is not None else torch.cuda.current_stream(device))
         return self._t
 
 
@@ -568,6 +586,7 @@ class KvPages:
         self.pool, self.refs, self.tables, self.lens = pool, refs, tables, lens
         self.layers, _, self.pages, self.page_tokens, self.kv_heads, self.head_dim = pool.shape
         self._attn_ws = _Scratch()
+        self._attn_sizes, self._attn_bytes, self._layers = None, 0, {}
         self._attn_status = _zeroed(256, pool.device)[:4].view(torch.int32)
         self._kv = None
         if refs is None and tables is None and lens is None:
@@ -589,69 +608,73 @@ class KvPages:
                "hbf_kv_workspace_bytes")
         self._ws = _zeroed(b.value, pool.device)
         self._kv.dev_ws = self._ws.data_ptr()
+        self._kv_ref = ctypes.byref(self._kv)
 
     def _desc(self):
         if self._kv is None:
             raise HbfError(HBF_EINVAL, "this KvPages was made without refs, tables and lens")
-        return ctypes.byref(self._kv)
+        return self._kv_ref
 
     def extend(self, slots, add, stream=None):
         """Slot slots[i] grows by add[i] tokens (int32 device tensors [n])."""
         d = self._desc()
-        n = _dev(slots, "slots", _I32).numel()
-        _dev(add, "add", _I32, numel=n)
-        return self._lib.hbf_kv_extend(d, _dp(slots), _dp(add), n, self.max_list, _sp(stream))
+        n = _ints(slots, "slots")
+        _ints(add, "add", n)
+        return self._lib.hbf_kv_extend(d, slots.data_ptr(), add.data_ptr(), n, self.max_list, _raw(stream))
 
     def fork(self, parents, children, stream=None):
         """The empty slot children[i] gets parents[i]'s tokens (int32 [n])."""
         d = self._desc()
-        n = _dev(parents, "parents", _I32).numel()
-        _dev(children, "children", _I32, numel=n)
-        return self._lib.hbf_kv_fork(d, _dp(parents), _dp(children), n, self.max_list, _sp(stream))
+        n = _ints(parents, "parents")
+        _ints(children, "children", n)
+        return self._lib.hbf_kv_fork(d, parents.data_ptr(), children.data_ptr(), n, self.max_list, _raw(stream))
 
     def free(self, slots, stream=None):
         """Slots (int32 [n]) become empty and give their pages back."""
         d = self._desc()
-        n = _dev(slots, "slots", _I32).numel()
-        return self._lib.hbf_kv_free(d, _dp(slots), n, _sp(stream))
+        n = _ints(slots, "slots")
+        return self._lib.hbf_kv_free(d, slots.data_ptr(), n, _raw(stream))
 
     def copy(self, src, dst, stream=None):
         """Pages dst[i] become copies of pages src[i] (int32 [n])."""
         d = self._desc()
-        n = _dev(src, "src", _I32).numel()
-        _dev(dst, "dst", _I32, numel=n)
-        return self._lib.hbf_kv_copy(d, _dp(src), _dp(dst), n, _sp(stream))
+        n = _ints(src, "src")
+        _ints(dst, "dst", n)
+        return self._lib.hbf_kv_copy(d, src.data_ptr(), dst.data_ptr(), n, _raw(stream))
 
     def compact(self, remap, tables_out=None, refs_out=None, stream=None):
         """Pages in use move to the front.  remap: int32 [pages]; tables_out
         (shaped and strided as tables) and refs_out: None for in place."""
         d = self._desc()
-        _dev(remap, "remap", _I32, numel=self.pages)
+        _ints(remap, "remap", self.pages)
         if refs_out is not None:
-            _dev(refs_out, "refs_out", _I32, numel=self.pages)
+            _ints(refs_out, "refs_out", self.pages)
         if tables_out is not None and (not getattr(tables_out, "is_cuda", False)
                                        or tables_out.dtype != self.tables.dtype
                                        or tables_out.shape != self.tables.shape
                                        or tables_out.stride() != self.tables.stride()):
             raise HbfError(HBF_EINVAL, "tables_out: expected the shape, strides and type of tables")
-        return self._lib.hbf_kv_compact(d, _dp(remap), _dp(tables_out), _dp(refs_out), _sp(stream))
+        return self._lib.hbf_kv_compact(d, remap.data_ptr(), None if tables_out is None else tables_out.data_ptr(),
+                                        None if refs_out is None else refs_out.data_ptr(), _raw(stream))
 
     def write(self, k, v, slots, pos, first_layer=0, stream=None):
         """Token pos[i] of slot slots[i] (int32 [n]) gets k[:, i] and v[:, i]:
         [layers, n, kv_heads, head_dim] of the pool's type, for the layers from
         first_layer on (or [n, kv_heads, head_dim] for that layer alone)."""
+        import torch
         d = self._desc()
-        n = _dev(slots, "slots", _I32).numel()
-        _dev(pos, "pos", _I32, numel=n)
+        n = _ints(slots, "slots")
+        _ints(pos, "pos", n)
         for t, what in ((k, "k"), (v, "v")):
-            _dev(t, what, (str(self.pool.dtype).replace("torch.", ""),))
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is self.pool.dtype and t.is_contiguous()):
+                _dev(t, what, (str(self.pool.dtype).replace("torch.", ""),))
         shape = (n, self.kv_heads, self.head_dim)
         layers = k.shape[0] if k.dim() == 4 else 1
         if tuple(k.shape[-3:]) != shape or k.dim() not in (3, 4) or k.shape != v.shape:
             raise HbfError(HBF_EINVAL, f"k, v: shapes {tuple(k.shape)}, {tuple(v.shape)}, expected "
                                        f"[layers, {n}, {self.kv_heads}, {self.head_dim}]")
-        return self._lib.hbf_kv_write(d, int(first_layer), layers, _dp(k), _dp(v), _dp(slots), _dp(pos), n,
-                                      _sp(stream))
+        return self._lib.hbf_kv_write(d, int(first_layer), layers, k.data_ptr(), v.data_ptr(), slots.data_ptr(),
+                                      pos.data_ptr(), n, _raw(stream))
 
     def get_status(self, stream=None):
         """Synchronises; HBF_OK, HBF_EINVAL or HBF_ENOMEM since the last call
@@ -676,20 +699,21 @@ class KvPages:
         columns behind the prefix of a cache's table).  out: as q; lse: float32
         [rows, heads] or None; scale: 1 / sqrt(head_dim) if None."""
         import torch
-        name = (str(self.pool.dtype).replace("torch.", ""),)
+        dtype = (self.pool.dtype,)
         if not 0 <= layer < self.layers:
             raise HbfError(HBF_EINVAL, f"layer {layer}, the pool has {self.layers}")
-        _strided(q, "q", name, 3)
-        _writable(_strided(out, "out", name, 3), "out")
+        _strided(q, "q", dtype, 3)
+        _writable(_strided(out, "out", dtype, 3), "out")
         rows, heads, dim = q.shape
         if dim != self.head_dim or out.shape != q.shape:
             raise HbfError(HBF_EINVAL, f"q, out: shapes {tuple(q.shape)}, {tuple(out.shape)}, expected "
                                        f"[rows, heads, {self.head_dim}]")
-        if lse is not None:
+        if lse is not None and not (isinstance(lse, torch.Tensor) and lse.is_cuda and lse.dtype is torch.float32
+                                    and lse.is_contiguous() and lse.shape == (rows, heads)):
             _dev(lse, "lse", ("float32",), shape=(rows, heads))
         prefix_len = int(prefix_len)
-        if prefix_len > 0:
-            _dev(prefix_pages, "prefix_pages", _I32, numel=-(-prefix_len // self.page_tokens), at_least=True)
+        if prefix_len > 0 and _ints(prefix_pages, "prefix_pages") * self.page_tokens < prefix_len:
+            raise HbfError(HBF_EINVAL, f"prefix_pages: {prefix_pages.numel()} pages for {prefix_len} tokens")
         if (tables is None) != (own_lens is None):
             raise HbfError(HBF_EINVAL, "tables and own_lens: both or neither")
         max_own = stride = 0
@@ -698,25 +722,37 @@ class KvPages:
                     or tables.dim() != 2 or tables.shape[0] != rows \
                     or (tables.shape[1] > 1 and tables.stride(1) != 1):
                 raise HbfError(HBF_EINVAL, f"tables: expected int32 [{rows}, entries] in GPU memory, rows contiguous")
-            _dev(own_lens, "own_lens", _I32, shape=(rows,))
+            _ints(own_lens, "own_lens", rows)
             max_own, stride = min(tables.shape[1] * self.page_tokens, (1 << 31) - 1), _stride(tables, 0)
-        plane = self.pages * self.page_tokens * self.kv_heads * dim * self.pool.element_size()
-        base = self.pool.data_ptr() + 2 * layer * plane
-        kv = hbf_kv_layer(base, base + plane, self.page_tokens * self.kv_heads * dim, self.kv_heads * dim, dim,
-                          self.pages, self.page_tokens, self.kv_heads, dim, _dtype_code(self.pool))
+        kv = self._layer(layer)
         at = hbf_attention(q.data_ptr(), _stride(q, 0), _stride(q, 1), rows, heads,
-                           1.0 / dim ** 0.5 if scale is None else scale,
+                           dim ** -0.5 if scale is None else scale,
                            prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len,
                            tables.data_ptr() if max_own else None, stride,
-                           own_lens.data_ptr() if own_lens is not None else None, max_own, out.data_ptr(), _stride(out, 0),
-                           _stride(out, 1), None if lse is None else lse.data_ptr())
-        b = ctypes.c_size_t()
-        rc = self._lib.hbf_kv_attention_workspace_bytes(ctypes.byref(kv), ctypes.byref(at), ctypes.byref(b))
-        if rc != HBF_OK:
-            return rc
-        ws = self._attn_ws.get(b.value, self.pool.device, stream)
-        return self._lib.hbf_kv_attention(ctypes.byref(kv), ctypes.byref(at), _dp(self._attn_status), _dp(ws),
-                                          ws.numel(), _sp(stream))
+                           own_lens.data_ptr() if own_lens is not None else None, max_own, out.data_ptr(),
+                           _stride(out, 0), _stride(out, 1), None if lse is None else lse.data_ptr())
+        sizes = (rows, heads, prefix_len, max_own)
+        if sizes != self._attn_sizes:
+            b = ctypes.c_size_t()
+            rc = self._lib.hbf_kv_attention_workspace_bytes(kv, at, ctypes.byref(b))
+            if rc != HBF_OK:
+                return rc
+            self._attn_sizes, self._attn_bytes = sizes, b.value
+        ws = self._attn_ws.get(self._attn_bytes, self.pool.device, stream)
+        return self._lib.hbf_kv_attention(kv, at, self._attn_status.data_ptr(), ws.data_ptr(), ws.numel(),
+                                          _raw(stream))
+
+    def _layer(self, layer):
+        """The library's description of one layer's pages."""
+        kv = self._layers.get(layer)
+        if kv is None:
+            tok = self.kv_heads * self.head_dim
+            plane = self.pages * self.page_tokens * tok * 2
+            base = self.pool.data_ptr() + 2 * layer * plane
+            kv = self._layers[layer] = hbf_kv_layer(base, base + plane, self.page_tokens * tok, tok, self.head_dim,
+                                                    self.pages, self.page_tokens, self.kv_heads, self.head_dim,
+                                                    _dtype_code(self.pool))
+        return kv
 
 
 class MoeLayer:
@@ -733,17 +769,17 @@ class MoeLayer:
     def __init__(self, gate_up, down, topk, router=None, renormalize=True, max_tokens=64):
         import torch
         self._lib = load_library()
-        _strided(gate_up, "gate_up", _HALF, 3, 2)
-        name = (str(gate_up.dtype).replace("torch.", ""),)
-        _strided(down, "down", name, 3, 2)
+        _strided(gate_up, "gate_up", (torch.bfloat16, torch.float16), 3, 2)
+        dtype = (gate_up.dtype,)
+        _strided(down, "down", dtype, 3, 2)
         E, F2, H = gate_up.shape
         if F2 % 2 or tuple(down.shape) != (E, H, F2 // 2):
             raise HbfError(HBF_EINVAL, f"gate_up, down: shapes {tuple(gate_up.shape)}, {tuple(down.shape)}, expected "
                                        "[experts, 2 * ffn, hidden], [experts, hidden, ffn]")
         if router is not None:
-            _dev(router, "router", name, shape=(E, H))
+            _dev(router, "router", (str(gate_up.dtype).replace("torch.", ""),), shape=(E, H))
         self._keep = (gate_up, down, router)
-        self._name, self.topk, self.hidden, self.device = name, int(topk), H, gate_up.device
+        self._dtype, self.topk, self.hidden = dtype, int(topk), H
         self._m = hbf_moe(E, self.topk, H, F2 // 2, _dtype_code(gate_up), HBF_MOE_RENORM if renormalize else 0,
                           None if router is None else router.data_ptr(), gate_up.data_ptr(), down.data_ptr(),
                           _stride(gate_up, 0), _stride(down, 0))
@@ -760,17 +796,20 @@ class MoeLayer:
         """x, y: [tokens, hidden] (rows may be strided); ids: int32 [tokens,
         topk], weights: float32 [tokens, topk]: outputs, or the caller's
         choices where the layer has no router (-1: none)."""
-        _strided(x, "x", self._name, 2)
-        _writable(_strided(y, "y", self._name, 2), "y")
+        import torch
+        _strided(x, "x", self._dtype, 2)
+        _writable(_strided(y, "y", self._dtype, 2), "y")
         T = x.shape[0]
         if x.shape[1] != self.hidden or y.shape != x.shape:
             raise HbfError(HBF_EINVAL, f"x, y: shapes {tuple(x.shape)}, {tuple(y.shape)}, expected "
                                        f"[tokens, {self.hidden}]")
-        _dev(ids, "ids", _I32, shape=(T, self.topk))
-        _dev(weights, "weights", ("float32",), shape=(T, self.topk))
-        return self._lib.hbf_moe_layer(ctypes.byref(self._m), _dp(x), _stride(x, 0), T, _dp(ids), _dp(weights),
-                                       _dp(y), _stride(y, 0), _dp(self._status), _dp(self._ws), self._ws.numel(),
-                                       _sp(stream))
+        for t, what, dt in ((ids, "ids", torch.int32), (weights, "weights", torch.float32)):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dt and t.is_contiguous()
+                    and t.shape == (T, self.topk)):
+                _dev(t, what, (str(dt).replace("torch.", ""),), shape=(T, self.topk))
+        return self._lib.hbf_moe_layer(self._m, x.data_ptr(), _stride(x, 0), T, ids.data_ptr(), weights.data_ptr(),
+                                       y.data_ptr(), _stride(y, 0), self._status.data_ptr(), self._ws.data_ptr(),
+                                       self._ws.numel(), _raw(stream))
 
     def get_status(self, stream=None):
         """Synchronises; HBF_OK, or HBF_EINVAL if an id was out of range since
