@@ -48,16 +48,48 @@ __device__ __forceinline__ u32x2 read_transposed(const void *at) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)at));
 }
 
+// op over the wave, in every lane (op associative and commutative).
+template <typename V, typename F>
+__device__ __forceinline__ V across_wave(V x, F op) {
+  uint32_t u = __builtin_bit_cast(uint32_t, x);
+  auto join = [&](uint32_t a, uint32_t b) {
+    u = __builtin_bit_cast(uint32_t, op(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b)));
+  };
+  join(u, __builtin_amdgcn_update_dpp(u, u, 0xb1, 0xf, 0xf, false));   // quad_perm 1,0,3,2
+  join(u, __builtin_amdgcn_update_dpp(u, u, 0x4e, 0xf, 0xf, false));   // quad_perm 2,3,0,1
+  join(u, __builtin_amdgcn_update_dpp(u, u, 0x141, 0xf, 0xf, false));  // row_half_mirror
+  join(u, __builtin_amdgcn_update_dpp(u, u, 0x140, 0xf, 0xf, false));  // row_mirror
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  join(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  join(b[0], b[1]);
+  return __builtin_bit_cast(V, u);
+}
+
 // op over the four lanes that hold the same column of a tile (l % 16), in each of them.
 template <typename F>
 __device__ __forceinline__ float across_rows(float x, F op) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  uint32_t u = __builtin_bit_cast(uint32_t, x);
+  auto join = [&](uint32_t a, uint32_t b) {
+    u = __builtin_bit_cast(uint32_t, op(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)));
+  };
   const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const float y = op(__builtin_bit_cast(float, a[0]), __builtin_bit_cast(float, a[1]));
-  const uint32_t v = __builtin_bit_cast(uint32_t, y);
-  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return op(__builtin_bit_cast(float, b[0]), __builtin_bit_cast(float, b[1]));
+  join(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  join(b[0], b[1]);
+  return __builtin_bit_cast(float, u);
 }
+
+// Values that workgroups of one launch hand to each other: written past the
+// caches of one XCD, and read past them.  A writer waits for its stores
+// (stores_done) before it tells of them.
+__device__ __forceinline__ void hand_over(float *to, float v) {
+  __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float handed(const float *from) {
+  return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // What the lanes of one wave have written to LDS is read by others of it: the
 // LDS serves a wave's accesses in order, so only the compiler is held.

@@ -98,44 +98,28 @@ constexpr u32x4 ZERO4 = {0, 0, 0, 0};
 
 // ------------------------------------------------------------ route
 
-// Maximum over the wave, in every lane.
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#define HBF_DPP_MAX(ctrl) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, ctrl, 0xf, 0xf, false))
-  HBF_DPP_MAX(0xb1);   // quad_perm 1,0,3,2
-  HBF_DPP_MAX(0x4e);   // quad_perm 2,3,0,1
-  HBF_DPP_MAX(0x141);  // row_half_mirror
-  HBF_DPP_MAX(0x140);  // row_mirror
-#undef HBF_DPP_MAX
-  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = max(a[0], a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return max(b[0], b[1]);
-}
-
 // The topk choices of token t by one wave; lane l holds experts l EPL .. + EPL-1.
 template <int EPL>
-__device__ void choose(const Args &a, int t) {
+__device__ void choose(const Args &a, int t, int32_t *ids) {
   const int lane = threadIdx.x & 63, E = a.m.experts, k = a.m.topk;
   float v[EPL];
   uint32_t key[EPL];
-  float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < EPL; i++) {
     const int e = lane * EPL + i;
-    v[i] = e < E ? a.logits[(int64_t)t * a.e_pad + e] : 0.f;
+    v[i] = e < E ? handed(a.logits + (int64_t)t * a.e_pad + e) : 0.f;
     const uint32_t u = __float_as_uint(v[i]);
     // the floats' order as that of whole numbers; NaN below all, 0 for none (left)
     key[i] = e >= E ? 0 : isnan(v[i]) ? 1 : u & 0x80000000u ? ~u : u | 0x80000000u;
     if (key[i] == 0x7fffffffu) key[i] = 0x80000000u;  // -0 ties with 0
-    if (e < E) top = fmaxf(top, v[i]);
   }
-  float mine = 0.f;
+  float mine = 0.f, top = 0.f;  // top: the largest logit
   int chosen = 0;
   for (int j = 0; j < k; j++) {
     uint32_t best = key[0];
 #pragma unroll
     for (int i = 1; i < EPL; i++) best = max(best, key[i]);
-    const uint32_t all = wave_max(best);
+    const uint32_t all = across_wave(best, [](uint32_t x, uint32_t y) { return max(x, y); });
     const int from = __ffsll((unsigned long long)__ballot(best == all)) - 1;  // ties: the lowest index
     int e = 0;
     float val = 0.f;
@@ -152,13 +136,12 @@ __device__ void choose(const Args &a, int t) {
     }
     e = __builtin_amdgcn_readlane(e, from);
     val = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(val), from));
+    if (j == 0) top = val;
     if (lane == j) {
       chosen = e;
       mine = val;
     }
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   float w = lane < k ? expf(mine - top) : 0.f, sum = 0.f;
   if (a.m.flags & HBF_MOE_RENORM) {
     sum = w;
@@ -167,26 +150,24 @@ __device__ void choose(const Args &a, int t) {
     for (int i = 0; i < EPL; i++)
       if (lane * EPL + i < E) sum += expf(v[i] - top);
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+  sum = across_wave(sum, [](float x, float y) { return x + y; });
   if (lane < k) {
-    a.ids[t * k + lane] = chosen;
+    ids[t * k + lane] = chosen;  // (LDS: complete where this workgroup chooses for all tokens)
+    __hip_atomic_store(a.ids + t * k + lane, chosen, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     a.weights[t * k + lane] = w / sum;
   }
 }
 
-// This workgroup's part is written.  True in every thread of the last of n
-// workgroups to get here, which then sees what all of them wrote; the counter
-// is 0 again.
+// True in every thread of the last of n workgroups to get here; the counter is
+// 0 again.  What a workgroup hands over before, its stores done, the last one
+// finds.
 __device__ bool last_of(uint32_t *counter, uint32_t n) {
   __shared__ uint32_t last;
   __syncthreads();
   if (n == 1) return true;
   if (threadIdx.x == 0) {
-    __threadfence();
-    last = atomicAdd(counter, 1) + 1 == n;
-    if (last) *counter = 0;
-    __threadfence();
+    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == n;
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   return last != 0;
@@ -197,7 +178,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
   __shared__ f32x4 red[ROUTE_WAVES][64];
   __shared__ int32_t ids[MAX_PAIRS];
   __shared__ int32_t cnt[MOE_MAX_EXPERTS];
-  __shared__ uint32_t wsum[ROUTE_WAVES], asum[ROUTE_WAVES];
+  __shared__ uint32_t wsum[ROUTE_WAVES];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   const int E = a.m.experts, H = a.m.hidden, pairs = a.tokens * a.m.topk;
   if (a.m.dev_router) {
@@ -226,18 +207,26 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
     if (w == 0) {
 #pragma unroll
       for (int i = 1; i < ROUTE_WAVES; i++) acc += red[i][lane];
-      if (t0 + col < a.tokens) *(f32x4 *)(a.logits + (int64_t)(t0 + col) * a.e_pad + e0 + kg * 4) = acc;
+      if (t0 + col < a.tokens)
+#pragma unroll
+        for (int i = 0; i < 4; i++) hand_over(a.logits + (int64_t)(t0 + col) * a.e_pad + e0 + kg * 4 + i, acc[i]);
+      stores_done();
     }
     const int tile = blockIdx.x / e_tiles;
     if (!last_of(&a.ctl->arrived[tile], e_tiles)) return;
     for (int tt = t0 + w; tt < min(t0 + 16, a.tokens); tt += ROUTE_WAVES) {
-      if (E <= 64) choose<1>(a, tt);
-      else if (E <= 128) choose<2>(a, tt);
-      else if (E <= 256) choose<4>(a, tt);
-      else choose<16>(a, tt);
+      if (E <= 64) choose<1>(a, tt, ids);
+      else if (E <= 128) choose<2>(a, tt, ids);
+      else if (E <= 256) choose<4>(a, tt, ids);
+      else choose<16>(a, tt, ids);
     }
-    if (!last_of(&a.ctl->chosen, gridDim.x / e_tiles)) return;
-    for (int p = threadIdx.x; p < pairs; p += ROUTE_THREADS) ids[p] = a.ids[p];
+    const int t_tiles = gridDim.x / e_tiles;
+    if (t_tiles > 1) {
+      stores_done();
+      if (!last_of(&a.ctl->chosen, t_tiles)) return;
+      for (int p = threadIdx.x; p < pairs; p += ROUTE_THREADS)
+        ids[p] = __hip_atomic_load(a.ids + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
   } else {
     for (int p = threadIdx.x; p < pairs; p += ROUTE_THREADS) {
       const int e = a.ids[p];
@@ -254,31 +243,24 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
   __syncthreads();
   constexpr int PER = MOE_MAX_EXPERTS / ROUTE_THREADS;
   int c[PER];
-  uint32_t sum = 0, act = 0;
+  uint32_t sum = 0;  // pairs, and tiles above them
 #pragma unroll
   for (int i = 0; i < PER; i++) {
     c[i] = cnt[threadIdx.x * PER + i];
-    sum += c[i];
-    act += (c[i] + 15) / 16;
+    sum += c[i] + ((uint32_t)(c[i] + 15) / 16 << 16);
   }
-  uint32_t xs = sum, xa = act;
+  uint32_t x = sum;
+#pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t ys = __shfl_up(xs, d), ya = __shfl_up(xa, d);
-    if (lane >= d) {
-      xs += ys;
-      xa += ya;
-    }
+    const uint32_t y = __shfl_up(x, d);
+    if (lane >= d) x += y;
   }
-  if (lane == 63) {
-    wsum[w] = xs;
-    asum[w] = xa;
-  }
+  if (lane == 63) wsum[w] = x;
   __syncthreads();
-  uint32_t at = xs - sum, ti = xa - act;
-  for (int i = 0; i < w; i++) {
-    at += wsum[i];
-    ti += asum[i];
-  }
+  x -= sum;
+#pragma unroll
+  for (int i = 0; i < ROUTE_WAVES; i++) x += i < w ? wsum[i] : 0;
+  uint32_t at = x & 0xffff, ti = x >> 16;
 #pragma unroll
   for (int i = 0; i < PER; i++) {
     for (int j = 0; j < c[i]; j += 16)
