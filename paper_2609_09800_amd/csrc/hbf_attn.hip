@@ -9,11 +9,13 @@
 // batch.  Own tokens are met by one row's G queries.  Both run in one launch,
 // each workgroup taking a part of the token axis for some queries:
 //  - few queries (own tokens; a prefix with at most 32 of them): bound by
-//    memory.  Each of four waves takes 32 tokens at a time, K straight from
+//    memory.  Each of eight waves takes 32 tokens at a time, K straight from
 //    memory into the matrix operand, V through LDS for its transpose, the next
 //    tokens' loads in flight meanwhile; the waves meet once, at the end.
 //  - many queries: bound by the matrix cores and the LDS.  64 tokens are staged
-//    for four waves of 32 queries each.
+//    for four waves of 32 queries each; two such groups of waves take turns
+//    with the tokens of a part, which halves the parts that leave the chip's
+//    registers (520 bytes a query and part).
 // Scores are computed transposed, S^T = K Q^T: a lane then holds one query's
 // scores of four consecutive tokens per tile of 16, which, rounded, are
 // already the operand of O^T = V^T P^T (the order of the tokens within a step
@@ -28,17 +30,22 @@
 namespace hbf {
 namespace {
 
-constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int THREADS = 512, WAVES = THREADS / 64;
 constexpr int FEW_TILE = 32;    // tokens of a wave's step where queries are few
 constexpr int MANY_TILE = 64;   // tokens staged where they are many
 constexpr int MANY_Q = 128;     // queries per workgroup there
+constexpr int MANY_GROUPS = 2;  // groups of MANY_Q / 32 waves, each with tokens of its own
+constexpr int JOIN_THREADS = 256, JOIN_WAVES = JOIN_THREADS / 64;
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
 struct Args {
   hbf_kv_layer kv;
   hbf_attention at;
   int group;            // query heads per KV head
-  float c;              // scale * log2(e)
+  float c;              // |scale| * log2(e), not 0
+  uint32_t flip;        // sign bits of two 16-bit values if the scale is negative
+  uint32_t page_mul;    // token / page_tokens = token * page_mul >> page_shift, for tokens below 2^31
+  int page_shift;
   int few_q;            // the prefix's queries per workgroup if they are few (16 or 32), else 0
   int m_tiles;          // workgroups across the prefix's queries
   int prefix_splits;
@@ -68,38 +75,52 @@ __device__ __forceinline__ u32x4 v_operand(const char *v, int t0, int t1, int dt
   return u32x4{a[0], a[1], b[0], b[1]};
 }
 
-__device__ __forceinline__ float max_of_groups(float x) {  // over the four lanes of a query
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float sum_of_groups(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
+constexpr auto MAX_OP = [](float a, float b) { return fmaxf(a, b); };
+constexpr auto SUM_OP = [](float a, float b) { return a + b; };
 
-// One step of the running softmax for one query (column): U tiles of 16 tokens'
-// scores s (already times c, masked with -infinity) become probabilities.
-// Returns the factor for what was summed before.
-template <int U>
-__device__ __forceinline__ float softmax_step(f32x4 *s, float &m, float &l) {
-  float mx = -INFINITY;
+// One step of the running softmax for QT queries per lane (columns): their
+// scores s of U tiles of 16 tokens become probabilities exp2((s - m) c), and l
+// collects the lane's own.  m is any number that keeps exp2 in range, the same
+// in a column's four lanes: it moves up, to the maximum so far, only where a
+// score passes it by more than LAZY / c (then p <= 2^LAZY otherwise), which
+// few steps do, and then what was summed before is scaled.
+constexpr float LAZY = 8.f;
+template <int QT, int U, int DT>
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[QT][U], float c, float (&m)[QT], float (&l)[QT],
+                                             f32x4 (&o)[QT][DT]) {
+  float mx[QT];
+  bool up = false;
 #pragma unroll
-  for (int u = 0; u < U; u++)
+  for (int q = 0; q < QT; q++) {
+    mx[q] = s[q][0][0];
 #pragma unroll
-    for (int i = 0; i < 4; i++) mx = fmaxf(mx, s[u][i]);
-  mx = fmaxf(m, max_of_groups(mx));
-  const float ref = mx == -INFINITY ? 0.f : mx;  // nothing seen yet: every p is 0
-  const float alpha = __builtin_amdgcn_exp2f(m - ref);
-  m = mx;
-  l *= alpha;
+    for (int u = 0; u < U; u++)
 #pragma unroll
-  for (int u = 0; u < U; u++)
+      for (int i = 0; i < 4; i++) mx[q] = fmaxf(mx[q], s[q][u][i]);
+    up |= mx[q] * c > m[q] * c + LAZY;
+  }
+  if (__any(up)) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      s[u][i] = __builtin_amdgcn_exp2f(s[u][i] - ref);
-      l += s[u][i];
+    for (int q = 0; q < QT; q++) {
+      const float top = fmaxf(m[q], across_rows(mx[q], MAX_OP));
+      const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[q] - top) * c);
+      m[q] = top;
+      l[q] *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; d++) o[q][d] *= alpha;
     }
-  return alpha;
+  }
+#pragma unroll
+  for (int q = 0; q < QT; q++) {
+    const float ref = m[q] == -INFINITY ? 0.f : -m[q] * c;  // nothing seen yet: every p is 0
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        s[q][u][i] = __builtin_amdgcn_exp2f(fmaf(s[q][u][i], c, ref));
+        l[q] += s[q][u][i];
+      }
+  }
 }
 
 template <typename T>
@@ -107,16 +128,19 @@ __device__ __forceinline__ u32x4 p_operand(f32x4 a, f32x4 b) {
   return u32x4{pack2<T>(a[0], a[1]), pack2<T>(a[2], a[3]), pack2<T>(b[0], b[1]), pack2<T>(b[2], b[3])};
 }
 
+__device__ __forceinline__ uint32_t page_index(const Args &a, uint32_t token) {
+  return (uint32_t)((uint64_t)token * a.page_mul >> a.page_shift);
+}
 // Page of a token, with a page id out of range noted and page 0 read instead.
 __device__ __forceinline__ int page_of(const Args &a, const int32_t *pages, uint32_t token, bool *bad) {
-  const int p = pages[token / (uint32_t)a.kv.page_tokens];
+  const int p = pages[page_index(a, token)];
   if (p >= 0 && p < a.kv.pages) return p;
   *bad = true;
   return 0;
 }
 __device__ __forceinline__ int64_t token_at(const Args &a, int page, uint32_t token, int head) {
-  return (int64_t)page * a.kv.page_stride + (int64_t)(token % (uint32_t)a.kv.page_tokens) * a.kv.token_stride +
-         (int64_t)head * a.kv.head_stride;
+  const uint32_t in_page = token - page_index(a, token) * (uint32_t)a.kv.page_tokens;
+  return page * a.kv.page_stride + in_page * a.kv.token_stride + head * a.kv.head_stride;
 }
 
 struct Query {
@@ -132,7 +156,7 @@ __device__ __forceinline__ void load_query(const Args &a, Query q, int kgroup, u
                   2 * ((q.row < 0 ? 0 : q.row) * a.at.q_row_stride + (q.row < 0 ? 0 : q.head) * a.at.q_head_stride);
 #pragma unroll
   for (int k = 0; k < D / 32; k++) {
-    const u32x4 v = *(const u32x4 *)(p + (k * 32 + kgroup * 8) * 2);
+    const u32x4 v = *(const u32x4 *)(p + (k * 32 + kgroup * 8) * 2) ^ a.flip;
     out[k] = q.row < 0 ? u32x4{0, 0, 0, 0} : v;
   }
 }
@@ -208,28 +232,23 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
         load(base + STEP);
         if (t1 - base > 2 * STEP) find(base + 2 * STEP);
       }
+      if (tail)
+#pragma unroll
+        for (int q = 0; q < QT; q++)
+#pragma unroll
+          for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+              if (base + u * 16 + kg * 4 + i >= t1) s[q][u][i] = -INFINITY;
+      softmax_step<QT, 2, DT>(s, a.c, m, l, o);
       u32x4 p[QT];
-      float alpha[QT];
 #pragma unroll
-      for (int q = 0; q < QT; q++) {
-#pragma unroll
-        for (int u = 0; u < 2; u++)
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            const float x = s[q][u][i] * a.c;
-            s[q][u][i] = !tail || base + u * 16 + kg * 4 + i < t1 ? x : -INFINITY;
-          }
-        alpha[q] = softmax_step<2>(s[q], m[q], l[q]);
-        p[q] = p_operand<T>(s[q][0], s[q][1]);
-      }
+      for (int q = 0; q < QT; q++) p[q] = p_operand<T>(s[q][0], s[q][1]);
 #pragma unroll
       for (int d = 0; d < DT; d++) {
         const u32x4 v = v_operand<D>(vt, kg * 4, 16 + kg * 4, d, lane);
 #pragma unroll
-        for (int q = 0; q < QT; q++) {
-          o[q][d] *= alpha[q];
-          o[q][d] = T::mfma(v, p[q], o[q][d]);
-        }
+        for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q], o[q][d]);
       }
       wave_lds_fence();
       if (!more) break;
@@ -244,12 +263,12 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
 #pragma unroll
   for (int q = 0; q < QT; q++) {
-    const float lq = sum_of_groups(l[q]);
-    if (kg == 0) rml[w * 16 + col] = make_float2(m[q], lq);
+    const float lq = across_rows(l[q], SUM_OP);
+    if (kg == 0) rml[w * 16 + col] = make_float2(m[q] * a.c, lq);
 #pragma unroll
     for (int d = 0; d < DT; d++) *(f32x4 *)(ro + (w * 16 + col) * RS + d * 16 + kg * 4) = o[q][d];
     __syncthreads();
-    const int n = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 4;
+    const int n = threadIdx.x >> 5, d0 = (threadIdx.x & 31) * 4;
     const Query qq = query(q * 16 + n);
     if (qq.row >= 0) {
       float mx = -INFINITY, sum = 0.f;
@@ -263,12 +282,11 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
         sum += f[i] * rml[i * 16 + n].y;
       }
       const int64_t slot = part_slot(a, split, qq);
-#pragma unroll
-      for (int d = d0; d < D; d += 64) {
+      if (d0 < D) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < WAVES; i++) x += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
-        *(f32x4 *)(a.part + slot * D + d) = x;
+        for (int i = 0; i < WAVES; i++) x += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d0);
+        *(f32x4 *)(a.part + slot * D + d0) = x;
       }
       if (d0 == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum);
     }
@@ -282,31 +300,24 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
 template <typename T, int D>
 __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int split, int m0, char *lds) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
+  constexpr int GW = MANY_Q / 32, GT = GW * 64;  // waves and threads of a group
+  const int group = w / GW, gw = w % GW, gt = threadIdx.x % GT;
   constexpr int KS = D / 32, DT = D / 16, QT = 2, U = MANY_TILE / 16;
   constexpr int TILE_BYTES = MANY_TILE * D * 2;
+  char *mine = lds + group * 4 * TILE_BYTES;  // K and V of one step, then of the next
   auto query = [&](int n) {
     const int mm = m0 + n;
     const int row = mm / a.group;
     return row < a.at.rows ? Query{row, head * a.group + mm - row * a.group} : Query{-1, 0};
   };
-  u32x4 qv[QT][KS];
-#pragma unroll
-  for (int q = 0; q < QT; q++) load_query<T, D>(a, query(w * 32 + q * 16 + col), kg, qv[q]);
-  f32x4 o[QT][DT];
-  float m[QT], l[QT];
-#pragma unroll
-  for (int q = 0; q < QT; q++) {
-    m[q] = -INFINITY;
-    l[q] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
   // staging: four threads per token, each every fourth 16-byte piece
-  const int st = threadIdx.x >> 2, sp = threadIdx.x & 3;
+  const int st = gt >> 2, sp = gt & 3;
   constexpr int SP = D / 32;
+  constexpr uint32_t STEP = MANY_GROUPS * MANY_TILE;
   u32x4 kv[SP], vv[SP];
   bool bad = false;
   int page = 0;
+  uint32_t base = t0 + group * MANY_TILE;
   auto find = [&](uint32_t b) { page = page_of(a, a.at.dev_prefix_pages, min(b + st, t1 - 1), &bad); };
   auto load = [&](uint32_t b) {
     const int64_t at = 2 * (token_at(a, page, min(b + st, t1 - 1), head) + sp * 8);
@@ -316,101 +327,128 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
       vv[k] = *(const u32x4 *)((const char *)a.kv.dev_v + at + k * 64);
     }
   };
-  auto store = [&](uint32_t b, char *buf) {
+  auto store = [&](uint32_t b, char *to) {
     const bool on = b + st < t1;  // behind the last token: zero, whatever lies there
 #pragma unroll
     for (int k = 0; k < SP; k++) {
-      *(u32x4 *)(buf + tile_at<D>(st, k * 4 + sp)) = kv[k];
-      *(u32x4 *)(buf + TILE_BYTES + tile_at<D>(st, k * 4 + sp)) = on ? vv[k] : u32x4{0, 0, 0, 0};
+      *(u32x4 *)(to + tile_at<D>(st, k * 4 + sp)) = kv[k];
+      *(u32x4 *)(to + TILE_BYTES + tile_at<D>(st, k * 4 + sp)) = on ? vv[k] : u32x4{0, 0, 0, 0};
     }
   };
-  find(t0);
-  load(t0);
-  store(t0, lds);
-  if (t1 - t0 > MANY_TILE) {
-    find(t0 + MANY_TILE);
-    load(t0 + MANY_TILE);
-    if (t1 - t0 > 2 * MANY_TILE) find(t0 + 2 * MANY_TILE);
+  find(base);
+  u32x4 qv[QT][KS];
+#pragma unroll
+  for (int q = 0; q < QT; q++) load_query<T, D>(a, query(gw * 32 + q * 16 + col), kg, qv[q]);
+  load(base);
+  f32x4 o[QT][DT];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int q = 0; q < QT; q++) {
+    m[q] = -INFINITY;
+    l[q] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  find(base + STEP);
+  store(base, mine);
+  load(base + STEP);  // (past the end: the last token again)
+  find(base + 2 * STEP);
   __syncthreads();
   int cur = 0;
-  for (uint32_t base = t0;; base += MANY_TILE) {
-    const char *kt = lds + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
-    f32x4 s[QT][U];
+  for (uint32_t b0 = t0;;) {
+    const char *kt = mine + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+    if (base < t1) {
+      f32x4 s[QT][U];
 #pragma unroll
-    for (int u = 0; u < U; u++) {
+      for (int u = 0; u < U; u++) {
 #pragma unroll
-      for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; k++) {
-        const u32x4 kk = *(const u32x4 *)(kt + tile_at<D>(u * 16 + col, k * 4 + kg));
+        for (int k = 0; k < KS; k++) {
+          const u32x4 kk = *(const u32x4 *)(kt + tile_at<D>(u * 16 + col, k * 4 + kg));
 #pragma unroll
-        for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
-      }
-    }
-    const bool tail = t1 - base < MANY_TILE;
-    float alpha[QT];
-    u32x4 p[QT][U / 2];
-#pragma unroll
-    for (int q = 0; q < QT; q++) {
-#pragma unroll
-      for (int u = 0; u < U; u++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const float x = s[q][u][i] * a.c;
-          s[q][u][i] = !tail || base + u * 16 + kg * 4 + i < t1 ? x : -INFINITY;
+          for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
         }
-      alpha[q] = softmax_step<U>(s[q], m[q], l[q]);
+      }
+      if (t1 - base < MANY_TILE)
 #pragma unroll
-      for (int u = 0; u < U / 2; u++) p[q][u] = p_operand<T>(s[q][2 * u], s[q][2 * u + 1]);
-    }
+        for (int q = 0; q < QT; q++)
 #pragma unroll
-    for (int d = 0; d < DT; d++) {
+          for (int u = 0; u < U; u++)
 #pragma unroll
-      for (int q = 0; q < QT; q++) o[q][d] *= alpha[q];
+            for (int i = 0; i < 4; i++)
+              if (base + u * 16 + kg * 4 + i >= t1) s[q][u][i] = -INFINITY;
+      softmax_step<QT, U, DT>(s, a.c, m, l, o);
+      u32x4 p[QT][U / 2];
 #pragma unroll
-      for (int u = 0; u < U / 2; u++) {
-        const u32x4 v = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
+      for (int q = 0; q < QT; q++)
 #pragma unroll
-        for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][u], o[q][d]);
+        for (int u = 0; u < U / 2; u++) p[q][u] = p_operand<T>(s[q][2 * u], s[q][2 * u + 1]);
+#pragma unroll
+      for (int d = 0; d < DT; d++) {
+#pragma unroll
+        for (int u = 0; u < U / 2; u++) {
+          const u32x4 v = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
+#pragma unroll
+          for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][u], o[q][d]);
+        }
       }
     }
-    if (t1 - base <= MANY_TILE) break;
-    const uint32_t next = base + MANY_TILE;
-    store(next, lds + (cur ^ 1) * 2 * TILE_BYTES);
-    if (t1 - next > MANY_TILE) {
-      load(next + MANY_TILE);
-      if (t1 - next > 2 * MANY_TILE) find(next + 2 * MANY_TILE);
+    if (t1 - b0 <= STEP) break;
+    b0 += STEP;
+    base += STEP;
+    store(base, mine + (cur ^ 1) * 2 * TILE_BYTES);
+    if (t1 - b0 > STEP) {
+      load(base + STEP);
+      find(base + 2 * STEP);
     }
     __syncthreads();
     cur ^= 1;
   }
   const bool any_bad = __syncthreads_or(bad);
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
+  // the second group's sums join the first's, lane by lane
+  f32x4 *ro = (f32x4 *)lds;  // [QT][DT][GT]
+  float2 *rml = (float2 *)(lds + QT * DT * GT * 16);
+  if (group == 1) {
+#pragma unroll
+    for (int q = 0; q < QT; q++) {
+#pragma unroll
+      for (int d = 0; d < DT; d++) ro[(q * DT + d) * GT + gt] = o[q][d];
+      rml[q * GT + gt] = make_float2(m[q], l[q]);
+    }
+  }
+  __syncthreads();
+  if (group == 1) return;
 #pragma unroll
   for (int q = 0; q < QT; q++) {
-    const Query qq = query(w * 32 + q * 16 + col);
-    const float lq = sum_of_groups(l[q]);
+    const float2 other = rml[q * GT + gt];
+    const float top = fmaxf(m[q], other.x);
+    const float f0 = m[q] == top ? 1.f : __builtin_amdgcn_exp2f((m[q] - top) * a.c);
+    const float f1 = other.x == top ? 1.f : __builtin_amdgcn_exp2f((other.x - top) * a.c);
+    const float lq = across_rows(f0 * l[q] + f1 * other.y, SUM_OP);
+    const Query qq = query(gw * 32 + q * 16 + col);
     if (qq.row < 0) continue;
     const int64_t slot = part_slot(a, split, qq);
 #pragma unroll
-    for (int d = 0; d < DT; d++) *(f32x4 *)(a.part + slot * D + d * 16 + kg * 4) = o[q][d];
-    if (kg == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(m[q], lq);
+    for (int d = 0; d < DT; d++)
+      *(f32x4 *)(a.part + slot * D + d * 16 + kg * 4) = f0 * o[q][d] + f1 * ro[(q * DT + d) * GT + gt];
+    if (kg == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(top * a.c, lq);
   }
 }
 
 template <int D>
 constexpr int lds_bytes() {
-  const int many_b = 4 * MANY_TILE * D * 2, few_b = WAVES * FEW_TILE * D * 2;
-  const int join_b = WAVES * 16 * (D + 4) * 4 + WAVES * 16 * 8;
-  return many_b > few_b ? (many_b > join_b ? many_b : join_b) : (few_b > join_b ? few_b : join_b);
+  const int many_b = MANY_GROUPS * 4 * MANY_TILE * D * 2;  // K and V, twice; the groups' join is smaller
+  const int few_b = WAVES * 16 * (D + 4) * 4 + WAVES * 16 * 8;  // the waves' join; V is smaller
+  return many_b > few_b ? many_b : few_b;
 }
 
 // Workgroups [0, prefix_blocks): the prefix, those of one part and KV head on
 // one XCD (block numbers equal modulo 8) so that they share its L2.  Then the
 // own tokens'.
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
+__global__ __launch_bounds__(THREADS) void k_attn(Args a) {
   __shared__ __align__(16) char lds[lds_bytes<D>()];
   int b = blockIdx.x;
   if (b < a.prefix_blocks) {
@@ -455,12 +493,13 @@ __global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
                min(t0 + (uint32_t)a.own_chunk, (uint32_t)len), head, a.prefix_splits + split, query, lds);
 }
 
-// Join a query's parts, a wave each.
+// Join a query's parts: a workgroup per query, its waves taking every fourth part.
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS) void k_attn_join(Args a) {
-  const int64_t qi = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
-  if (qi >= (int64_t)a.at.rows * a.at.heads) return;
-  const int lane = threadIdx.x & 63;
+__global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
+  constexpr int V = D / 64;
+  __shared__ float so[JOIN_WAVES][D], sm[JOIN_WAVES], sl[JOIN_WAVES];
+  const int64_t qi = blockIdx.x;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int row = (int)(qi / a.at.heads), head = (int)(qi - (int64_t)row * a.at.heads);
   int own = 0;
   bool bad = false;
@@ -471,38 +510,66 @@ __global__ __launch_bounds__(THREADS) void k_attn_join(Args a) {
   }
   const int n = a.prefix_splits + own;
   const int64_t stride = (int64_t)a.at.rows * a.at.heads;
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 64) {
-    const float x = a.part_ml[i * stride + qi].x;
-    bad |= isnan(x);
-    m = fmaxf(m, x);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  bad = __any(bad);
-  if (bad && a.status && lane == 0) *a.status = HBF_EINVAL;
-  const float ref = m == -INFINITY ? 0.f : m;
-  constexpr int V = D / 64;
-  float o[V], l = 0.f;
+  float m = -INFINITY, l = 0.f, o[V];
 #pragma unroll
   for (int v = 0; v < V; v++) o[v] = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < n; i++) {
-    const float2 ml = a.part_ml[i * stride + qi];
-    const float *p = a.part + (i * stride + qi) * D + lane * V;
-    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-    l += f * ml.y;
+  // sums relative to a first maximum, raised as parts of larger ones come (NaN, a part of bad pages, stays)
+  constexpr int U = 8;
+  for (int i0 = w; i0 < n; i0 += JOIN_WAVES * U) {
+    float2 ml[U];
+    float p[U][V];
 #pragma unroll
-    for (int v = 0; v < V; v++) o[v] += f * p[v];
+    for (int u = 0; u < U; u++) {
+      const int i = i0 + u * JOIN_WAVES;
+      ml[u] = i < n ? a.part_ml[i * stride + qi] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int v = 0; v < V; v++) p[u][v] = i < n ? a.part[(i * stride + qi) * D + lane * V + v] : 0.f;
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < U; u++) top = fmaxf(top, ml[u].x);
+    const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
+    m = top;
+    l *= alpha;
+#pragma unroll
+    for (int v = 0; v < V; v++) o[v] *= alpha;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
+      l += f * ml[u].y;
+#pragma unroll
+      for (int v = 0; v < V; v++) o[v] += f * p[u][v];
+    }
   }
-  if (bad) l = NAN;
-  const float inv = n == 0 ? 0.f : 1.f / l;
+#pragma unroll
+  for (int v = 0; v < V; v++) so[w][lane * V + v] = o[v];
+  sm[w] = m;
+  sl[w] = l;
+  __syncthreads();
+  if (w) return;
+#pragma unroll
+  for (int i = 1; i < JOIN_WAVES; i++) m = fmaxf(m, sm[i]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  l = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; v++) o[v] = 0.f;
+#pragma unroll
+  for (int i = 0; i < JOIN_WAVES; i++) {
+    const float f = __builtin_amdgcn_exp2f(sm[i] - ref);
+    l += f * sl[i];
+#pragma unroll
+    for (int v = 0; v < V; v++) o[v] += f * so[i][lane * V + v];
+  }
+  if (bad) {
+    l = NAN;
+    if (a.status && lane == 0) *a.status = HBF_EINVAL;
+  }
+  const float inv = n == 0 && !bad ? 0.f : 1.f / l;
   typename T::elem *out =
       (typename T::elem *)a.at.dev_out + row * a.at.out_row_stride + head * a.at.out_head_stride + lane * V;
 #pragma unroll
-  for (int v = 0; v < V; v++) out[v] = (typename T::elem)(bad ? NAN : o[v] * inv);
-  if (a.at.dev_lse && lane == 0)
-    a.at.dev_lse[qi] = bad ? NAN : n == 0 ? -INFINITY : m * LN2 + logf(l);
+  for (int v = 0; v < V; v++) out[v] = (typename T::elem)(o[v] * inv);
+  if (a.at.dev_lse && lane == 0) a.at.dev_lse[qi] = n == 0 && !bad ? -INFINITY : m * LN2 + logf(l);
 }
 
 // Sizes of a call: how the token axes are cut.
@@ -511,25 +578,31 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
   a.kv = kv;
   a.at = at;
   a.group = at.heads / kv.kv_heads;
-  a.c = at.scale * LOG2E;
+  a.c = std::max(fabsf(at.scale) * LOG2E, 1e-30f);  // (as flat as 0 is, and -infinity times it stays that)
+  a.flip = at.scale < 0 ? 0x80008000u : 0;
+  // with M = ceil(2^k / d), k = 31 + ceil(log2 d): token * M / 2^k is at most token / 2^31 < 1 / d above token / d
+  while ((1 << a.page_shift) < kv.page_tokens) a.page_shift++;
+  a.page_shift += 31;
+  a.page_mul = (uint32_t)(((uint64_t(1) << a.page_shift) + kv.page_tokens - 1) / kv.page_tokens);
   const int64_t m = (int64_t)at.rows * a.group;
   a.few_q = m <= 16 ? 16 : m <= 32 ? 32 : 0;
   a.m_tiles = (int)(a.few_q ? 1 : (m + MANY_Q - 1) / MANY_Q);
   a.own_tiles = (a.group + 15) / 16;
-  // parts so that the chip's 256 CUs have two workgroups each, no shorter than a step of the waves
-  constexpr int64_t WANT = 512;
-  auto cut = [](int64_t tokens, int64_t others, int64_t step, int *chunk) {
-    if (tokens <= 0 || others <= 0) return 0;
-    int64_t n = (WANT + others - 1) / others;
-    n = std::max<int64_t>(1, std::min(n, (tokens + step - 1) / step));
-    int64_t c = (tokens + n - 1) / n;
-    c = (c + step - 1) / step * step;
-    *chunk = (int)std::min<int64_t>(c, INT32_MAX / 2 / step * step);
+  // Parts: a workgroup per CU, the prefix's and the own ones' shares of the 256 as their shares of the work, in steps of a
+  // workgroup (128 tokens for many queries, 256 for few; rows' own tokens taken to be half of the most there can be).
+  const int64_t pre_step = a.few_q ? WAVES * FEW_TILE : MANY_GROUPS * MANY_TILE, own_step = WAVES * FEW_TILE;
+  const int64_t pre_groups = (int64_t)kv.kv_heads * a.m_tiles, own_groups = (int64_t)at.rows * kv.kv_heads * a.own_tiles;
+  const int64_t pre_steps = (at.prefix_len + pre_step - 1) / pre_step, own_steps = (at.max_own + own_step - 1) / own_step;
+  const double pre_work = (double)pre_groups * pre_steps, own_work = (double)own_groups * own_steps / 2;
+  auto cut = [](int64_t tokens, int64_t all, int64_t step, double groups, int *chunk) {
+    if (tokens <= 0) return 0;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(all, (int64_t)groups)), each = (all + parts - 1) / parts;
+    *chunk = (int)std::min<int64_t>(each * step, INT32_MAX / 2 / step * step);
     return (int)((tokens + *chunk - 1) / *chunk);
   };
-  a.prefix_splits = cut(at.prefix_len, (int64_t)kv.kv_heads * a.m_tiles, a.few_q ? 4 * FEW_TILE : MANY_TILE,
-                        &a.prefix_chunk);
-  a.own_splits = cut(at.max_own, (int64_t)at.rows * kv.kv_heads * a.own_tiles, 4 * FEW_TILE, &a.own_chunk);
+  const double slots = 256.0 / (pre_work + own_work + 1e-9);
+  a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, slots * pre_work / pre_groups, &a.prefix_chunk);
+  a.own_splits = cut(at.max_own, own_steps, own_step, slots * own_work / std::max<int64_t>(1, own_groups), &a.own_chunk);
   a.prefix_blocks = (a.prefix_splits * kv.kv_heads + 7) / 8 * 8 * a.m_tiles;
   return a;
 }
@@ -539,7 +612,7 @@ hipError_t run(const Args &a, hipStream_t s) {
   const int64_t blocks =
       a.prefix_blocks + (int64_t)a.own_splits * a.at.rows * a.kv.kv_heads * a.own_tiles;
   if (blocks > 0) k_attn<T, D><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
-  k_attn_join<T, D><<<(uint32_t)(((int64_t)a.at.rows * a.at.heads + WAVES - 1) / WAVES), THREADS, 0, s>>>(a);
+  k_attn_join<T, D><<<(uint32_t)a.at.rows * a.at.heads, JOIN_THREADS, 0, s>>>(a);
   return hipGetLastError();
 }
 
