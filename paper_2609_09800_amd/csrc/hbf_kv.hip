@@ -2,14 +2,17 @@
 // copying and compacting sequences, and writing tokens.
 //
 // Nothing here is arithmetic: a call moves the bytes of whole tokens or pages
-// and the whole numbers of the tables.  A call that takes or moves pages is
-// two or three launches.  The plan checks every entry and counts the free
-// pages by tiles of refs; its last workgroup turns the tiles' counts into
-// offsets and decides whether the call goes ahead, so that a refused call has
-// changed nothing.  The launches after it find each free page's rank from its
-// tile's offset, and the entry that the rank belongs to by a search in the
-// entries' offsets: the k-th free page, in page order, serves the k-th need, in
-// list order, whatever runs first.
+// and the whole numbers of the tables.  A call that takes or moves pages first
+// checks every entry and counts the free pages, and changes something only if
+// all of it can be done.  Then each free page's rank, from counts of those
+// before it, gives the entry it serves, by a search in the entries' offsets: the
+// k-th free page, in page order, serves the k-th need, in list order, whatever
+// runs first.
+//
+// Small calls (SMALL_PAGES, SMALL_ENTRIES) are bound by latency, and one
+// workgroup does all of that in one launch.  In larger ones many workgroups check
+// and count, the last of them to finish turns the counts into offsets and
+// decides, and another launch applies.
 #include "hbf_half.h"
 #include "hbf_ops.h"
 
@@ -17,10 +20,16 @@ namespace hbf {
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int ONE = 1024;                         // threads of a workgroup that does a call by itself
 constexpr int PER_THREAD = 16;
-constexpr int TILE = THREADS * PER_THREAD;        // pages per tile
+constexpr int TILE = THREADS * PER_THREAD;        // pages per workgroup in large calls
 constexpr int MAX_TILES = KV_MAX_PAGES / TILE;
 static_assert(MAX_TILES <= THREADS, "one thread per tile in the plan's end");
+constexpr int SMALL_PAGES = ONE * PER_THREAD;
+constexpr int SMALL_ENTRIES = 1 << 16;            // table entries that the call can touch
+constexpr int SMALL_LIST = 1024;
+constexpr int ROW = 16;                           // threads per table row there: many rows' latencies side by side
+constexpr uint64_t SMALL_COPY = 256 << 10;        // bytes of pages that one workgroup copies sooner than a launch does
 constexpr int COPY_BYTES = 16384;                 // bytes a workgroup copies at a time
 constexpr int MOVE_GROUPS = 2048;
 
@@ -29,6 +38,7 @@ struct KvWs {
   uint32_t *tile_cnt, *tile_off;   // [MAX_TILES]
   uint32_t *need_off;              // [list + 1] pages needed by the entries before
   int32_t *at;                     // [list] extend: pages held before; fork: the child's own page
+  int32_t *len;                    // [list] fork: the parent's tokens
   int32_t *code, *movers, *holes;  // [pages] compact
 };
 
@@ -50,6 +60,7 @@ size_t carve(void *base, int pages, int list, KvWs *w) {
   w->holes = (int32_t *)take((size_t)pages * 4);
   w->need_off = (uint32_t *)take(((size_t)list + 1) * 4);
   w->at = (int32_t *)take((size_t)list * 4);
+  w->len = (int32_t *)take((size_t)list * 4);
   return o;
 }
 
@@ -63,10 +74,12 @@ __device__ __forceinline__ int32_t *row_of(const hbf_kv &kv, int32_t *tables, in
   return tables + (int64_t)slot * kv.table_stride;
 }
 
-// Exclusive prefix sum over the workgroup; *total: the sum.
-__device__ uint32_t block_scan(uint32_t v, uint32_t *total, uint32_t *lds /* [THREADS / 64] */) {
+// Exclusive prefix sum over a workgroup of N threads; *total: the sum.
+template <int N>
+__device__ uint32_t block_scan(uint32_t v, uint32_t *total, uint32_t *lds /* [N / 64] */) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   uint32_t x = v;
+#pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const uint32_t y = __shfl_up(x, d);
     if (lane >= d) x += y;
@@ -74,9 +87,10 @@ __device__ uint32_t block_scan(uint32_t v, uint32_t *total, uint32_t *lds /* [TH
   if (lane == 63) lds[w] = x;
   __syncthreads();
   uint32_t before = 0, sum = 0;
-  for (int i = 0; i < THREADS / 64; i++) {
+#pragma unroll
+  for (int i = 0; i < N / 64; i++) {
     const uint32_t y = lds[i];
-    if (i < w) before += y;
+    before += i < w ? y : 0;
     sum += y;
   }
   __syncthreads();
@@ -105,7 +119,7 @@ __device__ bool plan_done(KvCtl *ctl, uint32_t err) {
 __device__ void plan_end(const KvWs &w, int tiles, uint32_t *scan_lds, uint32_t *count) {
   const uint32_t c = (int)threadIdx.x < tiles ? w.tile_cnt[threadIdx.x] : 0;
   uint32_t total;
-  const uint32_t before = block_scan(c, &total, scan_lds);
+  const uint32_t before = block_scan<THREADS>(c, &total, scan_lds);
   if ((int)threadIdx.x < tiles) w.tile_off[threadIdx.x] = before;
   *count = total;
 }
@@ -119,30 +133,233 @@ __device__ void plan_publish(KvCtl *ctl, uint32_t err, uint32_t total, uint32_t 
   if (err) atomicOr(&ctl->sticky, err);
 }
 
-// refs of this thread's pages of a tile; pages behind the last read as `past`.
-__device__ __forceinline__ void load_refs(const hbf_kv &kv, int tile, int32_t past, int32_t *r) {
-  const int p0 = tile * TILE + threadIdx.x * PER_THREAD;
+// refs of this thread's PT pages from p0 on; those behind the last page read as `past`.
+template <int PT>
+__device__ __forceinline__ void load_refs(const hbf_kv &kv, int p0, int32_t past, int32_t (&r)[PT]) {
 #pragma unroll
-  for (int i = 0; i < PER_THREAD; i++) r[i] = p0 + i < kv.pages ? kv.dev_refs[p0 + i] : past;
+  for (int i = 0; i < PT; i++) r[i] = p0 + i < kv.pages ? kv.dev_refs[p0 + i] : past;
 }
 
-__device__ void copy_bytes(char *dst, const char *src, int64_t bytes) {
-  constexpr int STEP = THREADS * 16, U = COPY_BYTES / STEP;
-  int64_t o = (int64_t)threadIdx.x * 16;
-  for (; o + (U - 1) * STEP < bytes; o += COPY_BYTES) {
+// By nt threads (a workgroup, or one wave of it).
+__device__ __forceinline__ void copy_bytes(char *dst, const char *src, int64_t bytes, int nt) {
+  constexpr int U = COPY_BYTES / (THREADS * 16);
+  const int step = nt * 16;
+  int64_t o = (int64_t)(threadIdx.x & (nt - 1)) * 16;
+  for (; o + (U - 1) * step < bytes; o += U * step) {
     u32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; u++) v[u] = *(const u32x4 *)(src + o + u * STEP);
+    for (int u = 0; u < U; u++) v[u] = *(const u32x4 *)(src + o + u * step);
 #pragma unroll
-    for (int u = 0; u < U; u++) *(u32x4 *)(dst + o + u * STEP) = v[u];
+    for (int u = 0; u < U; u++) *(u32x4 *)(dst + o + u * step) = v[u];
   }
-  for (; o < bytes; o += STEP) *(u32x4 *)(dst + o) = *(const u32x4 *)(src + o);
+  for (; o < bytes; o += step) *(u32x4 *)(dst + o) = *(const u32x4 *)(src + o);
 }
 
 // ------------------------------------------------------------ extend and fork
 
-// Workgroups 0 .. tiles-1 count their tile's free pages; the next one checks
-// the list and sums its needs; fork's others check one parent's row each.
+// What a list's check leaves of it: entry i changes row slot[i]; a fork's
+// parent is from[i], its length len[i]; extend's held[i] pages come before
+// those it gets; off[i] pages are needed by the entries before i.
+struct List {
+  int32_t *slot, *from, *len;
+  int32_t *held;
+  uint32_t *off;
+};
+
+// Checks the list (`seen`: a bit per slot, in LDS) and fills `out` (whose
+// pointers may be LDS; null ones are left out); the errors this thread met.
+template <bool FORK, int N>
+__device__ uint32_t check_list(const hbf_kv &kv, const List &out, const int32_t *first, const int32_t *second, int n,
+                               uint32_t *seen, uint32_t *lds) {
+  const int t = threadIdx.x;
+  uint32_t err = 0;
+  for (int i = t; i < (kv.slots + 31) / 32; i += N) seen[i] = 0;
+  __syncthreads();
+  uint64_t sum = 0;
+  for (int i0 = 0; i0 < n; i0 += N) {
+    const int i = i0 + t;
+    uint32_t need = 0;
+    if (i < n) {
+      const int a = first[i], b = second[i];
+      const int slot = FORK ? b : a;  // the one whose row changes
+      int len = 0, held = 0;
+      bool ok = slot >= 0 && slot < kv.slots;
+      if (ok) ok = !(atomicOr(&seen[slot >> 5], 1u << (slot & 31)) >> (slot & 31) & 1);
+      if (ok && FORK) {
+        ok = a >= 0 && a < kv.slots;
+        if (ok) {
+          len = kv.dev_lens[a];
+          ok = kv.dev_lens[slot] == 0 && len_fits(kv, len);
+          need = ok && len % kv.page_tokens != 0;
+        }
+      } else if (ok) {
+        len = kv.dev_lens[slot];
+        const int64_t grown = (int64_t)len + b;
+        ok = len_fits(kv, len) && b >= 0 && grown <= (int64_t)kv.table_cols * kv.page_tokens;
+        if (ok) {
+          held = pages_of(len, kv.page_tokens);
+          need = pages_of((int)grown, kv.page_tokens) - held;
+          if (b > 0 && len % kv.page_tokens != 0) {
+            const int p = row_of(kv, kv.dev_tables, slot)[held - 1];
+            ok = p >= 0 && p < kv.pages && kv.dev_refs[p] == 1;
+          }
+        }
+      }
+      if (!ok) {
+        err |= KV_ERR_ARG;
+        need = 0;
+        len = 0;
+      }
+      if (out.slot) out.slot[i] = slot;
+      if (out.from) out.from[i] = a;
+      if (out.len) out.len[i] = len;
+      if (out.held) out.held[i] = held;
+      // (a need past every page is refused below; clamped, the sums stay in range)
+      if (need > KV_MAX_PAGES) need = KV_MAX_PAGES + 1;
+    }
+    uint32_t total;
+    const uint32_t before = block_scan<N>(need, &total, lds);
+    if (i < n) out.off[i] = (uint32_t)sum + before;
+    sum += total;
+    if (sum > KV_MAX_PAGES) {
+      err |= KV_ERR_PAGES;
+      sum = KV_MAX_PAGES + 1;
+    }
+  }
+  if (t == 0) out.off[n] = (uint32_t)sum;
+  if (FORK)  // a parent's row must not change under those that read it
+    for (int i = t; i < n; i += N) {
+      const int from = first[i];
+      if (from >= 0 && from < kv.slots && (seen[from >> 5] >> (from & 31) & 1)) err |= KV_ERR_ARG;
+    }
+  return err;
+}
+
+// A fork's parent's row of `len` tokens, by threads t of nt.
+__device__ uint32_t check_row(const hbf_kv &kv, int from, int len, int t, int nt) {
+  uint32_t err = 0;
+  const int held = pages_of(len, kv.page_tokens);
+  if (held == 0) return 0;
+  const int32_t *row = row_of(kv, kv.dev_tables, from);
+#pragma unroll 4
+  for (int c = t; c < held; c += nt) {
+    const int p = row[c];
+    if (p < 0 || p >= kv.pages || kv.dev_refs[p] <= 0) err = KV_ERR_ARG;
+  }
+  return err;
+}
+
+// The free pages of a workgroup's N * PT from p0 on (refs r), the first of them
+// of rank `rank`, go to the entries that need them.  `pages`: LDS.  FORK:
+// taken[i] receives the child's page.
+template <bool FORK, int N, int PT>
+__device__ void give_pages(const hbf_kv &kv, const List &list, int n, int p0, const int32_t (&r)[PT], uint32_t rank,
+                           uint32_t need, uint16_t *pages, uint32_t *lds, int32_t *taken) {
+  uint32_t c = 0, total;
+#pragma unroll
+  for (int i = 0; i < PT; i++) c += r[i] == 0;
+  uint32_t at = block_scan<N>(c, &total, lds);
+#pragma unroll
+  for (int i = 0; i < PT; i++)
+    if (r[i] == 0) pages[at++] = (uint16_t)(threadIdx.x * PT + i);
+  __syncthreads();
+  for (uint32_t k = threadIdx.x; k < total && rank + k < need; k += N) {
+    const uint32_t mine = rank + k;
+    int lo = 0, hi = n;  // the last entry whose offset is at most the rank
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (list.off[mid] <= mine) lo = mid; else hi = mid;
+    }
+    const int page = p0 + pages[k];
+    const int col = FORK ? list.len[lo] / kv.page_tokens : list.held[lo] + (int)(mine - list.off[lo]);
+    row_of(kv, kv.dev_tables, list.slot[lo])[col] = page;
+    kv.dev_refs[page] = 1;
+    if (FORK) taken[lo] = page;
+  }
+}
+
+// A fork's child gets its parent's full pages; by threads t of nt.
+__device__ void share_row(const hbf_kv &kv, int from, int len, int to, int t, int nt) {
+  const int full = len / kv.page_tokens;
+  const int32_t *src = row_of(kv, kv.dev_tables, from);
+  int32_t *dst = row_of(kv, kv.dev_tables, to);
+#pragma unroll 4
+  for (int c = t; c < full; c += nt) {
+    const int p = src[c];
+    dst[c] = p;
+    atomicAdd(&kv.dev_refs[p], 1);  // (never zero here: no free page is taken for used or the other way)
+  }
+  if (t == 0) kv.dev_lens[to] = len;
+}
+
+// The tokens of a fork's part-full pages, in one plane.
+__device__ __forceinline__ void copy_part(const hbf_kv &kv, int plane, int src, int dst, int len, int nt) {
+  char *base = (char *)kv.dev_pool + (uint64_t)plane * kv.plane_stride;
+  copy_bytes(base + (uint64_t)dst * kv.page_stride, base + (uint64_t)src * kv.page_stride,
+             (int64_t)(len % kv.page_tokens) * kv.token_bytes, nt);
+}
+
+// PT pages per thread.  copy: the part-full pages too.
+template <bool FORK, int PT>
+__global__ __launch_bounds__(ONE) void k_kv_one(hbf_kv kv, KvWs w, const int32_t *first, const int32_t *second, int n,
+                                                bool copy) {
+  extern __shared__ uint32_t seen[];
+  __shared__ uint16_t pages[ONE * PT];
+  __shared__ int32_t slot[SMALL_LIST], from[SMALL_LIST], len[SMALL_LIST], held[SMALL_LIST];
+  __shared__ uint32_t off[SMALL_LIST + 1], lds[ONE / 64];
+  const List list = {slot, from, len, held, off};
+  const int t = threadIdx.x;
+  int32_t r[PT];
+  load_refs(kv, t * PT, 1, r);
+  uint32_t err = check_list<FORK, ONE>(kv, list, first, second, n, seen, lds);
+  __syncthreads();
+  if (FORK)
+    for (int i = t / ROW; i < n; i += ONE / ROW) err |= check_row(kv, from[i], len[i], t % ROW, ROW);
+  uint32_t c = 0, free_pages;
+#pragma unroll
+  for (int i = 0; i < PT; i++) c += r[i] == 0;
+  block_scan<ONE>(c, &free_pages, lds);
+  const uint32_t need = off[n];
+  const bool bad = __syncthreads_or(err & KV_ERR_ARG), full = __syncthreads_or(err & KV_ERR_PAGES) || need > free_pages;
+  if (t == 0) {
+    w.ctl->go = !bad && !full;
+    if (bad || full) w.ctl->sticky |= bad ? KV_ERR_ARG : KV_ERR_PAGES;
+  }
+  if (bad || full) return;
+  // (the pages that the children get: `held`, which fork has no other use for)
+  give_pages<FORK, ONE>(kv, list, n, 0, r, 0, need, pages, lds, held);
+  if (!FORK) {
+    for (int i = t; i < n; i += ONE) kv.dev_lens[slot[i]] = len[i] + second[i];
+    return;
+  }
+  for (int i = t / ROW; i < n; i += ONE / ROW) share_row(kv, from[i], len[i], slot[i], t % ROW, ROW);
+  __syncthreads();
+  if (copy) {
+    for (int i = t >> 6; i < n * kv.planes; i += ONE / 64) {  // a wave each
+      const int e = i / kv.planes;
+      if (off[e + 1] != off[e])
+        copy_part(kv, i - e * kv.planes, row_of(kv, kv.dev_tables, from[e])[len[e] / kv.page_tokens], held[e], len[e],
+                  64);
+    }
+  } else {
+    for (int i = t; i < n; i += ONE) {
+      w.len[i] = len[i];
+      w.at[i] = held[i];
+      w.need_off[i] = off[i];
+    }
+    if (t == 0) w.need_off[n] = need;
+  }
+}
+
+// The list as the launches of a large call hand it on.
+template <bool FORK>
+__device__ List list_of(const KvWs &w) {
+  return List{nullptr, nullptr, FORK ? w.len : nullptr, FORK ? nullptr : w.at, w.need_off};
+}
+
+// Large calls.  Workgroups 0 .. tiles-1 count their tile's free pages; the next
+// one checks the list and sums its needs; fork's others check one parent's row
+// each.
 template <bool FORK>
 __global__ __launch_bounds__(THREADS) void k_kv_plan(hbf_kv kv, KvWs w, const int32_t *first, const int32_t *second,
                                                      int n, int tiles) {
@@ -152,78 +369,19 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(hbf_kv kv, KvWs w, const in
   uint32_t err = 0;
   if (b < tiles) {
     int32_t r[PER_THREAD];
-    load_refs(kv, b, 1, r);
+    load_refs(kv, b * TILE + t * PER_THREAD, 1, r);
     uint32_t c = 0, total;
 #pragma unroll
     for (int i = 0; i < PER_THREAD; i++) c += r[i] == 0;
-    block_scan(c, &total, lds);
+    block_scan<THREADS>(c, &total, lds);
     if (t == 0) w.tile_cnt[b] = total;
   } else if (b == tiles) {
-    for (int i = t; i < (kv.slots + 31) / 32; i += THREADS) seen[i] = 0;
-    __syncthreads();
-    uint64_t sum = 0;
-    for (int i0 = 0; i0 < n; i0 += THREADS) {
-      const int i = i0 + t;
-      uint32_t need = 0;
-      if (i < n) {
-        const int slot = FORK ? second[i] : first[i];  // the one whose row changes
-        bool ok = slot >= 0 && slot < kv.slots;
-        if (ok) ok = !(atomicOr(&seen[slot >> 5], 1u << (slot & 31)) >> (slot & 31) & 1);
-        if (ok && FORK) {
-          const int from = first[i];
-          ok = from >= 0 && from < kv.slots && kv.dev_lens[slot] == 0;
-          if (ok) {
-            const int len = kv.dev_lens[from];
-            ok = len_fits(kv, len);
-            need = ok && len % kv.page_tokens != 0;
-          }
-        } else if (ok) {
-          const int len = kv.dev_lens[slot], add = second[i];
-          const int64_t grown = (int64_t)len + add;
-          ok = len_fits(kv, len) && add >= 0 && grown <= (int64_t)kv.table_cols * kv.page_tokens;
-          if (ok) {
-            const int held = pages_of(len, kv.page_tokens);
-            w.at[i] = held;
-            need = pages_of((int)grown, kv.page_tokens) - held;
-            if (add > 0 && len % kv.page_tokens != 0) {
-              const int p = row_of(kv, kv.dev_tables, slot)[held - 1];
-              ok = p >= 0 && p < kv.pages && kv.dev_refs[p] == 1;
-            }
-          }
-        }
-        if (!ok) {
-          err |= KV_ERR_ARG;
-          need = 0;
-        }
-        // (a need past every page is refused below; clamped, the sums stay in range)
-        if (need > KV_MAX_PAGES) need = KV_MAX_PAGES + 1;
-      }
-      uint32_t total;
-      const uint32_t before = block_scan(need, &total, lds);
-      if (i < n) w.need_off[i] = (uint32_t)sum + before;
-      sum += total;
-      if (sum > KV_MAX_PAGES) {
-        err |= KV_ERR_PAGES;
-        sum = KV_MAX_PAGES + 1;
-      }
-    }
-    if (t == 0) w.need_off[n] = (uint32_t)sum;
-    if (FORK)  // a parent's row must not change under those that read it
-      for (int i = t; i < n; i += THREADS) {
-        const int from = first[i];
-        if (from >= 0 && from < kv.slots && (seen[from >> 5] >> (from & 31) & 1)) err |= KV_ERR_ARG;
-      }
+    err = check_list<FORK, THREADS>(kv, list_of<FORK>(w), first, second, n, seen, lds);
   } else {
     const int from = first[b - tiles - 1];
-    if (from >= 0 && from < kv.slots) {
+    if (from >= 0 && from < kv.slots) {  // (the list's check has the others)
       const int len = kv.dev_lens[from];
-      if (len_fits(kv, len)) {
-        const int32_t *row = row_of(kv, kv.dev_tables, from);
-        for (int c = t; c < pages_of(len, kv.page_tokens); c += THREADS) {
-          const int p = row[c];
-          if (p < 0 || p >= kv.pages || kv.dev_refs[p] <= 0) err = KV_ERR_ARG;
-        }
-      }
+      if (len_fits(kv, len)) err = check_row(kv, from, len, t, THREADS);
     }
   }
   if (!plan_done(w.ctl, err)) return;
@@ -240,49 +398,20 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(hbf_kv kv, KvWs w, const in
 template <bool FORK>
 __global__ __launch_bounds__(THREADS) void k_kv_apply(hbf_kv kv, KvWs w, const int32_t *first, const int32_t *second,
                                                       int n, int tiles) {
+  __shared__ uint16_t pages[TILE];
   __shared__ uint32_t lds[THREADS / 64];
   if (!w.ctl->go) return;
   const int b = blockIdx.x, t = threadIdx.x;
   if (b < tiles) {
-    const uint32_t need = w.ctl->total;
-    uint32_t rank = w.tile_off[b];
+    const uint32_t need = w.ctl->total, rank = w.tile_off[b];
     if (rank >= need) return;
     int32_t r[PER_THREAD];
-    load_refs(kv, b, 1, r);
-    uint32_t c = 0, total;
-#pragma unroll
-    for (int i = 0; i < PER_THREAD; i++) c += r[i] == 0;
-    rank += block_scan(c, &total, lds);
-#pragma unroll
-    for (int i = 0; i < PER_THREAD; i++) {
-      if (r[i] != 0) continue;
-      if (rank < need) {
-        int lo = 0, hi = n;  // the last entry whose offset is at most rank
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (w.need_off[mid] <= rank) lo = mid; else hi = mid;
-        }
-        const int page = b * TILE + t * PER_THREAD + i;
-        const int slot = FORK ? second[lo] : first[lo];
-        const int col = FORK ? kv.dev_lens[first[lo]] / kv.page_tokens : w.at[lo] + (int)(rank - w.need_off[lo]);
-        row_of(kv, kv.dev_tables, slot)[col] = page;
-        kv.dev_refs[page] = 1;
-        if (FORK) w.at[lo] = page;
-      }
-      rank++;
-    }
+    load_refs(kv, b * TILE + t * PER_THREAD, 1, r);
+    List list = list_of<FORK>(w);
+    list.slot = (int32_t *)(FORK ? second : first);
+    give_pages<FORK, THREADS>(kv, list, n, b * TILE, r, rank, need, pages, lds, w.at);
   } else if (FORK) {
-    const int i = b - tiles;
-    const int from = first[i], to = second[i];
-    const int len = kv.dev_lens[from];
-    const int32_t *src = row_of(kv, kv.dev_tables, from);
-    int32_t *dst = row_of(kv, kv.dev_tables, to);
-    for (int c = t; c < len / kv.page_tokens; c += THREADS) {
-      const int p = src[c];
-      dst[c] = p;
-      atomicAdd(&kv.dev_refs[p], 1);  // (never zero here: no free page is taken for used or the other way)
-    }
-    if (t == 0) kv.dev_lens[to] = len;
+    share_row(kv, first[b - tiles], w.len[b - tiles], second[b - tiles], t, THREADS);
   } else {
     const int i = (b - tiles) * THREADS + t;
     if (i < n) kv.dev_lens[first[i]] += second[i];
@@ -294,11 +423,8 @@ __global__ __launch_bounds__(THREADS) void k_kv_fork_copy(hbf_kv kv, KvWs w, con
   if (!w.ctl->go) return;
   const int i = blockIdx.y;
   if (w.need_off[i + 1] == w.need_off[i]) return;
-  const int len = kv.dev_lens[parents[i]];
-  const int src = row_of(kv, kv.dev_tables, parents[i])[len / kv.page_tokens], dst = w.at[i];
-  char *plane = (char *)kv.dev_pool + blockIdx.x * kv.plane_stride;
-  copy_bytes(plane + dst * kv.page_stride, plane + src * kv.page_stride,
-             (int64_t)(len % kv.page_tokens) * kv.token_bytes);
+  const int len = w.len[i];
+  copy_part(kv, blockIdx.x, row_of(kv, kv.dev_tables, parents[i])[len / kv.page_tokens], w.at[i], len, THREADS);
 }
 
 // ------------------------------------------------------------ free
@@ -375,7 +501,7 @@ __device__ void move_pages(const hbf_kv &kv, const int32_t *src, const int32_t *
     const uint32_t plane = rest / parts, part = rest - plane * parts;
     char *base = (char *)kv.dev_pool + plane * kv.plane_stride + (uint64_t)part * COPY_BYTES;
     const int64_t left = bytes - (int64_t)part * COPY_BYTES;
-    copy_bytes(base + dst[i] * kv.page_stride, base + src[i] * kv.page_stride, left < COPY_BYTES ? left : COPY_BYTES);
+    copy_bytes(base + dst[i] * kv.page_stride, base + src[i] * kv.page_stride, left < COPY_BYTES ? left : COPY_BYTES, THREADS);
   }
 }
 
@@ -385,71 +511,36 @@ __global__ __launch_bounds__(THREADS) void k_kv_copy(hbf_kv kv, KvCtl *ctl, cons
 
 // ------------------------------------------------------------ compact
 
-// Workgroups 0 .. tiles-1 count their tile's pages in use; the others check
-// the rows, a wave each.
-__global__ __launch_bounds__(THREADS) void k_kv_pack_plan(hbf_kv kv, KvWs w, int tiles) {
-  __shared__ uint32_t lds[THREADS / 64];
-  const int b = blockIdx.x, t = threadIdx.x;
+// The rows' entries, N threads a row, by group `group` of `groups`.
+template <int N>
+__device__ uint32_t check_rows(const hbf_kv &kv, int group, int groups) {
   uint32_t err = 0;
-  int32_t r[PER_THREAD];
-  if (b < tiles) {
-    load_refs(kv, b, 0, r);
-    uint32_t c = 0, total;
-#pragma unroll
-    for (int i = 0; i < PER_THREAD; i++) {
-      c += r[i] > 0;
-      if (r[i] < 0) err = KV_ERR_ARG;
+  for (int slot = group; slot < kv.slots; slot += groups) {
+    const int len = kv.dev_lens[slot];
+    if (!len_fits(kv, len)) {
+      err = KV_ERR_ARG;
+      continue;
     }
-    block_scan(c, &total, lds);
-    if (t == 0) w.tile_cnt[b] = total;
-  } else {
-    const int slot = (b - tiles) * (THREADS / 64) + (t >> 6);
-    if (slot < kv.slots) {
-      const int len = kv.dev_lens[slot];
-      if (!len_fits(kv, len)) {
-        err = KV_ERR_ARG;
-      } else {
-        const int32_t *row = row_of(kv, kv.dev_tables, slot);
-        for (int c = t & 63; c < pages_of(len, kv.page_tokens); c += 64) {
-          const int p = row[c];
-          if (p < 0 || p >= kv.pages || kv.dev_refs[p] <= 0) err = KV_ERR_ARG;
-        }
-      }
+    const int32_t *row = row_of(kv, kv.dev_tables, slot);
+    const int held = pages_of(len, kv.page_tokens);
+#pragma unroll 4
+    for (int c = threadIdx.x % N; c < held; c += N) {
+      const int p = row[c];
+      if (p < 0 || p >= kv.pages || kv.dev_refs[p] <= 0) err = KV_ERR_ARG;
     }
   }
-  if (!plan_done(w.ctl, err)) return;
-  uint32_t live;
-  plan_end(w, tiles, lds, &live);
-  err = atomicOr(&w.ctl->err, 0);
-  __syncthreads();  // (and tile_off is written)
-  // pages in use below `live` stay; the rest move
-  uint32_t stay = live;
-  const int tl = (int)live / TILE;
-  if (tl < tiles) {
-    load_refs(kv, tl, 0, r);
-    uint32_t c = 0, total;
-#pragma unroll
-    for (int i = 0; i < PER_THREAD; i++) c += r[i] > 0 && tl * TILE + t * PER_THREAD + i < (int)live;
-    block_scan(c, &total, lds);
-    stay = w.tile_off[tl] + total;
-  }
-  plan_publish(w.ctl, err, live - stay, live);
+  return err;
 }
 
-// Number the pages: those that stay, those that move and the places they move to.
-__global__ __launch_bounds__(THREADS) void k_kv_pack_number(hbf_kv kv, KvWs w, int32_t *remap, int32_t *refs_out) {
-  __shared__ uint32_t lds[THREADS / 64];
-  if (!w.ctl->go) return;
-  const int live = (int)w.ctl->live, stay = live - (int)w.ctl->total;
-  int32_t r[PER_THREAD];
-  load_refs(kv, blockIdx.x, 0, r);
-  uint32_t c = 0, total;
+// Number this thread's pages from p0 on (refs r, `before` of them in use before
+// these): those that stay, those that move and the places they move to.  The
+// first `live` pages will be in use; `stay` of the pages in use lie there.
+template <int PT>
+__device__ void number_pages(const hbf_kv &kv, const KvWs &w, int p0, const int32_t (&r)[PT], int before, int live,
+                             int stay, int32_t *remap, int32_t *refs_out) {
 #pragma unroll
-  for (int i = 0; i < PER_THREAD; i++) c += r[i] > 0;
-  int before = (int)(w.tile_off[blockIdx.x] + block_scan(c, &total, lds));
-#pragma unroll
-  for (int i = 0; i < PER_THREAD; i++) {
-    const int p = blockIdx.x * TILE + threadIdx.x * PER_THREAD + i;
+  for (int i = 0; i < PT; i++) {
+    const int p = p0 + i;
     if (p >= kv.pages) break;
     if (r[i] > 0) {
       if (p < live) {
@@ -466,6 +557,84 @@ __global__ __launch_bounds__(THREADS) void k_kv_pack_number(hbf_kv kv, KvWs w, i
     }
     if (refs_out != kv.dev_refs) refs_out[p] = r[i];
   }
+}
+
+template <int PT>
+__global__ __launch_bounds__(ONE) void k_kv_pack_one(hbf_kv kv, KvWs w, int32_t *remap, int32_t *refs_out) {
+  __shared__ uint32_t lds[ONE / 64];
+  const int t = threadIdx.x;
+  int32_t r[PT];
+  load_refs(kv, t * PT, 0, r);
+  uint32_t err = check_rows<ROW>(kv, t / ROW, ONE / ROW), c = 0, live, stay;
+#pragma unroll
+  for (int i = 0; i < PT; i++) {
+    c += r[i] > 0;
+    if (r[i] < 0) err = KV_ERR_ARG;
+  }
+  const int before = (int)block_scan<ONE>(c, &live, lds);
+  c = 0;
+#pragma unroll
+  for (int i = 0; i < PT; i++) c += r[i] > 0 && t * PT + i < (int)live;
+  block_scan<ONE>(c, &stay, lds);
+  const bool bad = __syncthreads_or(err);
+  if (t == 0) {
+    w.ctl->go = !bad;
+    w.ctl->total = live - stay;
+    if (bad) w.ctl->sticky |= KV_ERR_ARG;
+  }
+  if (!bad) number_pages(kv, w, t * PT, r, before, (int)live, (int)stay, remap, refs_out);
+}
+
+// Workgroups 0 .. tiles-1 count their tile's pages in use; the others check
+// the rows, a wave each.
+__global__ __launch_bounds__(THREADS) void k_kv_pack_plan(hbf_kv kv, KvWs w, int tiles) {
+  __shared__ uint32_t lds[THREADS / 64];
+  const int b = blockIdx.x, t = threadIdx.x;
+  uint32_t err = 0;
+  int32_t r[PER_THREAD];
+  if (b < tiles) {
+    load_refs(kv, b * TILE + t * PER_THREAD, 0, r);
+    uint32_t c = 0, total;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; i++) {
+      c += r[i] > 0;
+      if (r[i] < 0) err = KV_ERR_ARG;
+    }
+    block_scan<THREADS>(c, &total, lds);
+    if (t == 0) w.tile_cnt[b] = total;
+  } else {
+    err = check_rows<64>(kv, (b - tiles) * (THREADS / 64) + (t >> 6), (gridDim.x - tiles) * (THREADS / 64));
+  }
+  if (!plan_done(w.ctl, err)) return;
+  uint32_t live;
+  plan_end(w, tiles, lds, &live);
+  err = atomicOr(&w.ctl->err, 0);
+  __syncthreads();  // (and tile_off is written)
+  // pages in use below `live` stay; the rest move
+  uint32_t stay = live;
+  const int tl = (int)live / TILE;
+  if (tl < tiles) {
+    load_refs(kv, tl * TILE + t * PER_THREAD, 0, r);
+    uint32_t c = 0, total;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; i++) c += r[i] > 0 && tl * TILE + t * PER_THREAD + i < (int)live;
+    block_scan<THREADS>(c, &total, lds);
+    stay = w.tile_off[tl] + total;
+  }
+  plan_publish(w.ctl, err, live - stay, live);
+}
+
+__global__ __launch_bounds__(THREADS) void k_kv_pack_number(hbf_kv kv, KvWs w, int32_t *remap, int32_t *refs_out) {
+  __shared__ uint32_t lds[THREADS / 64];
+  if (!w.ctl->go) return;
+  const int live = (int)w.ctl->live, p0 = blockIdx.x * TILE + threadIdx.x * PER_THREAD;
+  int32_t r[PER_THREAD];
+  load_refs(kv, p0, 0, r);
+  uint32_t c = 0, total;
+#pragma unroll
+  for (int i = 0; i < PER_THREAD; i++) c += r[i] > 0;
+  const int before = (int)(w.tile_off[blockIdx.x] + block_scan<THREADS>(c, &total, lds));
+  number_pages(kv, w, p0, r, before, live, live - (int)w.ctl->total, remap, refs_out);
 }
 
 __global__ __launch_bounds__(THREADS) void k_kv_pack_move(hbf_kv kv, KvWs w, int32_t *remap, int32_t *tables_out,
@@ -527,9 +696,19 @@ int tiles_of(int pages) { return (pages + TILE - 1) / TILE; }
 
 template <bool FORK>
 hipError_t plan_apply(const hbf_kv &kv, const KvWs &w, const int32_t *first, const int32_t *second, int n,
-                      hipStream_t s) {
+                      bool *copy /* done */, hipStream_t s) {
   const int tiles = tiles_of(kv.pages);
   const size_t lds = (size_t)((kv.slots + 31) / 32) * 4;
+  if (kv.pages <= SMALL_PAGES && kv.slots <= SMALL_ENTRIES && n <= SMALL_LIST &&
+      (!FORK || (int64_t)n * kv.table_cols <= SMALL_ENTRIES)) {
+    *copy = FORK && (uint64_t)n * kv.planes * kv.page_tokens * kv.token_bytes <= SMALL_COPY;
+    if (kv.pages <= ONE * 4)
+      k_kv_one<FORK, 4><<<1, ONE, lds, s>>>(kv, w, first, second, n, *copy);
+    else
+      k_kv_one<FORK, PER_THREAD><<<1, ONE, lds, s>>>(kv, w, first, second, n, *copy);
+    return hipGetLastError();
+  }
+  *copy = false;
   k_kv_plan<FORK><<<tiles + 1 + (FORK ? n : 0), THREADS, lds, s>>>(kv, w, first, second, n, tiles);
   k_kv_apply<FORK><<<tiles + (FORK ? n : (n + THREADS - 1) / THREADS), THREADS, 0, s>>>(kv, w, first, second, n,
                                                                                         tiles);
@@ -547,15 +726,17 @@ hipError_t launch_kv_extend(const hbf_kv &kv, const int32_t *slots, const int32_
                             hipStream_t s) {
   KvWs w;
   carve(kv.dev_ws, kv.pages, ws_list, &w);
-  return plan_apply<false>(kv, w, slots, add, n, s);
+  bool copied;
+  return plan_apply<false>(kv, w, slots, add, n, &copied, s);
 }
 
 hipError_t launch_kv_fork(const hbf_kv &kv, const int32_t *parents, const int32_t *children, int n, int ws_list,
                           hipStream_t s) {
   KvWs w;
   carve(kv.dev_ws, kv.pages, ws_list, &w);
-  const hipError_t e = plan_apply<true>(kv, w, parents, children, n, s);
-  if (e != hipSuccess) return e;
+  bool copied;
+  const hipError_t e = plan_apply<true>(kv, w, parents, children, n, &copied, s);
+  if (e != hipSuccess || copied) return e;
   k_kv_fork_copy<<<dim3(kv.planes, n), THREADS, 0, s>>>(kv, w, parents);
   return hipGetLastError();
 }
@@ -585,8 +766,16 @@ hipError_t launch_kv_compact(const hbf_kv &kv, int32_t *remap, int32_t *tables_o
   KvWs w;
   carve(kv.dev_ws, kv.pages, 0, &w);
   const int tiles = tiles_of(kv.pages);
-  k_kv_pack_plan<<<tiles + (kv.slots + THREADS / 64 - 1) / (THREADS / 64), THREADS, 0, s>>>(kv, w, tiles);
-  k_kv_pack_number<<<tiles, THREADS, 0, s>>>(kv, w, remap, refs_out);
+  if (kv.pages <= SMALL_PAGES && (int64_t)kv.slots * kv.table_cols <= SMALL_ENTRIES) {
+    if (kv.pages <= ONE * 4)
+      k_kv_pack_one<4><<<1, ONE, 0, s>>>(kv, w, remap, refs_out);
+    else
+      k_kv_pack_one<PER_THREAD><<<1, ONE, 0, s>>>(kv, w, remap, refs_out);
+  } else {
+    const int rows = (kv.slots + THREADS / 64 - 1) / (THREADS / 64);
+    k_kv_pack_plan<<<tiles + rows, THREADS, 0, s>>>(kv, w, tiles);
+    k_kv_pack_number<<<tiles, THREADS, 0, s>>>(kv, w, remap, refs_out);
+  }
   k_kv_pack_move<<<MOVE_GROUPS, THREADS, 0, s>>>(kv, w, remap, tables_out, refs_out);
   return hipGetLastError();
 }

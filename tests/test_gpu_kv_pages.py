@@ -144,7 +144,7 @@ class Both:
 
 @pytest.mark.parametrize("layers,pages,pt,heads,dim,slots,cols", [
     (1, 40, 16, 1, 8, 6, 12), (3, 700, 8, 2, 64, 40, 30), (2, 9000, 1, 1, 8, 30, 700), (1, 4097, 24, 1, 16, 64, 50),
-    (5, 300, 5, 4, 24, 20, 21)])
+    (5, 300, 5, 4, 24, 20, 21), (1, 20000, 2, 1, 8, 40, 900), (2, 16390, 3, 1, 8, 90, 1200)])
 def test_random_life_of_a_cache(torch, layers, pages, pt, heads, dim, slots, cols):
     say(f"kv life {layers} {pages} {pt} {heads} {dim} {slots} {cols}")
     rng = np.random.default_rng(pages)
@@ -222,13 +222,14 @@ def test_large_pool_many_tiles(torch):
     b.same()
 
 
-def test_compact_to_other_arrays(torch):
-    b = Both(torch, 2, 50, 4, 1, 8, 6, 8, extra_cols=2)
+@pytest.mark.parametrize("pages", [50, 17000])
+def test_compact_to_other_arrays(torch, pages):
+    b = Both(torch, 2, pages, 4, 1, 8, 6, 8, extra_cols=2)
     b.call("extend", [0, 1, 2], [30, 17, 25])
     b.call("fork", [1], [4])
     b.call("free", [0])
     before = {k: v.cpu().clone() for k, v in b.t.items()}
-    remap, refs = (torch.full((50,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
+    remap, refs = (torch.full((pages,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
     tables = torch.full((6, 10), -9, dtype=torch.int32, device="cuda")[:, :8]
     for _ in range(2):   # the same again: pages that moved keep their bytes
         assert b.kv.compact(remap, tables_out=tables, refs_out=refs) == OK
@@ -276,11 +277,18 @@ BAD = [
 ]
 
 
+@pytest.mark.parametrize("pages", [12, 17000])
 @pytest.mark.parametrize("name,first,second,want", BAD)
-def test_refused_calls_change_nothing(torch, name, first, second, want):
-    b = Both(torch, 1, 12, 4, 1, 8, 6, 8)
+def test_refused_calls_change_nothing(torch, name, first, second, want, pages):
+    b = Both(torch, 1, pages, 4, 1, 8, 6, 8)
     b.call("extend", [0, 1], [7, 6])
     b.hold(b.plain.tables[1, 1])     # slot 1's part-full page is held twice
+    if pages > 12:
+        if name == "copy" and max(first + second) == 12:
+            second = [pages]
+        for page in range(12, pages):    # as full as the small pool
+            b.plain.refs[page] += 1
+        b.t["refs"][12:] += 1
     assert getattr(b.kv, name)(b.dev(first), b.dev(second)) == OK
     assert b.kv.get_status() == want
     assert b.kv.get_status() == OK   # cleared
