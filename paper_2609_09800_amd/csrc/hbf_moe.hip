@@ -8,7 +8,7 @@
 // are gathered by expert, a tile of 16 of them being the narrow side of the
 // matrix instruction, and the weights are its wide side, loaded straight from
 // memory into the operand (16 rows of 64 bytes at a time; a row's next 64 follow
-// at once).  Four launches, each a pass over one kind of weights:
+// at once).  Four launches or three, each a pass over one kind of weights:
 //  - route: logits by tiles of 16 experts and 16 tokens; a token tile's last
 //    workgroup chooses, and the last of these sorts the (token, choice) pairs
 //    by expert, in tiles of up to 16 (an expert with more is read once per
@@ -18,7 +18,8 @@
 //  - down: 32 rows of y per tile and unit, each pair's product to a place of its
 //    own;
 //  - sum: a token's products in the order of its choices, so that the result
-//    does not depend on who computed them.
+//    does not depend on who computed them (in down's launch where that has a
+//    workgroup per unit).
 // Up and down are one scheme: a workgroup goes through consecutive units (a
 // token tile's rows, then the next tile's) with the tile's tokens kept in
 // registers, so that only weights are loaded, the next unit's while this one
@@ -72,6 +73,8 @@ struct Args {
   int e_pad;
   char *h_hi, *h_lo;                    // [pairs][F], in the order of `pair`
   float *part;                          // [pairs][H] products, by token and choice
+  uint32_t *block_done;                 // [H / 16] token tiles whose products of these rows are there
+  bool sum_in_down;                     // few units: the last workgroup of a block of rows sums it
 };
 
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
@@ -90,6 +93,7 @@ size_t carve(const hbf_moe &m, int tokens, char *base, Args *a) {
   a->h_hi = take((size_t)tokens * m.topk * m.ffn * 2);
   a->h_lo = take((size_t)tokens * m.topk * m.ffn * 2);
   a->part = (float *)take((size_t)tokens * m.topk * m.hidden * 4);
+  a->block_done = (uint32_t *)take((size_t)m.hidden / 16 * 4 + 4);
   return o;
 }
 
@@ -237,6 +241,8 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
   }
   // pairs by expert
   for (int i = threadIdx.x; i < MOE_MAX_EXPERTS; i += ROUTE_THREADS) cnt[i] = 0;
+  if (a.sum_in_down)
+    for (int i = threadIdx.x; i <= H / 16; i += ROUTE_THREADS) a.block_done[i] = 0;
   __syncthreads();
   for (int p = threadIdx.x; p < pairs; p += ROUTE_THREADS)
     if (ids[p] >= 0) atomicAdd(&cnt[ids[p]], 1);
@@ -355,6 +361,31 @@ __global__ __launch_bounds__(THREADS) void k_moe_up(Args a) {
 
 // ------------------------------------------------------------ down
 
+__device__ __forceinline__ bool used(const Args &a, int pair) {
+  return a.m.dev_router || (uint32_t)a.ids[pair] < (uint32_t)a.m.experts;
+}
+
+// y of rows r0 .. r0 + rows - 1 of every token, from products that others of this
+// launch handed over.
+__device__ void sum_handed(const Args &a, int r0, int rows, void (*store)(char *, float)) {
+  const int k = a.m.topk, H = a.m.hidden;
+  for (int i = threadIdx.x; i < a.tokens * rows; i += THREADS) {
+    const int t = i / rows, r = r0 + i - t * rows;
+    if (r >= H) continue;
+    float y = 0.f;
+#pragma unroll 8
+    for (int j = 0; j < k; j++) {
+      const int p = t * k + j;
+      if (used(a, p)) y += a.weights[p] * handed(a.part + (int64_t)p * H + r);
+    }
+    store(a.y + 2 * (t * a.ys + r), y);
+  }
+}
+template <typename T>
+__device__ void store_elem(char *to, float v) {
+  *(typename T::elem *)to = (typename T::elem)v;
+}
+
 // KS steps of 32 per wave and pass, RB tiles of 16 rows per unit; EXACT: F is one
 // pass and H whole units.
 template <typename T, int KS, int RB, bool EXACT>
@@ -362,7 +393,12 @@ __global__ __launch_bounds__(THREADS) void k_moe_down(Args a) {
   __shared__ f32x4 red[2][WAVES][RB][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   const int H = a.m.hidden, F = a.m.ffn, blocks = (H + 16 * RB - 1) / (16 * RB);
-  const int64_t units = (int64_t)a.lists->n_tiles * blocks;
+  const int n_tiles = a.lists->n_tiles;
+  const int64_t units = (int64_t)n_tiles * blocks;
+  if (a.sum_in_down && n_tiles == 0) {  // no choice at all: y is 0
+    if ((int)blockIdx.x < blocks) sum_handed(a, blockIdx.x * 16 * RB, 16 * RB, store_elem<T>);
+    return;
+  }
   const int u0 = (int)(units * blockIdx.x / gridDim.x), u1 = (int)(units * (blockIdx.x + 1) / gridDim.x);
   if (u0 >= u1) return;
   const int passes = EXACT ? 1 : (F + WAVES * KS * 32 - 1) / (WAVES * KS * 32);
@@ -432,8 +468,15 @@ __global__ __launch_bounds__(THREADS) void k_moe_down(Args a) {
         float o = 0.f;
 #pragma unroll
         for (int i = 0; i < WAVES; i++) o += red[buf][i][b][(r >> 2) * 16 + n][r & 3];
-        if (EXACT || row0 + b * 16 + r < H) a.part[to + b * 16] = o;
+        if (EXACT || row0 + b * 16 + r < H) {
+          if (a.sum_in_down) hand_over(a.part + to + b * 16, o);
+          else a.part[to + b * 16] = o;
+        }
       }
+    }
+    if (a.sum_in_down) {
+      stores_done();
+      if (last_of(a.block_done + row0 / (16 * RB), n_tiles)) sum_handed(a, row0, 16 * RB, store_elem<T>);
     }
     buf ^= 1;
   }
@@ -451,8 +494,7 @@ __global__ __launch_bounds__(SUM_THREADS) void k_moe_sum(Args a) {
 #pragma unroll 8
   for (int j = 0; j < k; j++) {
     const int p = t * k + j;
-    if (a.m.dev_router || (uint32_t)a.ids[p] < (uint32_t)a.m.experts)
-      y += a.weights[p] * *(const f32x4 *)(a.part + (int64_t)p * a.m.hidden + r);
+    if (used(a, p)) y += a.weights[p] * *(const f32x4 *)(a.part + (int64_t)p * a.m.hidden + r);
   }
   *(u32x2 *)(a.y + 2 * (t * a.ys + r)) = u32x2{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
 }
@@ -475,11 +517,15 @@ void down(const Args &a, int tiles, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t run(const Args &a, hipStream_t s) {
+hipError_t run(Args a, hipStream_t s) {
   const int pairs = a.tokens * a.m.topk;
+  const int tiles = std::min(pairs, a.m.experts + pairs / 16);  // at most
+  // A workgroup per unit: summed there, the layer is a launch shorter (one token of the 128-expert layer: 31.8 us, 33.0
+  // with it; 5 tokens of 20 small experts: 14.9, 16.9).  Where workgroups have several units, waiting for each one's
+  // stores would cost more.
+  a.sum_in_down = (int64_t)tiles * ((a.m.hidden + 31) / 32) <= GROUPS;
   const int route = a.m.dev_router ? a.e_pad / 16 * ((a.tokens + 15) / 16) : 1;
   k_moe_route<T><<<route, ROUTE_THREADS, 0, s>>>(a);
-  const int tiles = std::min(pairs, a.m.experts + pairs / 16);  // at most
   const int groups = (int)std::min<int64_t>((int64_t)tiles * (a.m.ffn / 8), GROUPS);
   // steps per wave
   const int up_steps = ((a.m.hidden + 31) / 32 + WAVES - 1) / WAVES;
@@ -492,7 +538,8 @@ hipError_t run(const Args &a, hipStream_t s) {
   else if (down_steps <= 4) down<T, 4, 2>(a, tiles, s);
   else if (down_steps <= 6) down<T, 6, 2>(a, tiles, s);
   else down<T, 8, 2>(a, tiles, s);
-  k_moe_sum<T><<<(a.tokens * (a.m.hidden / 4) + SUM_THREADS - 1) / SUM_THREADS, SUM_THREADS, 0, s>>>(a);
+  if (!a.sum_in_down)
+    k_moe_sum<T><<<(a.tokens * (a.m.hidden / 4) + SUM_THREADS - 1) / SUM_THREADS, SUM_THREADS, 0, s>>>(a);
   return hipGetLastError();
 }
 
