@@ -477,20 +477,29 @@ def cache_sweep(frames, prefetch, range_pages, pages, counts, stream=None):
 
 _I32 = ("int32",)
 _HALF = ("bfloat16", "float16")
+torch = None   # the module, once a KvPages or MoeLayer is made: their calls last about 10 us, an import statement 0.2
+
+
+def _import_torch():
+    global torch
+    import torch
+    return load_library()
 
 
 def _raw(stream):
     """hipStream_t of a torch stream (None -> current stream), as a number.
-    (torch.cuda.current_stream() builds an object: 2.8 us of a call that lasts 10.)"""
-    import torch
+    (torch.cuda.current_stream() builds an object, which takes 2.8 us.)"""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
 
 
+def _is(t, dtype):
+    """A contiguous tensor of that type on the GPU: what most calls pass."""
+    return isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()
+
+
 def _ints(t, what, numel=None):
-    """_dev for an int32 tensor, its checks in the order that passes soonest."""
-    import torch
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.int32 and t.is_contiguous()
-            and (numel is None or t.numel() == numel)):
+    """_dev for an int32 tensor; its number of elements."""
+    if not _is(t, torch.int32) or numel is not None and t.numel() != numel:
         _dev(t, what, _I32, numel=numel)
     return t.numel()
 
@@ -498,7 +507,6 @@ def _ints(t, what, numel=None):
 def _strided(t, what, dtypes, dim, inner=1):
     """As _dev, for a tensor of `dim` dimensions whose last `inner` are
     contiguous and whose others may be strided (by 16-byte multiples)."""
-    import torch
     bad = None
     if not isinstance(t, torch.Tensor):
         bad = f"not a tensor ({type(t).__name__})"
@@ -536,7 +544,6 @@ class _Scratch:
         self._stream = None   # the one that the block was made on
 
     def get(self, nbytes, device, stream):
-        import torch
         if self._t is None or self._t.numel() < nbytes:
             # (the allocator takes the old block back once the streams it was used on are through with it)
             self._t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
@@ -553,7 +560,6 @@ def _stride(t, d):
 
 def _zeroed(nbytes, device):
     """Device bytes, the first 256 zero and seen so by every stream."""
-    import torch
     t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
     t[:256].zero_()
     torch.cuda.current_stream(device).synchronize()
@@ -577,8 +583,7 @@ class KvPages:
     on one stream."""
 
     def __init__(self, pool, refs=None, tables=None, lens=None, max_list=1024):
-        import torch
-        self._lib = load_library()
+        self._lib = _import_torch()
         _dev(pool, "pool", _HALF)
         if pool.dim() != 6 or pool.shape[1] != 2 or 0 in pool.shape:
             raise HbfError(HBF_EINVAL, f"pool: shape {tuple(pool.shape)}, expected "
@@ -661,12 +666,11 @@ class KvPages:
         """Token pos[i] of slot slots[i] (int32 [n]) gets k[:, i] and v[:, i]:
         [layers, n, kv_heads, head_dim] of the pool's type, for the layers from
         first_layer on (or [n, kv_heads, head_dim] for that layer alone)."""
-        import torch
         d = self._desc()
         n = _ints(slots, "slots")
         _ints(pos, "pos", n)
         for t, what in ((k, "k"), (v, "v")):
-            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is self.pool.dtype and t.is_contiguous()):
+            if not _is(t, self.pool.dtype):
                 _dev(t, what, (str(self.pool.dtype).replace("torch.", ""),))
         shape = (n, self.kv_heads, self.head_dim)
         layers = k.shape[0] if k.dim() == 4 else 1
@@ -698,39 +702,44 @@ class KvPages:
         pages tables[r] (int32 [rows, entries], rows may be strided; e.g. the
         columns behind the prefix of a cache's table).  out: as q; lse: float32
         [rows, heads] or None; scale: 1 / sqrt(head_dim) if None."""
-        import torch
-        dtype = (self.pool.dtype,)
+        dtype = self.pool.dtype
         if not 0 <= layer < self.layers:
             raise HbfError(HBF_EINVAL, f"layer {layer}, the pool has {self.layers}")
-        _strided(q, "q", dtype, 3)
-        _writable(_strided(out, "out", dtype, 3), "out")
-        rows, heads, dim = q.shape
-        if dim != self.head_dim or out.shape != q.shape:
-            raise HbfError(HBF_EINVAL, f"q, out: shapes {tuple(q.shape)}, {tuple(out.shape)}, expected "
+        if not _is(q, dtype) or q.dim() != 3:
+            _strided(q, "q", (dtype,), 3)
+        if not _is(out, dtype):
+            _writable(_strided(out, "out", (dtype,), 3), "out")
+        shape = q.shape
+        rows, heads, dim = shape
+        if dim != self.head_dim or out.shape != shape:
+            raise HbfError(HBF_EINVAL, f"q, out: shapes {tuple(shape)}, {tuple(out.shape)}, expected "
                                        f"[rows, heads, {self.head_dim}]")
-        if lse is not None and not (isinstance(lse, torch.Tensor) and lse.is_cuda and lse.dtype is torch.float32
-                                    and lse.is_contiguous() and lse.shape == (rows, heads)):
+        if lse is not None and (not _is(lse, torch.float32) or lse.shape != shape[:2]):
             _dev(lse, "lse", ("float32",), shape=(rows, heads))
         prefix_len = int(prefix_len)
         if prefix_len > 0 and _ints(prefix_pages, "prefix_pages") * self.page_tokens < prefix_len:
             raise HbfError(HBF_EINVAL, f"prefix_pages: {prefix_pages.numel()} pages for {prefix_len} tokens")
         if (tables is None) != (own_lens is None):
             raise HbfError(HBF_EINVAL, "tables and own_lens: both or neither")
-        max_own = stride = 0
+        max_own = stride = own = 0
         if tables is not None:
-            if not isinstance(tables, torch.Tensor) or not tables.is_cuda or tables.dtype != torch.int32 \
-                    or tables.dim() != 2 or tables.shape[0] != rows \
-                    or (tables.shape[1] > 1 and tables.stride(1) != 1):
-                raise HbfError(HBF_EINVAL, f"tables: expected int32 [{rows}, entries] in GPU memory, rows contiguous")
+            if not _is(tables, torch.int32) or tables.dim() != 2 or tables.shape[0] != rows:
+                if not isinstance(tables, torch.Tensor) or not tables.is_cuda or tables.dtype != torch.int32 \
+                        or tables.dim() != 2 or tables.shape[0] != rows \
+                        or (tables.shape[1] > 1 and tables.stride(1) != 1):
+                    raise HbfError(HBF_EINVAL,
+                                   f"tables: expected int32 [{rows}, entries] in GPU memory, rows contiguous")
             _ints(own_lens, "own_lens", rows)
             max_own, stride = min(tables.shape[1] * self.page_tokens, (1 << 31) - 1), _stride(tables, 0)
+            own = own_lens.data_ptr()
         kv = self._layer(layer)
-        at = hbf_attention(q.data_ptr(), _stride(q, 0), _stride(q, 1), rows, heads,
+        qs, os = q.stride(), out.stride()   # (of a dimension of one entry: never taken, but it may be odd)
+        at = hbf_attention(q.data_ptr(), qs[0] if rows > 1 else 0, qs[1] if heads > 1 else 0, rows, heads,
                            dim ** -0.5 if scale is None else scale,
                            prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len,
-                           tables.data_ptr() if max_own else None, stride,
-                           own_lens.data_ptr() if own_lens is not None else None, max_own, out.data_ptr(),
-                           _stride(out, 0), _stride(out, 1), None if lse is None else lse.data_ptr())
+                           tables.data_ptr() if max_own else None, stride, own, max_own, out.data_ptr(),
+                           os[0] if rows > 1 else 0, os[1] if heads > 1 else 0,
+                           None if lse is None else lse.data_ptr())
         sizes = (rows, heads, prefix_len, max_own)
         if sizes != self._attn_sizes:
             b = ctypes.c_size_t()
@@ -767,11 +776,10 @@ class MoeLayer:
     ordered on one stream."""
 
     def __init__(self, gate_up, down, topk, router=None, renormalize=True, max_tokens=64):
-        import torch
-        self._lib = load_library()
+        self._lib = _import_torch()
         _strided(gate_up, "gate_up", (torch.bfloat16, torch.float16), 3, 2)
-        dtype = (gate_up.dtype,)
-        _strided(down, "down", dtype, 3, 2)
+        dtype = gate_up.dtype
+        _strided(down, "down", (dtype,), 3, 2)
         E, F2, H = gate_up.shape
         if F2 % 2 or tuple(down.shape) != (E, H, F2 // 2):
             raise HbfError(HBF_EINVAL, f"gate_up, down: shapes {tuple(gate_up.shape)}, {tuple(down.shape)}, expected "
@@ -796,16 +804,17 @@ class MoeLayer:
         """x, y: [tokens, hidden] (rows may be strided); ids: int32 [tokens,
         topk], weights: float32 [tokens, topk]: outputs, or the caller's
         choices where the layer has no router (-1: none)."""
-        import torch
-        _strided(x, "x", self._dtype, 2)
-        _writable(_strided(y, "y", self._dtype, 2), "y")
+        dtype = self._dtype
+        if not _is(x, dtype) or x.dim() != 2:
+            _strided(x, "x", (dtype,), 2)
+        if not _is(y, dtype):
+            _writable(_strided(y, "y", (dtype,), 2), "y")
         T = x.shape[0]
         if x.shape[1] != self.hidden or y.shape != x.shape:
             raise HbfError(HBF_EINVAL, f"x, y: shapes {tuple(x.shape)}, {tuple(y.shape)}, expected "
                                        f"[tokens, {self.hidden}]")
         for t, what, dt in ((ids, "ids", torch.int32), (weights, "weights", torch.float32)):
-            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dt and t.is_contiguous()
-                    and t.shape == (T, self.topk)):
+            if not _is(t, dt) or t.shape != (T, self.topk):
                 _dev(t, what, (str(dt).replace("torch.", ""),), shape=(T, self.topk))
         return self._lib.hbf_moe_layer(self._m, x.data_ptr(), _stride(x, 0), T, ids.data_ptr(), weights.data_ptr(),
                                        y.data_ptr(), _stride(y, 0), self._status.data_ptr(), self._ws.data_ptr(),
