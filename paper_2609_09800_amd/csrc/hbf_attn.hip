@@ -9,13 +9,13 @@
 // batch.  Own tokens are met by one row's G queries.  Both run in one launch,
 // each workgroup taking a part of the token axis for some queries:
 //  - few queries (own tokens; a prefix with at most 32 of them): bound by
-//    memory.  Each of eight waves takes 32 tokens at a time, K straight from
+//    memory.  Each of four waves takes 32 tokens at a time, K straight from
 //    memory into the matrix operand, V through LDS for its transpose, the next
 //    tokens' loads in flight meanwhile; the waves meet once, at the end.
 //  - many queries: bound by the matrix cores and the LDS.  64 tokens are staged
-//    for four waves of 32 queries each; two such groups of waves take turns
-//    with the tokens of a part, which halves the parts that leave the chip's
-//    registers (520 bytes a query and part).
+//    for four waves of 32 queries each.  Two workgroups on a CU, out of step
+//    with each other, keep its matrix cores and its vector units busy by turns
+//    (as one workgroup of eight waves, in step, they took half as long again).
 // Scores are computed transposed, S^T = K Q^T: a lane then holds one query's
 // scores of four consecutive tokens per tile of 16, which, rounded, are
 // already the operand of O^T = V^T P^T (the order of the tokens within a step
@@ -30,11 +30,10 @@
 namespace hbf {
 namespace {
 
-constexpr int THREADS = 512, WAVES = THREADS / 64;
+constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int FEW_TILE = 32;    // tokens of a wave's step where queries are few
 constexpr int MANY_TILE = 64;   // tokens staged where they are many
 constexpr int MANY_Q = 128;     // queries per workgroup there
-constexpr int MANY_GROUPS = 2;  // groups of MANY_Q / 32 waves, each with tokens of its own
 constexpr int JOIN_THREADS = 256, JOIN_WAVES = JOIN_THREADS / 64;
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
@@ -268,7 +267,8 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
 #pragma unroll
     for (int d = 0; d < DT; d++) *(f32x4 *)(ro + (w * 16 + col) * RS + d * 16 + kg * 4) = o[q][d];
     __syncthreads();
-    const int n = threadIdx.x >> 5, d0 = (threadIdx.x & 31) * 4;
+    constexpr int PER = THREADS / 16;  // threads per query
+    const int n = threadIdx.x / PER, d0 = threadIdx.x % PER * 4;
     const Query qq = query(q * 16 + n);
     if (qq.row >= 0) {
       float mx = -INFINITY, sum = 0.f;
@@ -282,11 +282,12 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
         sum += f[i] * rml[i * 16 + n].y;
       }
       const int64_t slot = part_slot(a, split, qq);
-      if (d0 < D) {
+#pragma unroll
+      for (int d = d0; d < D; d += PER * 4) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < WAVES; i++) x += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d0);
-        *(f32x4 *)(a.part + slot * D + d0) = x;
+        for (int i = 0; i < WAVES; i++) x += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
+        *(f32x4 *)(a.part + slot * D + d) = x;
       }
       if (d0 == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum);
     }
@@ -300,24 +301,21 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
 template <typename T, int D>
 __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int split, int m0, char *lds) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
-  constexpr int GW = MANY_Q / 32, GT = GW * 64;  // waves and threads of a group
-  const int group = w / GW, gw = w % GW, gt = threadIdx.x % GT;
+  static_assert(MANY_Q == 32 * WAVES && MANY_TILE * 4 == THREADS, "queries per wave, threads per staged token");
   constexpr int KS = D / 32, DT = D / 16, QT = 2, U = MANY_TILE / 16;
   constexpr int TILE_BYTES = MANY_TILE * D * 2;
-  char *mine = lds + group * 4 * TILE_BYTES;  // K and V of one step, then of the next
   auto query = [&](int n) {
     const int mm = m0 + n;
     const int row = mm / a.group;
     return row < a.at.rows ? Query{row, head * a.group + mm - row * a.group} : Query{-1, 0};
   };
   // staging: four threads per token, each every fourth 16-byte piece
-  const int st = gt >> 2, sp = gt & 3;
+  const int st = threadIdx.x >> 2, sp = threadIdx.x & 3;
   constexpr int SP = D / 32;
-  constexpr uint32_t STEP = MANY_GROUPS * MANY_TILE;
+  constexpr uint32_t STEP = MANY_TILE;
   u32x4 kv[SP], vv[SP];
   bool bad = false;
   int page = 0;
-  uint32_t base = t0 + group * MANY_TILE;
   auto find = [&](uint32_t b) { page = page_of(a, a.at.dev_prefix_pages, min(b + st, t1 - 1), &bad); };
   auto load = [&](uint32_t b) {
     const int64_t at = 2 * (token_at(a, page, min(b + st, t1 - 1), head) + sp * 8);
@@ -335,11 +333,11 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
       *(u32x4 *)(to + TILE_BYTES + tile_at<D>(st, k * 4 + sp)) = on ? vv[k] : u32x4{0, 0, 0, 0};
     }
   };
-  find(base);
+  find(t0);
   u32x4 qv[QT][KS];
 #pragma unroll
-  for (int q = 0; q < QT; q++) load_query<T, D>(a, query(gw * 32 + q * 16 + col), kg, qv[q]);
-  load(base);
+  for (int q = 0; q < QT; q++) load_query<T, D>(a, query(w * 32 + q * 16 + col), kg, qv[q]);
+  load(t0);
   f32x4 o[QT][DT];
   float m[QT], l[QT];
 #pragma unroll
@@ -349,56 +347,53 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
 #pragma unroll
     for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  find(base + STEP);
-  store(base, mine);
-  load(base + STEP);  // (past the end: the last token again)
-  find(base + 2 * STEP);
+  find(t0 + STEP);
+  store(t0, lds);
+  load(t0 + STEP);  // (past the end: the last token again)
+  find(t0 + 2 * STEP);
   __syncthreads();
   int cur = 0;
-  for (uint32_t b0 = t0;;) {
-    const char *kt = mine + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
-    if (base < t1) {
-      f32x4 s[QT][U];
+  for (uint32_t base = t0;;) {
+    const char *kt = lds + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+    f32x4 s[QT][U];
 #pragma unroll
-      for (int u = 0; u < U; u++) {
+    for (int u = 0; u < U; u++) {
 #pragma unroll
-        for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < KS; k++) {
-          const u32x4 kk = *(const u32x4 *)(kt + tile_at<D>(u * 16 + col, k * 4 + kg));
+      for (int k = 0; k < KS; k++) {
+        const u32x4 kk = *(const u32x4 *)(kt + tile_at<D>(u * 16 + col, k * 4 + kg));
 #pragma unroll
-          for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
-        }
+        for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
       }
-      if (t1 - base < MANY_TILE)
-#pragma unroll
-        for (int q = 0; q < QT; q++)
-#pragma unroll
-          for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-              if (base + u * 16 + kg * 4 + i >= t1) s[q][u][i] = -INFINITY;
-      softmax_step<QT, U, DT>(s, a.c, m, l, o);
-      u32x4 p[QT][U / 2];
+    }
+    if (t1 - base < MANY_TILE)
 #pragma unroll
       for (int q = 0; q < QT; q++)
 #pragma unroll
-        for (int u = 0; u < U / 2; u++) p[q][u] = p_operand<T>(s[q][2 * u], s[q][2 * u + 1]);
+        for (int u = 0; u < U; u++)
 #pragma unroll
-      for (int d = 0; d < DT; d++) {
+          for (int i = 0; i < 4; i++)
+            if (base + u * 16 + kg * 4 + i >= t1) s[q][u][i] = -INFINITY;
+    softmax_step<QT, U, DT>(s, a.c, m, l, o);
+    u32x4 p[QT][U / 2];
 #pragma unroll
-        for (int u = 0; u < U / 2; u++) {
-          const u32x4 v = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
+    for (int q = 0; q < QT; q++)
 #pragma unroll
-          for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][u], o[q][d]);
-        }
+      for (int u = 0; u < U / 2; u++) p[q][u] = p_operand<T>(s[q][2 * u], s[q][2 * u + 1]);
+#pragma unroll
+    for (int d = 0; d < DT; d++) {
+#pragma unroll
+      for (int u = 0; u < U / 2; u++) {
+        const u32x4 v = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
+#pragma unroll
+        for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][u], o[q][d]);
       }
     }
-    if (t1 - b0 <= STEP) break;
-    b0 += STEP;
+    if (t1 - base <= STEP) break;
     base += STEP;
-    store(base, mine + (cur ^ 1) * 2 * TILE_BYTES);
-    if (t1 - b0 > STEP) {
+    store(base, lds + (cur ^ 1) * 2 * TILE_BYTES);
+    if (t1 - base > STEP) {
       load(base + STEP);
       find(base + 2 * STEP);
     }
@@ -407,39 +402,21 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
   }
   const bool any_bad = __syncthreads_or(bad);
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
-  // the second group's sums join the first's, lane by lane
-  f32x4 *ro = (f32x4 *)lds;  // [QT][DT][GT]
-  float2 *rml = (float2 *)(lds + QT * DT * GT * 16);
-  if (group == 1) {
-#pragma unroll
-    for (int q = 0; q < QT; q++) {
-#pragma unroll
-      for (int d = 0; d < DT; d++) ro[(q * DT + d) * GT + gt] = o[q][d];
-      rml[q * GT + gt] = make_float2(m[q], l[q]);
-    }
-  }
-  __syncthreads();
-  if (group == 1) return;
 #pragma unroll
   for (int q = 0; q < QT; q++) {
-    const float2 other = rml[q * GT + gt];
-    const float top = fmaxf(m[q], other.x);
-    const float f0 = m[q] == top ? 1.f : __builtin_amdgcn_exp2f((m[q] - top) * a.c);
-    const float f1 = other.x == top ? 1.f : __builtin_amdgcn_exp2f((other.x - top) * a.c);
-    const float lq = across_rows(f0 * l[q] + f1 * other.y, SUM_OP);
-    const Query qq = query(gw * 32 + q * 16 + col);
+    const Query qq = query(w * 32 + q * 16 + col);
+    const float lq = across_rows(l[q], SUM_OP);
     if (qq.row < 0) continue;
     const int64_t slot = part_slot(a, split, qq);
 #pragma unroll
-    for (int d = 0; d < DT; d++)
-      *(f32x4 *)(a.part + slot * D + d * 16 + kg * 4) = f0 * o[q][d] + f1 * ro[(q * DT + d) * GT + gt];
-    if (kg == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(top * a.c, lq);
+    for (int d = 0; d < DT; d++) *(f32x4 *)(a.part + slot * D + d * 16 + kg * 4) = o[q][d];
+    if (kg == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(m[q] * a.c, lq);
   }
 }
 
 template <int D>
 constexpr int lds_bytes() {
-  const int many_b = MANY_GROUPS * 4 * MANY_TILE * D * 2;  // K and V, twice; the groups' join is smaller
+  const int many_b = 4 * MANY_TILE * D * 2;                     // K and V, twice
   const int few_b = WAVES * 16 * (D + 4) * 4 + WAVES * 16 * 8;  // the waves' join; V is smaller
   return many_b > few_b ? many_b : few_b;
 }
@@ -448,7 +425,7 @@ constexpr int lds_bytes() {
 // one XCD (block numbers equal modulo 8) so that they share its L2.  Then the
 // own tokens'.
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS) void k_attn(Args a) {
+__global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
   __shared__ __align__(16) char lds[lds_bytes<D>()];
   int b = blockIdx.x;
   if (b < a.prefix_blocks) {
@@ -588,9 +565,11 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
   a.few_q = m <= 16 ? 16 : m <= 32 ? 32 : 0;
   a.m_tiles = (int)(a.few_q ? 1 : (m + MANY_Q - 1) / MANY_Q);
   a.own_tiles = (a.group + 15) / 16;
-  // Parts: a workgroup per CU, the prefix's and the own ones' shares of the 256 as their shares of the work, in steps of a
-  // workgroup (128 tokens for many queries, 256 for few; rows' own tokens taken to be half of the most there can be).
-  const int64_t pre_step = a.few_q ? WAVES * FEW_TILE : MANY_GROUPS * MANY_TILE, own_step = WAVES * FEW_TILE;
+  // Parts: two workgroups per CU, the prefix's and the own ones' shares of the 512 as their shares of the work, in
+  // steps of a workgroup (64 tokens for many queries, 128 for few; rows' own tokens taken to be half of the most
+  // there can be), so that all run at the same time.
+  constexpr double SLOTS = 512;
+  const int64_t pre_step = a.few_q ? WAVES * FEW_TILE : MANY_TILE, own_step = WAVES * FEW_TILE;
   const int64_t pre_groups = (int64_t)kv.kv_heads * a.m_tiles, own_groups = (int64_t)at.rows * kv.kv_heads * a.own_tiles;
   const int64_t pre_steps = (at.prefix_len + pre_step - 1) / pre_step, own_steps = (at.max_own + own_step - 1) / own_step;
   const double pre_work = (double)pre_groups * pre_steps, own_work = (double)own_groups * own_steps / 2;
@@ -600,7 +579,7 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
     *chunk = (int)std::min<int64_t>(each * step, INT32_MAX / 2 / step * step);
     return (int)((tokens + *chunk - 1) / *chunk);
   };
-  const double slots = 256.0 / (pre_work + own_work + 1e-9);
+  const double slots = SLOTS / (pre_work + own_work + 1e-9);
   a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, slots * pre_work / pre_groups, &a.prefix_chunk);
   a.own_splits = cut(at.max_own, own_steps, own_step, slots * own_work / std::max<int64_t>(1, own_groups), &a.own_chunk);
   a.prefix_blocks = (a.prefix_splits * kv.kv_heads + 7) / 8 * 8 * a.m_tiles;
