@@ -60,17 +60,23 @@ template <int D>
 __device__ __forceinline__ int swizzle(int token) {  // spreads a column of 16-byte pieces over the banks
   return D == 128 ? token & 15 : (token >> 1) & 7;
 }
-// Byte offset of 16-byte piece `piece` of a token in a staged tile.
+// Byte offset of 16-byte piece `piece` of a token in a staged tile of K, whose
+// readers take one piece of 16 tokens at a time,
 template <int D>
-__device__ __forceinline__ int tile_at(int token, int piece) {
+__device__ __forceinline__ int k_at(int token, int piece) {
   return token * (D * 2) + ((piece ^ swizzle<D>(token)) << 4);
+}
+// and of V, whose readers take two pieces of 8 tokens in one cycle.
+template <int D>
+__device__ __forceinline__ int v_at(int token, int piece) {
+  return token * (D * 2) + ((piece ^ (D == 128 ? (token & 7) << 1 : token & 6)) << 4);
 }
 // The lane's operand of V^T: dimensions 16 dt .. + 15, tokens t0 .. + 3 and t1 .. + 3.
 template <int D>
 __device__ __forceinline__ u32x4 v_operand(const char *v, int t0, int t1, int dt, int lane) {
   const int i = lane & 15, piece = dt * 2 + ((i & 3) >> 1), half = (i & 1) << 3;
-  const u32x2 a = read_transposed(v + tile_at<D>(t0 + (i >> 2), piece) + half);
-  const u32x2 b = read_transposed(v + tile_at<D>(t1 + (i >> 2), piece) + half);
+  const u32x2 a = read_transposed(v + v_at<D>(t0 + (i >> 2), piece) + half);
+  const u32x2 b = read_transposed(v + v_at<D>(t1 + (i >> 2), piece) + half);
   return u32x4{a[0], a[1], b[0], b[1]};
 }
 
@@ -224,7 +230,7 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
         const bool on = !tail || base + u * 16 + col < t1;
 #pragma unroll
         for (int k = 0; k < KS; k++)
-          *(u32x4 *)(vt + tile_at<D>(u * 16 + col, k * 4 + kg)) = on ? vv[u][k] : u32x4{0, 0, 0, 0};
+          *(u32x4 *)(vt + v_at<D>(u * 16 + col, k * 4 + kg)) = on ? vv[u][k] : u32x4{0, 0, 0, 0};
       }
       wave_lds_fence();
       if (more) {
@@ -329,8 +335,8 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
     const bool on = b + st < t1;  // behind the last token: zero, whatever lies there
 #pragma unroll
     for (int k = 0; k < SP; k++) {
-      *(u32x4 *)(to + tile_at<D>(st, k * 4 + sp)) = kv[k];
-      *(u32x4 *)(to + TILE_BYTES + tile_at<D>(st, k * 4 + sp)) = on ? vv[k] : u32x4{0, 0, 0, 0};
+      *(u32x4 *)(to + k_at<D>(st, k * 4 + sp)) = kv[k];
+      *(u32x4 *)(to + TILE_BYTES + v_at<D>(st, k * 4 + sp)) = on ? vv[k] : u32x4{0, 0, 0, 0};
     }
   };
   find(t0);
@@ -355,16 +361,33 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
   int cur = 0;
   for (uint32_t base = t0;;) {
     const char *kt = lds + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+    // Operands come from LDS one group of products ahead of their use: left to
+    // itself the compiler waits for each group's reads right before it.
+    u32x4 kk[2][KS];
+    auto read_k = [&](int u) {
+#pragma unroll
+      for (int k = 0; k < KS; k++) kk[u & 1][k] = *(const u32x4 *)(kt + k_at<D>(u * 16 + col, k * 4 + kg));
+    };
     f32x4 s[QT][U];
+    read_k(0);
 #pragma unroll
     for (int u = 0; u < U; u++) {
+      if (u + 1 < U) read_k(u + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; k++) {
-        const u32x4 kk = *(const u32x4 *)(kt + tile_at<D>(u * 16 + col, k * 4 + kg));
+      for (int k = 0; k < KS; k++)
 #pragma unroll
-        for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
+        for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk[u & 1][k], qv[q][k], s[q][u]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const bool more = t1 - base > STEP;
+    if (more) {  // the next step's tile, here so that its writes and loads run beside the softmax
+      store(base + STEP, lds + (cur ^ 1) * 2 * TILE_BYTES);
+      if (t1 - base > 2 * STEP) {
+        load(base + 2 * STEP);
+        find(base + 3 * STEP);
       }
     }
     if (t1 - base < MANY_TILE)
@@ -375,28 +398,31 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
 #pragma unroll
           for (int i = 0; i < 4; i++)
             if (base + u * 16 + kg * 4 + i >= t1) s[q][u][i] = -INFINITY;
+    u32x4 vv2[2][U / 2];
+    auto read_v = [&](int d) {
+#pragma unroll
+      for (int u = 0; u < U / 2; u++)
+        vv2[d & 1][u] = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
+    };
     softmax_step<QT, U, DT>(s, a.c, m, l, o);
     u32x4 p[QT][U / 2];
 #pragma unroll
     for (int q = 0; q < QT; q++)
 #pragma unroll
       for (int u = 0; u < U / 2; u++) p[q][u] = p_operand<T>(s[q][2 * u], s[q][2 * u + 1]);
+    read_v(0);
 #pragma unroll
     for (int d = 0; d < DT; d++) {
+      if (d + 1 < DT) read_v(d + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < U / 2; u++) {
-        const u32x4 v = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
+      for (int u = 0; u < U / 2; u++)
 #pragma unroll
-        for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][u], o[q][d]);
-      }
+        for (int q = 0; q < QT; q++) o[q][d] = T::mfma(vv2[d & 1][u], p[q][u], o[q][d]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (t1 - base <= STEP) break;
+    if (!more) break;
     base += STEP;
-    store(base, lds + (cur ^ 1) * 2 * TILE_BYTES);
-    if (t1 - base > STEP) {
-      load(base + STEP);
-      find(base + 2 * STEP);
-    }
     __syncthreads();
     cur ^= 1;
   }
