@@ -9,9 +9,9 @@
 // batch.  Own tokens are met by one row's G queries.  Both run in one launch,
 // each workgroup taking a part of the token axis for some queries:
 //  - few queries (own tokens; a prefix with at most 32 of them): bound by
-//    memory.  Each of four waves takes 32 tokens at a time, K straight from
-//    memory into the matrix operand, V through LDS for its transpose, the next
-//    tokens' loads in flight meanwhile; the waves meet once, at the end.
+//    memory.  Each of four waves takes 32 tokens at a time through LDS of its
+//    own, the next tokens' loads in flight meanwhile; the waves meet once, at the
+//    end.
 //  - many queries: bound by the matrix cores and the LDS.  64 tokens are staged
 //    for four waves of 32 queries each.  Two workgroups on a CU, out of step
 //    with each other, keep its matrix cores and its vector units busy by turns
@@ -20,6 +20,10 @@
 // scores of four consecutive tokens per tile of 16, which, rounded, are
 // already the operand of O^T = V^T P^T (the order of the tokens within a step
 // is free as long as V's are read in the same one), so P never leaves its lane.
+// K and V are loaded a head's whole row (128 or 256 bytes) by neighbouring lanes
+// and take the operands' shape on the way through LDS: loaded straight into it,
+// in pieces of 64 bytes, they pass the CU's vector cache at half its rate
+// (28 bytes a clock measured), which bound both paths.
 #include <math.h>
 
 #include <algorithm>
@@ -136,17 +140,51 @@ __device__ __forceinline__ u32x4 p_operand(f32x4 a, f32x4 b) {
 __device__ __forceinline__ uint32_t page_index(const Args &a, uint32_t token) {
   return (uint32_t)((uint64_t)token * a.page_mul >> a.page_shift);
 }
-// Page of a token, with a page id out of range noted and page 0 read instead.
-__device__ __forceinline__ int page_of(const Args &a, const int32_t *pages, uint32_t token, bool *bad) {
-  const int p = pages[page_index(a, token)];
-  if (p >= 0 && p < a.kv.pages) return p;
-  *bad = true;
-  return 0;
-}
-__device__ __forceinline__ int64_t token_at(const Args &a, int page, uint32_t token, int head) {
-  const uint32_t in_page = token - page_index(a, token) * (uint32_t)a.kv.page_tokens;
-  return page * a.kv.page_stride + in_page * a.kv.token_stride + head * a.kv.head_stride;
-}
+
+// A wave's share of the staging: NT tokens, a row of D values each by D / 8
+// neighbouring lanes.  Lane i looks up where token i lies, the others ask it.
+template <int D, int NT>
+struct Stage {
+  static constexpr int LANES = D / 8, AT_ONCE = 64 / LANES, PASSES = NT / AT_ONCE;
+  u32x4 k[PASSES], v[PASSES];
+  int page = 0;
+  bool bad = false;
+
+  // Tokens base .. of [.., t1): their page ids (past t1: of its last token).
+  __device__ __forceinline__ void find(const Args &a, const int32_t *pages, uint32_t base, uint32_t t1) {
+    if (NT < 64 && (threadIdx.x & 63) >= NT) return;
+    page = pages[page_index(a, min(base + (threadIdx.x & 63), t1 - 1))];
+  }
+  __device__ __forceinline__ void load(const Args &a, uint32_t base, uint32_t t1, int head) {
+    const int lane = threadIdx.x & 63;
+    if (page < 0 || page >= a.kv.pages) {  // noted; page 0 is read instead
+      bad = true;
+      page = 0;
+    }
+    const uint32_t token = min(base + lane, t1 - 1);
+    const uint32_t in_page = token - page_index(a, token) * (uint32_t)a.kv.page_tokens;
+    const int64_t at = 2 * (page * a.kv.page_stride + in_page * a.kv.token_stride + head * a.kv.head_stride);
+#pragma unroll
+    for (int j = 0; j < PASSES; j++) {
+      const int from = j * AT_ONCE + lane / LANES;
+      const int64_t mine = (int64_t)(((uint64_t)(uint32_t)__shfl((int)(at >> 32), from) << 32) |
+                                     (uint32_t)__shfl((int)at, from)) + lane % LANES * 16;
+      k[j] = *(const u32x4 *)((const char *)a.kv.dev_k + mine);
+      v[j] = *(const u32x4 *)((const char *)a.kv.dev_v + mine);
+    }
+  }
+  // To tiles of K and V, as tokens first .. of them.  What lies behind the last
+  // token may be anything: 0 * NaN must not reach the sums.
+  __device__ __forceinline__ void store(char *kt, char *vt, int first, uint32_t base, uint32_t t1) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < PASSES; j++) {
+      const int t = j * AT_ONCE + lane / LANES;
+      *(u32x4 *)(kt + k_at<D>(first + t, lane % LANES)) = k[j];
+      *(u32x4 *)(vt + v_at<D>(first + t, lane % LANES)) = base + t < t1 ? v[j] : u32x4{0, 0, 0, 0};
+    }
+  }
+};
 
 struct Query {
   int row, head;  // row < 0: none
@@ -187,55 +225,33 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
 #pragma unroll
     for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  char *vt = lds + w * FEW_TILE * D * 2;
-  bool bad = false;
+  char *kt = lds + w * FEW_TILE * D * 4, *vt = kt + FEW_TILE * D * 2;
   uint32_t base = t0 + w * FEW_TILE;
-  u32x4 kv[2][KS], vv[2][KS];
-  int page[2];
-  auto find = [&](uint32_t b) {
-#pragma unroll
-    for (int u = 0; u < 2; u++) page[u] = page_of(a, pages, min(b + u * 16 + col, t1 - 1), &bad);
-  };
-  auto load = [&](uint32_t b) {
-#pragma unroll
-    for (int u = 0; u < 2; u++) {
-      const int64_t at = 2 * (token_at(a, page[u], min(b + u * 16 + col, t1 - 1), head) + kg * 8);
-#pragma unroll
-      for (int k = 0; k < KS; k++) {
-        kv[u][k] = *(const u32x4 *)((const char *)a.kv.dev_k + at + k * 64);
-        vv[u][k] = *(const u32x4 *)((const char *)a.kv.dev_v + at + k * 64);
-      }
-    }
-  };
+  Stage<D, FEW_TILE> st;
   constexpr uint32_t STEP = WAVES * FEW_TILE;
   if (base < t1) {
-    find(base);
-    load(base);
-    if (t1 - base > STEP) find(base + STEP);
+    st.find(a, pages, base, t1);
+    st.load(a, base, t1, head);
+    st.find(a, pages, base + STEP, t1);
     while (true) {
-      const bool more = t1 - base > STEP;
-      f32x4 s[QT][2];
-#pragma unroll
-      for (int q = 0; q < QT; q++)
-#pragma unroll
-        for (int u = 0; u < 2; u++) {
-          s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < KS; k++) s[q][u] = T::mfma(kv[u][k], qv[q][k], s[q][u]);
-        }
-      const bool tail = t1 - base < FEW_TILE;
-#pragma unroll
-      for (int u = 0; u < 2; u++) {
-        // what lies behind the last token may be anything: 0 * NaN must not reach the sums
-        const bool on = !tail || base + u * 16 + col < t1;
-#pragma unroll
-        for (int k = 0; k < KS; k++)
-          *(u32x4 *)(vt + v_at<D>(u * 16 + col, k * 4 + kg)) = on ? vv[u][k] : u32x4{0, 0, 0, 0};
-      }
+      const bool more = t1 - base > STEP, tail = t1 - base < FEW_TILE;
+      st.store(kt, vt, 0, base, t1);
       wave_lds_fence();
       if (more) {
-        load(base + STEP);
-        if (t1 - base > 2 * STEP) find(base + 2 * STEP);
+        st.load(a, base + STEP, t1, head);
+        st.find(a, pages, base + 2 * STEP, t1);
+      }
+      f32x4 s[QT][2];
+#pragma unroll
+      for (int u = 0; u < 2; u++) {
+#pragma unroll
+        for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+          const u32x4 kk = *(const u32x4 *)(kt + k_at<D>(u * 16 + col, k * 4 + kg));
+#pragma unroll
+          for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
+        }
       }
       if (tail)
 #pragma unroll
@@ -264,7 +280,7 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
   constexpr int RS = D + 4;  // a query's row, padded against bank conflicts
   float *ro = (float *)lds;  // [WAVES][16][RS], then the maxima and sums
   float2 *rml = (float2 *)(lds + WAVES * 16 * RS * 4);
-  const bool any_bad = __syncthreads_or(bad);
+  const bool any_bad = __syncthreads_or(st.bad);
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
 #pragma unroll
   for (int q = 0; q < QT; q++) {
@@ -307,7 +323,7 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
 template <typename T, int D>
 __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int split, int m0, char *lds) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
-  static_assert(MANY_Q == 32 * WAVES && MANY_TILE * 4 == THREADS, "queries per wave, threads per staged token");
+  static_assert(MANY_Q == 32 * WAVES, "queries per wave");
   constexpr int KS = D / 32, DT = D / 16, QT = 2, U = MANY_TILE / 16;
   constexpr int TILE_BYTES = MANY_TILE * D * 2;
   auto query = [&](int n) {
@@ -315,35 +331,15 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
     const int row = mm / a.group;
     return row < a.at.rows ? Query{row, head * a.group + mm - row * a.group} : Query{-1, 0};
   };
-  // staging: four threads per token, each every fourth 16-byte piece
-  const int st = threadIdx.x >> 2, sp = threadIdx.x & 3;
-  constexpr int SP = D / 32;
+  constexpr int NT = MANY_TILE / WAVES;  // tokens of a tile that a wave stages
   constexpr uint32_t STEP = MANY_TILE;
-  u32x4 kv[SP], vv[SP];
-  bool bad = false;
-  int page = 0;
-  auto find = [&](uint32_t b) { page = page_of(a, a.at.dev_prefix_pages, min(b + st, t1 - 1), &bad); };
-  auto load = [&](uint32_t b) {
-    const int64_t at = 2 * (token_at(a, page, min(b + st, t1 - 1), head) + sp * 8);
-#pragma unroll
-    for (int k = 0; k < SP; k++) {
-      kv[k] = *(const u32x4 *)((const char *)a.kv.dev_k + at + k * 64);
-      vv[k] = *(const u32x4 *)((const char *)a.kv.dev_v + at + k * 64);
-    }
-  };
-  auto store = [&](uint32_t b, char *to) {
-    const bool on = b + st < t1;  // behind the last token: zero, whatever lies there
-#pragma unroll
-    for (int k = 0; k < SP; k++) {
-      *(u32x4 *)(to + k_at<D>(st, k * 4 + sp)) = kv[k];
-      *(u32x4 *)(to + TILE_BYTES + v_at<D>(st, k * 4 + sp)) = on ? vv[k] : u32x4{0, 0, 0, 0};
-    }
-  };
-  find(t0);
+  const int32_t *pages = a.at.dev_prefix_pages;
+  Stage<D, NT> st;
+  st.find(a, pages, t0 + w * NT, t1);
   u32x4 qv[QT][KS];
 #pragma unroll
   for (int q = 0; q < QT; q++) load_query<T, D>(a, query(w * 32 + q * 16 + col), kg, qv[q]);
-  load(t0);
+  st.load(a, t0 + w * NT, t1, head);
   f32x4 o[QT][DT];
   float m[QT], l[QT];
 #pragma unroll
@@ -353,10 +349,10 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
 #pragma unroll
     for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  find(t0 + STEP);
-  store(t0, lds);
-  load(t0 + STEP);  // (past the end: the last token again)
-  find(t0 + 2 * STEP);
+  st.find(a, pages, t0 + STEP + w * NT, t1);
+  st.store(lds, lds + TILE_BYTES, w * NT, t0 + w * NT, t1);
+  st.load(a, t0 + STEP + w * NT, t1, head);  // (past the end: the last token again)
+  st.find(a, pages, t0 + 2 * STEP + w * NT, t1);
   __syncthreads();
   int cur = 0;
   for (uint32_t base = t0;;) {
@@ -384,10 +380,11 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
     }
     const bool more = t1 - base > STEP;
     if (more) {  // the next step's tile, here so that its writes and loads run beside the softmax
-      store(base + STEP, lds + (cur ^ 1) * 2 * TILE_BYTES);
+      char *next = lds + (cur ^ 1) * 2 * TILE_BYTES;
+      st.store(next, next + TILE_BYTES, w * NT, base + STEP + w * NT, t1);
       if (t1 - base > 2 * STEP) {
-        load(base + 2 * STEP);
-        find(base + 3 * STEP);
+        st.load(a, base + 2 * STEP + w * NT, t1, head);
+        st.find(a, pages, base + 3 * STEP + w * NT, t1);
       }
     }
     if (t1 - base < MANY_TILE)
@@ -426,7 +423,7 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
     __syncthreads();
     cur ^= 1;
   }
-  const bool any_bad = __syncthreads_or(bad);
+  const bool any_bad = __syncthreads_or(st.bad);
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
 #pragma unroll
   for (int q = 0; q < QT; q++) {
@@ -443,7 +440,7 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
 template <int D>
 constexpr int lds_bytes() {
   const int many_b = 4 * MANY_TILE * D * 2;                     // K and V, twice
-  const int few_b = WAVES * 16 * (D + 4) * 4 + WAVES * 16 * 8;  // the waves' join; V is smaller
+  const int few_b = WAVES * FEW_TILE * D * 4;                 // K and V of each wave; the waves' join is smaller
   return many_b > few_b ? many_b : few_b;
 }
 
