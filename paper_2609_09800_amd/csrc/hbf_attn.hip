@@ -493,13 +493,14 @@ __global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
                min(t0 + (uint32_t)a.own_chunk, (uint32_t)len), head, a.prefix_splits + split, query, lds);
 }
 
-// Join a query's parts: a workgroup per query, its waves taking every fourth part.
-template <typename T, int D>
+// Join a query's parts by PER waves, each taking every PER-th part.
+template <typename T, int D, int PER>
 __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
   constexpr int V = D / 64;
   __shared__ float so[JOIN_WAVES][D], sm[JOIN_WAVES], sl[JOIN_WAVES];
-  const int64_t qi = blockIdx.x;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, pw = w % PER;
+  const int64_t qi = (int64_t)blockIdx.x * (JOIN_WAVES / PER) + w / PER;
+  if (PER < JOIN_WAVES && qi >= (int64_t)a.at.rows * a.at.heads) return;
   const int row = (int)(qi / a.at.heads), head = (int)(qi - (int64_t)row * a.at.heads);
   int own = 0;
   bool bad = false;
@@ -515,12 +516,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
   for (int v = 0; v < V; v++) o[v] = 0.f;
   // sums relative to a first maximum, raised as parts of larger ones come (NaN, a part of bad pages, stays)
   constexpr int U = 8;
-  for (int i0 = w; i0 < n; i0 += JOIN_WAVES * U) {
+  for (int i0 = pw; i0 < n; i0 += PER * U) {
     float2 ml[U];
     float p[U][V];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int i = i0 + u * JOIN_WAVES;
+      const int i = i0 + u * PER;
       ml[u] = i < n ? a.part_ml[i * stride + qi] : make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int v = 0; v < V; v++) p[u][v] = i < n ? a.part[(i * stride + qi) * D + lane * V + v] : 0.f;
@@ -541,24 +542,27 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
       for (int v = 0; v < V; v++) o[v] += f * p[u][v];
     }
   }
+  if (PER > 1) {
 #pragma unroll
-  for (int v = 0; v < V; v++) so[w][lane * V + v] = o[v];
-  sm[w] = m;
-  sl[w] = l;
-  __syncthreads();
-  if (w) return;
+    for (int v = 0; v < V; v++) so[w][lane * V + v] = o[v];
+    sm[w] = m;
+    sl[w] = l;
+    __syncthreads();
+    static_assert(PER == 1 || PER == JOIN_WAVES, "a query's waves are a workgroup");
+    if (w) return;
 #pragma unroll
-  for (int i = 1; i < JOIN_WAVES; i++) m = fmaxf(m, sm[i]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  l = 0.f;
+    for (int i = 1; i < JOIN_WAVES; i++) m = fmaxf(m, sm[i]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = 0.f;
 #pragma unroll
-  for (int v = 0; v < V; v++) o[v] = 0.f;
+    for (int v = 0; v < V; v++) o[v] = 0.f;
 #pragma unroll
-  for (int i = 0; i < JOIN_WAVES; i++) {
-    const float f = __builtin_amdgcn_exp2f(sm[i] - ref);
-    l += f * sl[i];
+    for (int i = 0; i < JOIN_WAVES; i++) {
+      const float f = __builtin_amdgcn_exp2f(sm[i] - ref);
+      l += f * sl[i];
 #pragma unroll
-    for (int v = 0; v < V; v++) o[v] += f * so[i][lane * V + v];
+      for (int v = 0; v < V; v++) o[v] += f * so[i][lane * V + v];
+    }
   }
   if (bad) {
     l = NAN;
@@ -589,22 +593,22 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
   a.m_tiles = (int)(a.few_q ? 1 : (m + MANY_Q - 1) / MANY_Q);
   a.own_tiles = (a.group + 15) / 16;
   // Parts: two workgroups per CU, the prefix's and the own ones' shares of the 512 as their shares of the work, in
-  // steps of a workgroup (64 tokens for many queries, 128 for few; rows' own tokens taken to be half of the most
-  // there can be), so that all run at the same time.
+  // steps of a workgroup (64 tokens for many queries, 128 for few), so that all run at the same time.  A part of many
+  // queries has 4 steps at least: its sums, 66 KB, take as long to write and join as two.
   constexpr double SLOTS = 512;
   const int64_t pre_step = a.few_q ? WAVES * FEW_TILE : MANY_TILE, own_step = WAVES * FEW_TILE;
   const int64_t pre_groups = (int64_t)kv.kv_heads * a.m_tiles, own_groups = (int64_t)at.rows * kv.kv_heads * a.own_tiles;
   const int64_t pre_steps = (at.prefix_len + pre_step - 1) / pre_step, own_steps = (at.max_own + own_step - 1) / own_step;
-  const double pre_work = (double)pre_groups * pre_steps, own_work = (double)own_groups * own_steps / 2;
-  auto cut = [](int64_t tokens, int64_t all, int64_t step, double groups, int *chunk) {
+  const double pre_work = (double)pre_groups * pre_steps, own_work = (double)own_groups * own_steps;
+  auto cut = [](int64_t tokens, int64_t all, int64_t step, int64_t least, double groups, int *chunk) {
     if (tokens <= 0) return 0;
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(all, (int64_t)groups)), each = (all + parts - 1) / parts;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((all + least - 1) / least, (int64_t)groups)), each = (all + parts - 1) / parts;
     *chunk = (int)std::min<int64_t>(each * step, INT32_MAX / 2 / step * step);
     return (int)((tokens + *chunk - 1) / *chunk);
   };
   const double slots = SLOTS / (pre_work + own_work + 1e-9);
-  a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, slots * pre_work / pre_groups, &a.prefix_chunk);
-  a.own_splits = cut(at.max_own, own_steps, own_step, slots * own_work / std::max<int64_t>(1, own_groups), &a.own_chunk);
+  a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, a.few_q ? 1 : 4, slots * pre_work / pre_groups, &a.prefix_chunk);
+  a.own_splits = cut(at.max_own, own_steps, own_step, 1, slots * own_work / std::max<int64_t>(1, own_groups), &a.own_chunk);
   a.prefix_blocks = (a.prefix_splits * kv.kv_heads + 7) / 8 * 8 * a.m_tiles;
   return a;
 }
@@ -614,7 +618,12 @@ hipError_t run(const Args &a, hipStream_t s) {
   const int64_t blocks =
       a.prefix_blocks + (int64_t)a.own_splits * a.at.rows * a.kv.kv_heads * a.own_tiles;
   if (blocks > 0) k_attn<T, D><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
-  k_attn_join<T, D><<<(uint32_t)a.at.rows * a.at.heads, JOIN_THREADS, 0, s>>>(a);
+  // a wave per query has the parts of two rounds of loads to wait for at most
+  const uint32_t queries = (uint32_t)a.at.rows * a.at.heads;
+  if (a.prefix_splits + a.own_splits <= 16 && queries >= 512)
+    k_attn_join<T, D, 1><<<(queries + JOIN_WAVES - 1) / JOIN_WAVES, JOIN_THREADS, 0, s>>>(a);
+  else
+    k_attn_join<T, D, JOIN_WAVES><<<queries, JOIN_THREADS, 0, s>>>(a);
   return hipGetLastError();
 }
 
