@@ -55,10 +55,10 @@ __device__ __forceinline__ V across_wave(V x, F op) {
   auto join = [&](uint32_t a, uint32_t b) {
     u = __builtin_bit_cast(uint32_t, op(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b)));
   };
-  join(u, __builtin_amdgcn_update_dpp(u, u, 0xb1, 0xf, 0xf, false));   // quad_perm 1,0,3,2
-  join(u, __builtin_amdgcn_update_dpp(u, u, 0x4e, 0xf, 0xf, false));   // quad_perm 2,3,0,1
-  join(u, __builtin_amdgcn_update_dpp(u, u, 0x141, 0xf, 0xf, false));  // row_half_mirror
-  join(u, __builtin_amdgcn_update_dpp(u, u, 0x140, 0xf, 0xf, false));  // row_mirror
+  join(u, __builtin_amdgcn_update_dpp(0, u, 0xb1, 0xf, 0xf, true));   // quad_perm 1,0,3,2
+  join(u, __builtin_amdgcn_update_dpp(0, u, 0x4e, 0xf, 0xf, true));   // quad_perm 2,3,0,1
+  join(u, __builtin_amdgcn_update_dpp(0, u, 0x141, 0xf, 0xf, true));  // row_half_mirror
+  join(u, __builtin_amdgcn_update_dpp(0, u, 0x140, 0xf, 0xf, true));  // row_mirror
   const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
   join(a[0], a[1]);
   const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
