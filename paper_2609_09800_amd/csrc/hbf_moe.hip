@@ -12,7 +12,8 @@
 //  - route: logits by tiles of 16 experts and 16 tokens; a token tile's last
 //    workgroup chooses, and the last of these sorts the (token, choice) pairs
 //    by expert, in tiles of up to 16 (an expert with more is read once per
-//    tile, by workgroups that run beside each other);
+//    tile, by workgroups that run beside each other).  For up to four tokens
+//    the logits only: up chooses;
 //  - up: 8 gate rows and the 8 up rows of the same channels per tile of weights,
 //    so that its products give 8 channels of h;
 //  - down: 32 rows of y per tile and unit, each pair's product to a place of its
@@ -41,6 +42,7 @@ constexpr int SUM_THREADS = 256;
 constexpr int MAX_PAIRS = MOE_MAX_PAIRS;
 constexpr int MAX_TILES = MOE_MAX_EXPERTS + MAX_PAIRS / 16;
 constexpr int TOKEN_TILES = MOE_MAX_TOKENS / 16;
+constexpr int FEW_TOKENS = WAVES, FEW_PAIRS = FEW_TOKENS * MOE_MAX_TOPK, FEW_EXPERTS = 256;
 
 struct Tile {                           // up to 16 pairs of one expert
   int32_t expert;
@@ -74,6 +76,7 @@ struct Args {
   char *h_hi, *h_lo;                    // [pairs][F], in the order of `pair`
   float *part;                          // [pairs][H] products, by token and choice
   uint32_t *block_done;                 // [H / 16] token tiles whose products of these rows are there
+  bool choose_in_up;                    // few tokens: every workgroup of up makes the choices for itself
   bool sum_in_down;                     // few units: the last workgroup of a block of rows sums it
 };
 
@@ -103,15 +106,18 @@ constexpr u32x4 ZERO4 = {0, 0, 0, 0};
 // ------------------------------------------------------------ route
 
 // The topk choices of token t by one wave; lane l holds experts l EPL .. + EPL-1.
-template <int EPL>
-__device__ void choose(const Args &a, int t, int32_t *ids) {
+// ids: in LDS.  HANDED: the logits are of this launch, and so may be the readers
+// of a.ids.  write: to the caller's arrays too.
+template <int EPL, bool HANDED>
+__device__ void choose(const Args &a, int t, int32_t *ids, bool write = true) {
   const int lane = threadIdx.x & 63, E = a.m.experts, k = a.m.topk;
   float v[EPL];
   uint32_t key[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; i++) {
     const int e = lane * EPL + i;
-    v[i] = e < E ? handed(a.logits + (int64_t)t * a.e_pad + e) : 0.f;
+    const float *from = a.logits + (int64_t)t * a.e_pad + min(e, E - 1);
+    v[i] = HANDED ? handed(from) : *from;
     const uint32_t u = __float_as_uint(v[i]);
     // the floats' order as that of whole numbers; NaN below all, 0 for none (left)
     key[i] = e >= E ? 0 : isnan(v[i]) ? 1 : u & 0x80000000u ? ~u : u | 0x80000000u;
@@ -156,7 +162,8 @@ __device__ void choose(const Args &a, int t, int32_t *ids) {
   }
   sum = across_wave(sum, [](float x, float y) { return x + y; });
   if (lane < k) {
-    ids[t * k + lane] = chosen;  // (LDS: complete where this workgroup chooses for all tokens)
+    ids[t * k + lane] = chosen;
+    if (!write) return;
     __hip_atomic_store(a.ids + t * k + lane, chosen, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     a.weights[t * k + lane] = w / sum;
   }
@@ -216,13 +223,14 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
         for (int i = 0; i < 4; i++) hand_over(a.logits + (int64_t)(t0 + col) * a.e_pad + e0 + kg * 4 + i, acc[i]);
       stores_done();
     }
+    if (a.choose_in_up) return;
     const int tile = blockIdx.x / e_tiles;
     if (!last_of(&a.ctl->arrived[tile], e_tiles)) return;
     for (int tt = t0 + w; tt < min(t0 + 16, a.tokens); tt += ROUTE_WAVES) {
-      if (E <= 64) choose<1>(a, tt, ids);
-      else if (E <= 128) choose<2>(a, tt, ids);
-      else if (E <= 256) choose<4>(a, tt, ids);
-      else choose<16>(a, tt, ids);
+      if (E <= 64) choose<1, true>(a, tt, ids);
+      else if (E <= 128) choose<2, true>(a, tt, ids);
+      else if (E <= 256) choose<4, true>(a, tt, ids);
+      else choose<16, true>(a, tt, ids);
     }
     const int t_tiles = gridDim.x / e_tiles;
     if (t_tiles > 1) {
@@ -283,13 +291,61 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
 
 // ------------------------------------------------------------ up
 
+// The route of at most FEW_TOKENS tokens from their logits, made by each
+// workgroup for itself in LDS; the first one leaves it for the others' launch.
+// All of them sort the pairs the same way: by expert, then token and choice.
+struct FewLists {
+  int32_t ids[FEW_PAIRS], pair[FEW_PAIRS], rank[FEW_PAIRS];
+  Tile tile[FEW_PAIRS];
+  int32_t n_tiles;
+};
+__device__ void route_few(const Args &a, FewLists &f) {
+  const int w = threadIdx.x >> 6, p = threadIdx.x, pairs = a.tokens * a.m.topk;
+  if (w < a.tokens) choose<FEW_EXPERTS / 64, false>(a, w, f.ids, blockIdx.x == 0);
+  if (p == 0) f.n_tiles = 0;
+  __syncthreads();
+  int before = 0, rank = 0, count = 0;  // pairs of lower experts; of mine, those before me and all
+  if (p < pairs) {
+    const int e = f.ids[p];
+    for (int q = 0; q < pairs; q++) {
+      before += f.ids[q] < e;
+      rank += f.ids[q] == e && q < p;
+      count += f.ids[q] == e;
+    }
+    f.pair[before + rank] = p;
+    f.rank[p] = rank;
+  }
+  __syncthreads();
+  if (p < pairs && rank % 16 == 0) {
+    int tile = rank / 16;
+    for (int q = 0; q < pairs; q++) tile += f.ids[q] < f.ids[p] && f.rank[q] % 16 == 0;
+    f.tile[tile] = Tile{f.ids[p], (uint16_t)(before + rank), (uint16_t)min(count - rank, 16)};
+    atomicAdd(&f.n_tiles, 1);
+  }
+  __syncthreads();
+  if (blockIdx.x) return;
+  if (p < pairs) a.lists->pair[p] = f.pair[p];
+  if (p < f.n_tiles) a.lists->tile[p] = f.tile[p];
+  if (p == 0) a.lists->n_tiles = f.n_tiles;
+  if (a.sum_in_down)
+    for (int i = p; i <= a.m.hidden / 16; i += THREADS) a.block_done[i] = 0;
+}
+
 // KS steps of 32 per wave and pass; EXACT: the hidden size is one pass of them.
 template <typename T, int KS, bool EXACT>
 __global__ __launch_bounds__(THREADS) void k_moe_up(Args a) {
   __shared__ f32x4 red[2][WAVES][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   const int H = a.m.hidden, F = a.m.ffn, blocks = F / 8;
-  const int64_t units = (int64_t)a.lists->n_tiles * blocks;
+  __shared__ FewLists few;
+  const Tile *tiles = a.lists->tile;
+  const int32_t *pairs = a.lists->pair;
+  if (a.choose_in_up) {
+    route_few(a, few);
+    tiles = few.tile;
+    pairs = few.pair;
+  }
+  const int64_t units = (int64_t)(a.choose_in_up ? few.n_tiles : (int)a.lists->n_tiles) * blocks;
   const int u0 = (int)(units * blockIdx.x / gridDim.x), u1 = (int)(units * (blockIdx.x + 1) / gridDim.x);
   if (u0 >= u1) return;
   const int passes = EXACT ? 1 : (H + WAVES * KS * 32 - 1) / (WAVES * KS * 32);
@@ -313,10 +369,10 @@ __global__ __launch_bounds__(THREADS) void k_moe_up(Args a) {
     }
   };
   int ti = u0 / blocks, block = u0 - ti * blocks, buf = 0;
-  Tile tile = a.lists->tile[ti];
+  Tile tile = tiles[ti];
   load_w(tile.expert, block, 0);
   // columns past the tokens repeat the last
-  int token = a.lists->pair[tile.start + min(col, (int)tile.count - 1)] / a.m.topk;
+  int token = pairs[tile.start + min(col, (int)tile.count - 1)] / a.m.topk;
   if (passes == 1) load_x(token, 0);  // kept for all of the tile's units
   for (int u = u0; u < u1; u++) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -331,8 +387,8 @@ __global__ __launch_bounds__(THREADS) void k_moe_up(Args a) {
     if (u + 1 < u1) {  // the next loads are in flight while this unit ends
       if (++block == blocks) {
         block = 0;
-        tile = a.lists->tile[++ti];
-        token = a.lists->pair[tile.start + min(col, (int)tile.count - 1)] / a.m.topk;
+        tile = tiles[++ti];
+        token = pairs[tile.start + min(col, (int)tile.count - 1)] / a.m.topk;
         if (passes == 1) load_x(token, 0);
       }
       load_w(tile.expert, block, 0);
@@ -524,6 +580,9 @@ hipError_t run(Args a, hipStream_t s) {
   // with it; 5 tokens of 20 small experts: 14.9, 16.9).  Where workgroups have several units, waiting for each one's
   // stores would cost more.
   a.sum_in_down = (int64_t)tiles * ((a.m.hidden + 31) / 32) <= GROUPS;
+  // A workgroup's four waves choose for four tokens side by side, which takes it 3 us, the route's hand-over from
+  // workgroup to workgroup 5 (one token of the 128-expert layer: 30.8 us, 32.6 without it).
+  a.choose_in_up = a.m.dev_router && a.tokens <= FEW_TOKENS && a.m.experts <= FEW_EXPERTS;
   const int route = a.m.dev_router ? a.e_pad / 16 * ((a.tokens + 15) / 16) : 1;
   k_moe_route<T><<<route, ROUTE_THREADS, 0, s>>>(a);
   const int groups = (int)std::min<int64_t>((int64_t)tiles * (a.m.ffn / 8), GROUPS);
