@@ -13,9 +13,11 @@
 //    own, the next tokens' loads in flight meanwhile; the waves meet once, at the
 //    end.
 //  - many queries: bound by the matrix cores and the LDS.  64 tokens are staged
-//    for four waves of 32 queries each.  Two workgroups on a CU, out of step
-//    with each other, keep its matrix cores and its vector units busy by turns
-//    (as one workgroup of eight waves, in step, they took half as long again).
+//    for four waves of 32 queries each, loaded past the registers (64 rows over
+//    32,771 tokens: 59.6 us, 63.3 by way of them).  Two workgroups on a CU, out of
+//    step with each other, keep its matrix cores and its vector units busy by
+//    turns (as one workgroup of eight waves, in step, they took half as long
+//    again).
 // Scores are computed transposed, S^T = K Q^T: a lane then holds one query's
 // scores of four consecutive tokens per tile of 16, which, rounded, are
 // already the operand of O^T = V^T P^T (the order of the tokens within a step
@@ -186,6 +188,47 @@ struct Stage {
   }
 };
 
+// The same share loaded past the registers: a wave's lanes' 16 bytes each fall
+// side by side into LDS, so that the pieces' order within a row is in the
+// addresses asked for.
+template <int D, int NT>
+struct StageLds {
+  static constexpr int LANES = D / 8, AT_ONCE = 64 / LANES, PASSES = NT / AT_ONCE;
+  int page = 0;
+  bool bad = false;
+
+  __device__ __forceinline__ void find(const Args &a, const int32_t *pages, uint32_t base, uint32_t t1) {
+    if (NT < 64 && (threadIdx.x & 63) >= NT) return;
+    page = pages[page_index(a, min(base + (threadIdx.x & 63), t1 - 1))];
+  }
+  // Tokens base .. (past t1: its last one again) to tokens first .. of a tile; there after loads_done().
+  __device__ __forceinline__ void load(const Args &a, uint32_t base, uint32_t t1, int head, uint32_t kt, uint32_t vt,
+                                       int first) {
+    const int lane = threadIdx.x & 63;
+    if (page < 0 || page >= a.kv.pages) {  // noted; page 0 is read instead
+      bad = true;
+      page = 0;
+    }
+    const uint32_t token = min(base + lane, t1 - 1);
+    const uint32_t in_page = token - page_index(a, token) * (uint32_t)a.kv.page_tokens;
+    const int64_t at = 2 * (page * a.kv.page_stride + in_page * a.kv.token_stride + head * a.kv.head_stride);
+    uint32_t hi[PASSES], lo[PASSES];
+#pragma unroll
+    for (int j = 0; j < PASSES; j++) {
+      hi[j] = (uint32_t)__shfl((int)(at >> 32), j * AT_ONCE + lane / LANES);
+      lo[j] = (uint32_t)__shfl((int)at, j * AT_ONCE + lane / LANES);
+    }
+#pragma unroll
+    for (int j = 0; j < PASSES; j++) {
+      const int t = first + j * AT_ONCE;  // of the wave's first lanes
+      const int64_t row = (int64_t)((uint64_t)hi[j] << 32 | lo[j]);
+      const int mine = t + lane / LANES, piece = lane % LANES * 16;
+      to_lds((const char *)a.kv.dev_k + row + (piece ^ (k_at<D>(mine, 0) - mine * (D * 2))), kt + t * (D * 2));
+      to_lds((const char *)a.kv.dev_v + row + (piece ^ (v_at<D>(mine, 0) - mine * (D * 2))), vt + t * (D * 2));
+    }
+  }
+};
+
 struct Query {
   int row, head;  // row < 0: none
 };
@@ -334,12 +377,13 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
   constexpr int NT = MANY_TILE / WAVES;  // tokens of a tile that a wave stages
   constexpr uint32_t STEP = MANY_TILE;
   const int32_t *pages = a.at.dev_prefix_pages;
-  Stage<D, NT> st;
+  const uint32_t lds0 = lds_address(lds);
+  StageLds<D, NT> st;
   st.find(a, pages, t0 + w * NT, t1);
   u32x4 qv[QT][KS];
 #pragma unroll
   for (int q = 0; q < QT; q++) load_query<T, D>(a, query(w * 32 + q * 16 + col), kg, qv[q]);
-  st.load(a, t0 + w * NT, t1, head);
+  st.load(a, t0 + w * NT, t1, head, lds0, lds0 + TILE_BYTES, w * NT);
   f32x4 o[QT][DT];
   float m[QT], l[QT];
 #pragma unroll
@@ -350,13 +394,17 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
     for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   st.find(a, pages, t0 + STEP + w * NT, t1);
-  st.store(lds, lds + TILE_BYTES, w * NT, t0 + w * NT, t1);
-  st.load(a, t0 + STEP + w * NT, t1, head);  // (past the end: the last token again)
-  st.find(a, pages, t0 + 2 * STEP + w * NT, t1);
+  loads_done();
   __syncthreads();
   int cur = 0;
   for (uint32_t base = t0;;) {
     const char *kt = lds + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
+    if (t1 - base < MANY_TILE) {  // 0 * infinity must not reach the sums: no V behind the last token
+      const int left = (int)(t1 - base);
+      for (int i = left * D * 2 + threadIdx.x * 16; i < TILE_BYTES; i += THREADS * 16)
+        *(u32x4 *)(lds + cur * 2 * TILE_BYTES + TILE_BYTES + i) = u32x4{0, 0, 0, 0};
+      __syncthreads();
+    }
     // Operands come from LDS one group of products ahead of their use: left to
     // itself the compiler waits for each group's reads right before it.
     u32x4 kk[2][KS];
@@ -379,13 +427,10 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
       __builtin_amdgcn_sched_barrier(0);
     }
     const bool more = t1 - base > STEP;
-    if (more) {  // the next step's tile, here so that its writes and loads run beside the softmax
-      char *next = lds + (cur ^ 1) * 2 * TILE_BYTES;
-      st.store(next, next + TILE_BYTES, w * NT, base + STEP + w * NT, t1);
-      if (t1 - base > 2 * STEP) {
-        st.load(a, base + 2 * STEP + w * NT, t1, head);
-        st.find(a, pages, base + 3 * STEP + w * NT, t1);
-      }
+    if (more) {  // the next step's tile, here so that its addresses are found beside the products
+      const uint32_t next = lds0 + (cur ^ 1) * 2 * TILE_BYTES;
+      st.load(a, base + STEP + w * NT, t1, head, next, next + TILE_BYTES, w * NT);
+      if (t1 - base > 2 * STEP) st.find(a, pages, base + 2 * STEP + w * NT, t1);
     }
     if (t1 - base < MANY_TILE)
 #pragma unroll
@@ -420,6 +465,7 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
     }
     if (!more) break;
     base += STEP;
+    loads_done();
     __syncthreads();
     cur ^= 1;
   }

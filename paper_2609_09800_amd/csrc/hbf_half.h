@@ -91,6 +91,19 @@ __device__ __forceinline__ float handed(const float *from) {
 }
 __device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// 16 bytes of each lane, from an address of its own, to LDS at `to` (the same in
+// all lanes) + 16 lane.  In flight until loads_done(); the compiler does not know.
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
+}
+__device__ __forceinline__ void to_lds(const void *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(
+                   __builtin_amdgcn_readfirstlane((int)to)),
+               "v"(from)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // What the lanes of one wave have written to LDS is read by others of it: the
 // LDS serves a wave's accesses in order, so only the compiler is held.
 __device__ __forceinline__ void wave_lds_fence() {
