@@ -159,10 +159,11 @@ __device__ __forceinline__ void copy_bytes(char *dst, const char *src, int64_t b
 
 // What a list's check leaves of it: entry i changes row slot[i]; a fork's
 // parent is from[i], its length len[i]; extend's held[i] pages come before
-// those it gets; off[i] pages are needed by the entries before i.
+// those it gets, and part[i], if not -1, is a part-full page that must be its own
+// (null: checked already); off[i] pages are needed by the entries before i.
 struct List {
   int32_t *slot, *from, *len;
-  int32_t *held;
+  int32_t *held, *part;
   uint32_t *off;
 };
 
@@ -180,6 +181,7 @@ __device__ uint32_t check_list(const hbf_kv &kv, const List &out, const int32_t 
     const int i = i0 + t;
     uint32_t need = 0;
     if (i < n) {
+      int part = -1;
       const int a = first[i], b = second[i];
       const int slot = FORK ? b : a;  // the one whose row changes
       int len = 0, held = 0;
@@ -200,8 +202,8 @@ __device__ uint32_t check_list(const hbf_kv &kv, const List &out, const int32_t 
           held = pages_of(len, kv.page_tokens);
           need = pages_of((int)grown, kv.page_tokens) - held;
           if (b > 0 && len % kv.page_tokens != 0) {
-            const int p = row_of(kv, kv.dev_tables, slot)[held - 1];
-            ok = p >= 0 && p < kv.pages && kv.dev_refs[p] == 1;
+            part = row_of(kv, kv.dev_tables, slot)[held - 1];
+            ok = part >= 0 && part < kv.pages && (out.part || kv.dev_refs[part] == 1);
           }
         }
       }
@@ -209,11 +211,13 @@ __device__ uint32_t check_list(const hbf_kv &kv, const List &out, const int32_t 
         err |= KV_ERR_ARG;
         need = 0;
         len = 0;
+        part = -1;
       }
       if (out.slot) out.slot[i] = slot;
       if (out.from) out.from[i] = a;
       if (out.len) out.len[i] = len;
       if (out.held) out.held[i] = held;
+      if (out.part) out.part[i] = part;
       // (a need past every page is refused below; clamped, the sums stay in range)
       if (need > KV_MAX_PAGES) need = KV_MAX_PAGES + 1;
     }
@@ -235,8 +239,9 @@ __device__ uint32_t check_list(const hbf_kv &kv, const List &out, const int32_t 
   return err;
 }
 
-// A fork's parent's row of `len` tokens, by threads t of nt.
-__device__ uint32_t check_row(const hbf_kv &kv, int from, int len, int t, int nt) {
+// A fork's parent's row of `len` tokens, by threads t of nt; used(p): page p has holders.
+template <typename F>
+__device__ uint32_t check_row(const hbf_kv &kv, int from, int len, int t, int nt, F used) {
   uint32_t err = 0;
   const int held = pages_of(len, kv.page_tokens);
   if (held == 0) return 0;
@@ -244,25 +249,25 @@ __device__ uint32_t check_row(const hbf_kv &kv, int from, int len, int t, int nt
 #pragma unroll 4
   for (int c = t; c < held; c += nt) {
     const int p = row[c];
-    if (p < 0 || p >= kv.pages || kv.dev_refs[p] <= 0) err = KV_ERR_ARG;
+    if (p < 0 || p >= kv.pages || !used(p)) err = KV_ERR_ARG;
   }
   return err;
 }
 
-// The free pages of a workgroup's N * PT from p0 on (refs r), the first of them
-// of rank `rank`, go to the entries that need them.  `pages`: LDS.  FORK:
-// taken[i] receives the child's page.
-template <bool FORK, int N, int PT>
-__device__ void give_pages(const hbf_kv &kv, const List &list, int n, int p0, const int32_t (&r)[PT], uint32_t rank,
-                           uint32_t need, uint16_t *pages, uint32_t *lds, int32_t *taken) {
-  uint32_t c = 0, total;
-#pragma unroll
-  for (int i = 0; i < PT; i++) c += r[i] == 0;
-  uint32_t at = block_scan<N>(c, &total, lds);
+// The free pages of this thread's (refs r), `at` of the workgroup's before them,
+// to the workgroup's list in LDS.
+template <int PT>
+__device__ __forceinline__ void list_free(const int32_t (&r)[PT], uint32_t at, uint16_t *pages) {
 #pragma unroll
   for (int i = 0; i < PT; i++)
     if (r[i] == 0) pages[at++] = (uint16_t)(threadIdx.x * PT + i);
-  __syncthreads();
+}
+// The workgroup's `total` free pages, from p0 on, the first of them of rank
+// `rank`, go to the entries that need them.  FORK: taken[i] receives the child's
+// page.
+template <bool FORK, int N>
+__device__ void give_pages(const hbf_kv &kv, const List &list, int n, int p0, uint32_t total, uint32_t rank,
+                           uint32_t need, const uint16_t *pages, int32_t *taken) {
   for (uint32_t k = threadIdx.x; k < total && rank + k < need; k += N) {
     const uint32_t mine = rank + k;
     int lo = 0, hi = n;  // the last entry whose offset is at most the rank
@@ -306,28 +311,43 @@ __global__ __launch_bounds__(ONE) void k_kv_one(hbf_kv kv, KvWs w, const int32_t
   extern __shared__ uint32_t seen[];
   __shared__ uint16_t pages[ONE * PT];
   __shared__ int32_t slot[SMALL_LIST], from[SMALL_LIST], len[SMALL_LIST], held[SMALL_LIST];
-  __shared__ uint32_t off[SMALL_LIST + 1], lds[ONE / 64];
-  const List list = {slot, from, len, held, off};
+  __shared__ uint32_t off[SMALL_LIST + 1], lds[ONE / 64], errs;
+  // a bit per page: has holders (fork), has one (extend); counts are looked up here, not in memory once more
+  __shared__ uint16_t held_by[ONE];
+  static_assert(PT <= 16, "bits of a word");
+  const List list = {slot, FORK ? from : nullptr, len, held, FORK ? nullptr : from, off};
   const int t = threadIdx.x;
   int32_t r[PT];
   load_refs(kv, t * PT, 1, r);
+  if (t == 0) errs = 0;
   uint32_t err = check_list<FORK, ONE>(kv, list, first, second, n, seen, lds);
-  __syncthreads();
-  if (FORK)
-    for (int i = t / ROW; i < n; i += ONE / ROW) err |= check_row(kv, from[i], len[i], t % ROW, ROW);
-  uint32_t c = 0, free_pages;
+  uint32_t c = 0, free_pages, bits = 0;
 #pragma unroll
-  for (int i = 0; i < PT; i++) c += r[i] == 0;
-  block_scan<ONE>(c, &free_pages, lds);
+  for (int i = 0; i < PT; i++) {
+    c += r[i] == 0;
+    bits |= (uint32_t)(FORK ? r[i] > 0 : r[i] == 1) << i;
+  }
+  held_by[t] = (uint16_t)bits;
+  const uint32_t before = block_scan<ONE>(c, &free_pages, lds);
+  auto has = [&](int p) { return held_by[p / PT] >> (p % PT) & 1; };
+  list_free(r, before, pages);
+  if (FORK) {
+    for (int i = t / ROW; i < n; i += ONE / ROW) err |= check_row(kv, from[i], len[i], t % ROW, ROW, has);
+  } else {
+    for (int i = t; i < n; i += ONE)
+      if (list.part[i] >= 0 && !has(list.part[i])) err |= KV_ERR_ARG;
+  }
+  if (err) atomicOr(&errs, err);
+  __syncthreads();
   const uint32_t need = off[n];
-  const bool bad = __syncthreads_or(err & KV_ERR_ARG), full = __syncthreads_or(err & KV_ERR_PAGES) || need > free_pages;
+  const bool bad = errs & KV_ERR_ARG, full = errs & KV_ERR_PAGES || need > free_pages;
   if (t == 0) {
     w.ctl->go = !bad && !full;
     if (bad || full) w.ctl->sticky |= bad ? KV_ERR_ARG : KV_ERR_PAGES;
   }
   if (bad || full) return;
   // (the pages that the children get: `held`, which fork has no other use for)
-  give_pages<FORK, ONE>(kv, list, n, 0, r, 0, need, pages, lds, held);
+  give_pages<FORK, ONE>(kv, list, n, 0, free_pages, 0, need, pages, held);
   if (!FORK) {
     for (int i = t; i < n; i += ONE) kv.dev_lens[slot[i]] = len[i] + second[i];
     return;
@@ -354,7 +374,7 @@ __global__ __launch_bounds__(ONE) void k_kv_one(hbf_kv kv, KvWs w, const int32_t
 // The list as the launches of a large call hand it on.
 template <bool FORK>
 __device__ List list_of(const KvWs &w) {
-  return List{nullptr, nullptr, FORK ? w.len : nullptr, FORK ? nullptr : w.at, w.need_off};
+  return List{nullptr, nullptr, FORK ? w.len : nullptr, FORK ? nullptr : w.at, nullptr, w.need_off};
 }
 
 // Large calls.  Workgroups 0 .. tiles-1 count their tile's free pages; the next
@@ -381,7 +401,7 @@ __global__ __launch_bounds__(THREADS) void k_kv_plan(hbf_kv kv, KvWs w, const in
     const int from = first[b - tiles - 1];
     if (from >= 0 && from < kv.slots) {  // (the list's check has the others)
       const int len = kv.dev_lens[from];
-      if (len_fits(kv, len)) err = check_row(kv, from, len, t, THREADS);
+      if (len_fits(kv, len)) err = check_row(kv, from, len, t, THREADS, [&](int p) { return kv.dev_refs[p] > 0; });
     }
   }
   if (!plan_done(w.ctl, err)) return;
@@ -409,7 +429,12 @@ __global__ __launch_bounds__(THREADS) void k_kv_apply(hbf_kv kv, KvWs w, const i
     load_refs(kv, b * TILE + t * PER_THREAD, 1, r);
     List list = list_of<FORK>(w);
     list.slot = (int32_t *)(FORK ? second : first);
-    give_pages<FORK, THREADS>(kv, list, n, b * TILE, r, rank, need, pages, lds, w.at);
+    uint32_t c = 0, total;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD; i++) c += r[i] == 0;
+    list_free(r, block_scan<THREADS>(c, &total, lds), pages);
+    __syncthreads();
+    give_pages<FORK, THREADS>(kv, list, n, b * TILE, total, rank, need, pages, w.at);
   } else if (FORK) {
     share_row(kv, first[b - tiles], w.len[b - tiles], second[b - tiles], t, THREADS);
   } else {
