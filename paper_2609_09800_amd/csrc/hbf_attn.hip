@@ -548,30 +548,37 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
   const int64_t qi = (int64_t)blockIdx.x * (JOIN_WAVES / PER) + w / PER;
   if (PER < JOIN_WAVES && qi >= (int64_t)a.at.rows * a.at.heads) return;
   const int row = (int)(qi / a.at.heads), head = (int)(qi - (int64_t)row * a.at.heads);
-  int own = 0;
-  bool bad = false;
-  if (a.at.dev_own_len) {
-    const int len = a.at.dev_own_len[row];
-    bad = len < 0 || len > a.at.max_own;
-    if (!bad && len > 0) own = (int)(((uint32_t)len + (uint32_t)a.own_chunk - 1) / (uint32_t)a.own_chunk);
-  }
-  const int n = a.prefix_splits + own;
+  const int len = a.at.dev_own_len ? a.at.dev_own_len[row] : 0;
   const int64_t stride = (int64_t)a.at.rows * a.at.heads;
   float m = -INFINITY, l = 0.f, o[V];
 #pragma unroll
   for (int v = 0; v < V; v++) o[v] = 0.f;
   // sums relative to a first maximum, raised as parts of larger ones come (NaN, a part of bad pages, stays)
   constexpr int U = 8;
-  for (int i0 = pw; i0 < n; i0 += PER * U) {
-    float2 ml[U];
-    float p[U][V];
+  float2 ml[U];
+  float p[U][V];
+  auto load = [&](int i0, int end) {
 #pragma unroll
     for (int u = 0; u < U; u++) {
       const int i = i0 + u * PER;
-      ml[u] = i < n ? a.part_ml[i * stride + qi] : make_float2(-INFINITY, 0.f);
+      ml[u] = i < end ? a.part_ml[i * stride + qi] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-      for (int v = 0; v < V; v++) p[u][v] = i < n ? a.part[(i * stride + qi) * D + lane * V + v] : 0.f;
+      for (int v = 0; v < V; v++) p[u][v] = i < end ? a.part[(i * stride + qi) * D + lane * V + v] : 0.f;
     }
+  };
+  load(pw, a.prefix_splits + a.own_splits);  // without waiting for the length: parts that are none are left out below
+  const bool bad = len < 0 || len > a.at.max_own;
+  const int own = bad || len == 0 ? 0 : (int)(((uint32_t)len + (uint32_t)a.own_chunk - 1) / (uint32_t)a.own_chunk);
+  const int n = a.prefix_splits + own;
+#pragma unroll
+  for (int u = 0; u < U; u++)
+    if (pw + u * PER >= n) {
+      ml[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int v = 0; v < V; v++) p[u][v] = 0.f;
+    }
+  for (int i0 = pw; i0 < n; i0 += PER * U) {
+    if (i0 != pw) load(i0, n);
     float top = m;
 #pragma unroll
     for (int u = 0; u < U; u++) top = fmaxf(top, ml[u].x);
