@@ -543,6 +543,8 @@ typedef struct {
   void *dev_out;              /* [rows][heads][head_dim], strides as q's, 16-byte aligned */
   int64_t out_row_stride, out_head_stride;
   float *dev_lse;             /* [rows][heads], or NULL */
+  uint32_t *dev_ctl;          /* 64 words, zero before the first call and kept by the calls from then on; calls that share
+                                 them must be ordered on one stream.  NULL: small calls take a launch more */
 } hbf_attention;
 
 /* Device scratch of a call, in bytes (only sizes and strides are looked at). */

@@ -18,6 +18,8 @@
 //    step with each other, keep its matrix cores and its vector units busy by
 //    turns (as one workgroup of eight waves, in step, they took half as long
 //    again).
+// The parts are joined by a launch of their own, or, where they are few, by the
+// last workgroup of each KV head.
 // Scores are computed transposed, S^T = K Q^T: a lane then holds one query's
 // scores of four consecutive tokens per tile of 16, which, rounded, are
 // already the operand of O^T = V^T P^T (the order of the tokens within a step
@@ -60,6 +62,8 @@ struct Args {
   float *part;          // [splits][rows][heads][head_dim] sums of p v
   float2 *part_ml;      // [splits][rows][heads] maximum (of s log2 e) and sum
   int32_t *status;
+  uint32_t *ctl;        // a KV head's workgroups that are done, where the last one joins; else null
+  uint32_t arrivals;    // workgroups per KV head
 };
 
 template <int D>
@@ -251,7 +255,7 @@ __device__ __forceinline__ void load_query(const Args &a, Query q, int kgroup, u
 
 // Tokens [t0, t1) (t0 < t1) of a page list for 16 QT queries, one per column;
 // query(col) names them.
-template <typename T, int D, int QT, typename Q>
+template <typename T, int D, int QT, bool HERE, typename Q>
 __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t1, int head, int split, Q query,
                     char *lds) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
@@ -352,9 +356,14 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < WAVES; i++) x += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
-        *(f32x4 *)(a.part + slot * D + d) = x;
+        if (HERE) hand_over((f32x4 *)(a.part + slot * D + d), x);
+        else *(f32x4 *)(a.part + slot * D + d) = x;
       }
-      if (d0 == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum);
+      if (d0 == 0) {
+        const float2 ml = any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum);
+        if (HERE) hand_over(a.part_ml + slot, ml);
+        else a.part_ml[slot] = ml;
+      }
     }
     __syncthreads();
   }
@@ -483,6 +492,96 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
   }
 }
 
+// ------------------------------------------------------------ join
+
+// Row `row`'s parts; bad: its length is out of range (then it counts as empty).
+__device__ __forceinline__ int parts_of(const Args &a, int len, bool *bad) {
+  *bad = len < 0 || len > a.at.max_own;
+  const int own = *bad || len == 0 ? 0 : (int)(((uint32_t)len + (uint32_t)a.own_chunk - 1) / (uint32_t)a.own_chunk);
+  return a.prefix_splits + own;
+}
+// V of a query's values, from d0 on, from its sums; none: it saw no token.  lead: the one thread that writes lse.
+template <typename T, int V>
+__device__ __forceinline__ void write_out(const Args &a, int row, int head, int d0, const float (&o)[V], float m, float l,
+                                          bool none, bool bad, bool lead) {
+  if (bad) {
+    l = NAN;
+    if (a.status && lead) *a.status = HBF_EINVAL;
+  }
+  none = none && !bad;
+  const float inv = none ? 0.f : 1.f / l;
+  typename T::elem *out = (typename T::elem *)a.at.dev_out + row * a.at.out_row_stride + head * a.at.out_head_stride + d0;
+#pragma unroll
+  for (int v = 0; v < V; v++) out[v] = (typename T::elem)(o[v] * inv);
+  if (a.at.dev_lse && lead) a.at.dev_lse[(int64_t)row * a.at.heads + head] = none ? -INFINITY : m * LN2 + logf(l);
+}
+
+// The running sums (m, l, o) take U parts in, relative to a first maximum, raised
+// as parts of larger ones come (NaN, a part of bad pages, stays).
+template <int U, int V>
+__device__ __forceinline__ void take_parts(const float2 (&ml)[U], const float (&p)[U][V], float &m, float &l,
+                                           float (&o)[V]) {
+  float top = m;
+#pragma unroll
+  for (int u = 0; u < U; u++) top = fmaxf(top, ml[u].x);
+  const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
+  m = top;
+  l *= alpha;
+#pragma unroll
+  for (int v = 0; v < V; v++) o[v] *= alpha;
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
+    l += f * ml[u].y;
+#pragma unroll
+    for (int v = 0; v < V; v++) o[v] += f * p[u][v];
+  }
+}
+
+// All queries of one KV head by one workgroup, from parts that others of the
+// launch handed over: D / 4 lanes a query, R queries each, at most HERE_PARTS / R
+// parts a query, so that a thread asks for all it needs at once (parts past a
+// row's own are none, and left out).
+constexpr int HERE_PARTS = 24;
+template <typename T, int D, int R>
+__device__ void join_here(const Args &a, int kv_head) {
+  constexpr int LANES = D / 4, U = HERE_PARTS / R;
+  const int d0 = threadIdx.x % LANES * 4, all = a.prefix_splits + a.own_splits;
+  const int64_t stride = (int64_t)a.at.rows * a.at.heads;
+  const int last = a.at.rows * a.group - 1;
+  int len[R];
+  float2 ml[R][U];
+  f32x4 x[R][U];
+  auto query = [&](int r) { return (int)threadIdx.x / LANES + r * (THREADS / LANES); };
+#pragma unroll
+  for (int r = 0; r < R; r++) {  // (no branches: past the last query its own again, past the last part that one)
+    const int mm = min(query(r), last), row = mm / a.group;
+    const int64_t qi = (int64_t)row * a.at.heads + kv_head * a.group + mm - row * a.group;
+    len[r] = a.at.dev_own_len ? a.at.dev_own_len[row] : 0;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int64_t slot = min(u, all - 1) * stride + qi;
+      ml[r][u] = a.part_ml[slot];
+      x[r][u] = *(const f32x4 *)(a.part + slot * D + d0);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; r++) {
+    bool bad;
+    const int n = parts_of(a, len[r], &bad);
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f}, p[U][4];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      if (u >= n) ml[r][u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int v = 0; v < 4; v++) p[u][v] = u < n ? x[r][u][v] : 0.f;
+    }
+    take_parts(ml[r], p, m, l, o);
+    const int mm = query(r), row = mm / a.group;
+    if (mm <= last) write_out<T>(a, row, kv_head * a.group + mm - row * a.group, d0, o, m, l, n == 0, bad, d0 == 0);
+  }
+}
+
 template <int D>
 constexpr int lds_bytes() {
   const int many_b = 4 * MANY_TILE * D * 2;                     // K and V, twice
@@ -490,10 +589,23 @@ constexpr int lds_bytes() {
   return many_b > few_b ? many_b : few_b;
 }
 
+// A workgroup's part is written.
+template <typename T, int D, bool HERE>
+__device__ void end(const Args &a, int kv_head) {
+  if (!HERE) return;
+  stores_done();
+  if (!last_of(a.ctl + kv_head, a.arrivals)) return;
+  see_handed();
+  const int m = a.at.rows * a.group, at_once = THREADS / (D / 4);
+  if (m <= at_once) join_here<T, D, 1>(a, kv_head);
+  else if (m <= 2 * at_once) join_here<T, D, 2>(a, kv_head);
+  else join_here<T, D, 4>(a, kv_head);
+}
+
 // Workgroups [0, prefix_blocks): the prefix, those of one part and KV head on
 // one XCD (block numbers equal modulo 8) so that they share its L2.  Then the
-// own tokens'.
-template <typename T, int D>
+// own tokens'.  HERE: few queries, joined by the last workgroups.
+template <typename T, int D, bool HERE>
 __global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
   __shared__ __align__(16) char lds[lds_bytes<D>()];
   int b = blockIdx.x;
@@ -503,7 +615,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
     const int head = sh % a.kv.kv_heads, split = sh / a.kv.kv_heads;
     const uint32_t t0 = (uint32_t)split * (uint32_t)a.prefix_chunk;
     const uint32_t t1 = min(t0 + (uint32_t)a.prefix_chunk, (uint32_t)a.at.prefix_len);
-    if (a.few_q == 0) {
+    if (!HERE && a.few_q == 0) {
       many<T, D>(a, t0, t1, head, split, mt * MANY_Q, lds);
       return;
     }
@@ -513,9 +625,10 @@ __global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
       return row < a.at.rows ? Query{row, head * a.group + mm - row * a.group} : Query{-1, 0};
     };
     if (a.few_q == 16)
-      few<T, D, 1>(a, a.at.dev_prefix_pages, t0, t1, head, split, query, lds);
+      few<T, D, 1, HERE>(a, a.at.dev_prefix_pages, t0, t1, head, split, query, lds);
     else
-      few<T, D, 2>(a, a.at.dev_prefix_pages, t0, t1, head, split, query, lds);
+      few<T, D, 2, HERE>(a, a.at.dev_prefix_pages, t0, t1, head, split, query, lds);
+    end<T, D, HERE>(a, head);
     return;
   }
   b -= a.prefix_blocks;
@@ -527,16 +640,21 @@ __global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
   const int len = a.at.dev_own_len[row];
   if (len < 0 || len > a.at.max_own) {
     if (threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
+    end<T, D, HERE>(a, head);
     return;
   }
   const uint32_t t0 = (uint32_t)split * (uint32_t)a.own_chunk;
-  if (t0 >= (uint32_t)len) return;
+  if (t0 >= (uint32_t)len) {
+    end<T, D, HERE>(a, head);
+    return;
+  }
   auto query = [&](int n) {
     const int g = tile * 16 + n;
     return g < a.group ? Query{row, head * a.group + g} : Query{-1, 0};
   };
-  few<T, D, 1>(a, a.at.dev_tables + (int64_t)row * a.at.table_stride, t0,
+  few<T, D, 1, HERE>(a, a.at.dev_tables + (int64_t)row * a.at.table_stride, t0,
                min(t0 + (uint32_t)a.own_chunk, (uint32_t)len), head, a.prefix_splits + split, query, lds);
+  end<T, D, HERE>(a, head);
 }
 
 // Join a query's parts by PER waves, each taking every PER-th part.
@@ -553,7 +671,6 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
   float m = -INFINITY, l = 0.f, o[V];
 #pragma unroll
   for (int v = 0; v < V; v++) o[v] = 0.f;
-  // sums relative to a first maximum, raised as parts of larger ones come (NaN, a part of bad pages, stays)
   constexpr int U = 8;
   float2 ml[U];
   float p[U][V];
@@ -567,9 +684,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
     }
   };
   load(pw, a.prefix_splits + a.own_splits);  // without waiting for the length: parts that are none are left out below
-  const bool bad = len < 0 || len > a.at.max_own;
-  const int own = bad || len == 0 ? 0 : (int)(((uint32_t)len + (uint32_t)a.own_chunk - 1) / (uint32_t)a.own_chunk);
-  const int n = a.prefix_splits + own;
+  bool bad;
+  const int n = parts_of(a, len, &bad);
 #pragma unroll
   for (int u = 0; u < U; u++)
     if (pw + u * PER >= n) {
@@ -579,21 +695,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
     }
   for (int i0 = pw; i0 < n; i0 += PER * U) {
     if (i0 != pw) load(i0, n);
-    float top = m;
-#pragma unroll
-    for (int u = 0; u < U; u++) top = fmaxf(top, ml[u].x);
-    const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
-    m = top;
-    l *= alpha;
-#pragma unroll
-    for (int v = 0; v < V; v++) o[v] *= alpha;
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
-      l += f * ml[u].y;
-#pragma unroll
-      for (int v = 0; v < V; v++) o[v] += f * p[u][v];
-    }
+    take_parts(ml, p, m, l, o);
   }
   if (PER > 1) {
 #pragma unroll
@@ -617,16 +719,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
       for (int v = 0; v < V; v++) o[v] += f * so[i][lane * V + v];
     }
   }
-  if (bad) {
-    l = NAN;
-    if (a.status && lane == 0) *a.status = HBF_EINVAL;
-  }
-  const float inv = n == 0 && !bad ? 0.f : 1.f / l;
-  typename T::elem *out =
-      (typename T::elem *)a.at.dev_out + row * a.at.out_row_stride + head * a.at.out_head_stride + lane * V;
-#pragma unroll
-  for (int v = 0; v < V; v++) out[v] = (typename T::elem)(o[v] * inv);
-  if (a.at.dev_lse && lane == 0) a.at.dev_lse[qi] = n == 0 && !bad ? -INFINITY : m * LN2 + logf(l);
+  write_out<T>(a, row, head, lane * V, o, m, l, n == 0, bad, lane == 0);
 }
 
 // Sizes of a call: how the token axes are cut.
@@ -662,6 +755,15 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
   const double slots = SLOTS / (pre_work + own_work + 1e-9);
   a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, a.few_q ? 1 : 4, slots * pre_work / pre_groups, &a.prefix_chunk);
   a.own_splits = cut(at.max_own, own_steps, own_step, 1, slots * own_work / std::max<int64_t>(1, own_groups), &a.own_chunk);
+  // A KV head's last workgroup joins its queries where a thread can ask for their parts at once: a launch less, 3.4 us
+  // of the host's time and 4 of the GPU's (7 rows of 3 queries over 1,003 tokens: 9.1 us, 11.9 with it; one row of 8
+  // over 300: 9.0, 11.7; one over 4,096 tokens: 11.1, 11.6).  A part is two steps if that makes them few enough.
+  const int64_t at_once = THREADS / (kv.head_dim / 4), each = m <= at_once ? 1 : m <= 2 * at_once ? 2 : 4;
+  const int64_t most = HERE_PARTS / each - a.own_splits;
+  if (a.few_q && a.prefix_splits > most && (pre_steps + 1) / 2 <= most)
+    a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, 2, INT32_MAX, &a.prefix_chunk);
+  a.arrivals = (uint32_t)(a.prefix_splits + (int64_t)at.rows * a.own_splits * a.own_tiles);
+  if (a.few_q && a.arrivals && kv.kv_heads <= ATTN_CTL_WORDS && a.prefix_splits <= most) a.ctl = at.dev_ctl;
   a.prefix_blocks = (a.prefix_splits * kv.kv_heads + 7) / 8 * 8 * a.m_tiles;
   return a;
 }
@@ -670,7 +772,11 @@ template <typename T, int D>
 hipError_t run(const Args &a, hipStream_t s) {
   const int64_t blocks =
       a.prefix_blocks + (int64_t)a.own_splits * a.at.rows * a.kv.kv_heads * a.own_tiles;
-  if (blocks > 0) k_attn<T, D><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+  if (a.ctl) {
+    k_attn<T, D, true><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  if (blocks > 0) k_attn<T, D, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
   // a wave per query has the parts of two rounds of loads to wait for at most
   const uint32_t queries = (uint32_t)a.at.rows * a.at.heads;
   if (a.prefix_splits + a.own_splits <= 16 && queries >= 512)

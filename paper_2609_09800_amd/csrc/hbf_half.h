@@ -86,10 +86,38 @@ __device__ __forceinline__ float across_rows(float x, F op) {
 __device__ __forceinline__ void hand_over(float *to, float v) {
   __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+__device__ __forceinline__ void hand_over(f32x4 *to, f32x4 v) {
+  const u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+    __hip_atomic_store((uint64_t *)to + i, (uint64_t)u[2 * i + 1] << 32 | u[2 * i], __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void hand_over(float2 *to, float2 v) {
+  __hip_atomic_store((uint64_t *)to, (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ float handed(const float *from) {
   return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+// After last_of: ordinary loads too find what was handed over.
+__device__ __forceinline__ void see_handed() { __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent"); }
 __device__ __forceinline__ void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// True in every thread of the last of n workgroups to get here; the counter is
+// 0 again.  What a workgroup hands over before, its stores done, the last one
+// finds.
+static __device__ bool last_of(uint32_t *counter, uint32_t n) {
+  __shared__ uint32_t last;
+  __syncthreads();
+  if (n == 1) return true;
+  if (threadIdx.x == 0) {
+    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == n;
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return last != 0;
+}
 
 // 16 bytes of each lane, from an address of its own, to LDS at `to` (the same in
 // all lanes) + 16 lane.  In flight until loads_done(); the compiler does not know.

@@ -169,21 +169,6 @@ __device__ void choose(const Args &a, int t, int32_t *ids, bool write = true) {
   }
 }
 
-// True in every thread of the last of n workgroups to get here; the counter is
-// 0 again.  What a workgroup hands over before, its stores done, the last one
-// finds.
-__device__ bool last_of(uint32_t *counter, uint32_t n) {
-  __shared__ uint32_t last;
-  __syncthreads();
-  if (n == 1) return true;
-  if (threadIdx.x == 0) {
-    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == n;
-    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  return last != 0;
-}
-
 template <typename T>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_moe_route(Args a) {
   __shared__ f32x4 red[ROUTE_WAVES][64];

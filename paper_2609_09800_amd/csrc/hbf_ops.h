@@ -36,6 +36,7 @@ hipError_t launch_kv_compact(const hbf_kv &kv, int32_t *remap, int32_t *tables_o
 hipError_t launch_kv_write(const hbf_kv &kv, int layer0, int layers, const void *k, const void *v,
                            const int32_t *slots, const int32_t *pos, int n, hipStream_t s);
 
+constexpr int ATTN_CTL_WORDS = 64;
 size_t attn_ws_bytes(const hbf_kv_layer &kv, const hbf_attention &at);
 hipError_t launch_attn(const hbf_kv_layer &kv, const hbf_attention &at, int32_t *status, void *ws, hipStream_t s);
 

@@ -163,7 +163,7 @@ int hbf_kv_attention(const hbf_kv_layer *kv, const hbf_attention *at, int32_t *s
   if (at->max_own > 0 && (!at->dev_tables || !at->dev_own_len || !aligned(at->dev_tables, 4) ||
                           !aligned(at->dev_own_len, 4)))
     return HBF_EINVAL;
-  if (!ws || !aligned(ws, 256)) return HBF_EINVAL;
+  if (!ws || !aligned(ws, 256) || !aligned(at->dev_ctl, 4)) return HBF_EINVAL;
   if (ws_bytes < attn_ws_bytes(*kv, *at)) return HBF_ENOWORKSPACE;
   return status_of(launch_attn(*kv, *at, status, ws, (hipStream_t)stream));
 }

@@ -80,7 +80,7 @@ class hbf_attention(ctypes.Structure):
                 ("dev_tables", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
                 ("dev_own_len", ctypes.c_void_p), ("max_own", ctypes.c_int32), ("dev_out", ctypes.c_void_p),
                 ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
-                ("dev_lse", ctypes.c_void_p)]
+                ("dev_lse", ctypes.c_void_p), ("dev_ctl", ctypes.c_void_p)]
 
 
 class hbf_moe(ctypes.Structure):
@@ -558,10 +558,10 @@ def _stride(t, d):
     return t.stride(d) if t.shape[d] > 1 else 0
 
 
-def _zeroed(nbytes, device):
-    """Device bytes, the first 256 zero and seen so by every stream."""
-    t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    t[:256].zero_()
+def _zeroed(nbytes, device, zero=256):
+    """Device bytes, the first `zero` zero and seen so by every stream."""
+    t = torch.empty(max(nbytes, zero), dtype=torch.uint8, device=device)
+    t[:zero].zero_()
     torch.cuda.current_stream(device).synchronize()
     return t
 
@@ -592,7 +592,9 @@ class KvPages:
         self.layers, _, self.pages, self.page_tokens, self.kv_heads, self.head_dim = pool.shape
         self._attn_ws = _Scratch()
         self._attn_sizes, self._attn_bytes, self._layers = None, 0, {}
-        self._attn_status = _zeroed(256, pool.device)[:4].view(torch.int32)
+        words = _zeroed(512, pool.device, 512).view(torch.int32)
+        self._attn_status, self._attn_ctl = words[:1], words[64:]
+        self._attn_at = (self._attn_status.data_ptr(), self._attn_ctl.data_ptr())
         self._kv = None
         if refs is None and tables is None and lens is None:
             return
@@ -739,7 +741,7 @@ class KvPages:
                            prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len,
                            tables.data_ptr() if max_own else None, stride, own, max_own, out.data_ptr(),
                            os[0] if rows > 1 else 0, os[1] if heads > 1 else 0,
-                           None if lse is None else lse.data_ptr())
+                           None if lse is None else lse.data_ptr(), self._attn_at[1])
         sizes = (rows, heads, prefix_len, max_own)
         if sizes != self._attn_sizes:
             b = ctypes.c_size_t()
@@ -748,7 +750,7 @@ class KvPages:
                 return rc
             self._attn_sizes, self._attn_bytes = sizes, b.value
         ws = self._attn_ws.get(self._attn_bytes, self.pool.device, stream)
-        return self._lib.hbf_kv_attention(kv, at, self._attn_status.data_ptr(), ws.data_ptr(), ws.numel(),
+        return self._lib.hbf_kv_attention(kv, at, self._attn_at[0], ws.data_ptr(), ws.numel(),
                                           _raw(stream))
 
     def _layer(self, layer):

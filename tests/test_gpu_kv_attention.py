@@ -306,3 +306,29 @@ def test_another_stream_and_graph(torch):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, run(torch, pool, q2, prefix, 900, tables, ln)[1])
+
+
+# rows, heads, kv heads, dim, prefix, own lengths, page: 1, 2 and 4 queries for each part of the joining workgroup, as
+# many parts as it takes and one more, a head with rows that have nothing, more heads than control words
+JOINED = [(1, 8, 1, 128, 3000, [20], 16), (1, 8, 2, 128, 4096, [300], 16), (1, 8, 2, 64, 24 * 256, [0], 16),
+          (2, 16, 1, 128, 700, [64, 0], 8), (2, 16, 2, 64, 1500, [0, 200], 16), (4, 32, 4, 128, 600, [9, 0, 90, 1], 16),
+          (4, 7, 1, 128, 130, [0, 0, 0, 0], 16), (5, 6, 1, 64, 0, [0, 0, 3, 0, 0], 16), (1, 65, 65, 64, 40, [5], 8)]
+
+
+@pytest.mark.parametrize("case", JOINED, ids=lambda c: "-".join(str(x) for x in c[:5]))
+def test_joined_in_the_launch_or_after_it(torch, case):
+    """Both forms, in turn on one object, from scratch that held anything."""
+    R, Hq, Hk, D, L, lens, pt = case
+    say(f"attention joined {case}")
+    pool, q, prefix, tables, ln = make(torch, R, Hq, Hk, D, L, lens, pt, seed=21)
+    kv, out, lse = run(torch, pool, q, prefix, L, tables, ln)
+    ref = reference(torch, pool[0], q, prefix, L, tables, ln, D ** -0.5)
+    status, words = kv._attn_at
+    for with_words in (True, False, True, True):
+        kv._attn_ws._t.fill_(255)
+        out.fill_(7.0)
+        kv._attn_at = (status, words if with_words else None)
+        assert kv.prefix_attention(0, q, out, prefix, L, tables, ln, lse=lse) == OK
+        check(torch, out, lse, ref, U["bfloat16"], L + max(lens), D)
+        assert not bool(kv._attn_ctl.any())
+    assert kv.get_status() == OK
