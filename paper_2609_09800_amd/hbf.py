@@ -7,6 +7,7 @@ fallback.
 """
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhbf.so")
@@ -81,6 +82,9 @@ class hbf_attention(ctypes.Structure):
                 ("dev_own_len", ctypes.c_void_p), ("max_own", ctypes.c_int32), ("dev_out", ctypes.c_void_p),
                 ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
                 ("dev_lse", ctypes.c_void_p), ("dev_ctl", ctypes.c_void_p)]
+
+
+_pack_attention = struct.Struct("@PqqiifPqPqPiPqqPP").pack_into   # its fields, in order
 
 
 class hbf_moe(ctypes.Structure):
@@ -481,26 +485,31 @@ torch = None   # the module, once a KvPages or MoeLayer is made: their calls las
 
 
 def _import_torch():
-    global torch
+    global torch, _Tensor, _int32, _raw_stream, _device
     import torch
+    _Tensor, _int32 = torch.Tensor, torch.int32
+    _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     return load_library()
 
 
 def _raw(stream):
     """hipStream_t of a torch stream (None -> current stream), as a number.
     (torch.cuda.current_stream() builds an object, which takes 2.8 us.)"""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+    return _raw_stream(_device()) if stream is None else stream.cuda_stream
 
 
 def _is(t, dtype):
     """A contiguous tensor of that type on the GPU: what most calls pass."""
-    return isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()
+    return isinstance(t, _Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()
 
 
 def _ints(t, what, numel=None):
     """_dev for an int32 tensor; its number of elements."""
-    if not _is(t, torch.int32) or numel is not None and t.numel() != numel:
-        _dev(t, what, _I32, numel=numel)
+    if isinstance(t, _Tensor) and t.is_cuda and t.dtype is _int32 and t.is_contiguous():
+        n = t.numel()
+        if numel is None or n == numel:
+            return n
+    _dev(t, what, _I32, numel=numel)
     return t.numel()
 
 
@@ -594,6 +603,7 @@ class KvPages:
         self._attn_sizes, self._attn_bytes, self._layers = None, 0, {}
         words = _zeroed(512, pool.device, 512).view(torch.int32)
         self._attn_status, self._attn_ctl = words[:1], words[64:]
+        self._attn_args = hbf_attention()
         self._attn_at = (self._attn_status.data_ptr(), self._attn_ctl.data_ptr())
         self._kv = None
         if refs is None and tables is None and lens is None:
@@ -674,9 +684,9 @@ class KvPages:
         for t, what in ((k, "k"), (v, "v")):
             if not _is(t, self.pool.dtype):
                 _dev(t, what, (str(self.pool.dtype).replace("torch.", ""),))
-        shape = (n, self.kv_heads, self.head_dim)
-        layers = k.shape[0] if k.dim() == 4 else 1
-        if tuple(k.shape[-3:]) != shape or k.dim() not in (3, 4) or k.shape != v.shape:
+        shape = k.shape
+        layers = shape[0] if len(shape) == 4 else 1
+        if shape[-3:] != (n, self.kv_heads, self.head_dim) or len(shape) not in (3, 4) or v.shape != shape:
             raise HbfError(HBF_EINVAL, f"k, v: shapes {tuple(k.shape)}, {tuple(v.shape)}, expected "
                                        f"[layers, {n}, {self.kv_heads}, {self.head_dim}]")
         return self._lib.hbf_kv_write(d, int(first_layer), layers, k.data_ptr(), v.data_ptr(), slots.data_ptr(),
@@ -736,12 +746,13 @@ class KvPages:
             own = own_lens.data_ptr()
         kv = self._layer(layer)
         qs, os = q.stride(), out.stride()   # (of a dimension of one entry: never taken, but it may be odd)
-        at = hbf_attention(q.data_ptr(), qs[0] if rows > 1 else 0, qs[1] if heads > 1 else 0, rows, heads,
-                           dim ** -0.5 if scale is None else scale,
-                           prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len,
-                           tables.data_ptr() if max_own else None, stride, own, max_own, out.data_ptr(),
-                           os[0] if rows > 1 else 0, os[1] if heads > 1 else 0,
-                           None if lse is None else lse.data_ptr(), self._attn_at[1])
+        at = self._attn_args   # (filled anew by each call, in a third of the time that making one takes)
+        _pack_attention(at, 0, q.data_ptr(), qs[0] if rows > 1 else 0, qs[1] if heads > 1 else 0, rows, heads,
+                        dim ** -0.5 if scale is None else scale,
+                        prefix_pages.data_ptr() if prefix_len > 0 else 0, prefix_len,
+                        tables.data_ptr() if max_own else 0, stride, own, max_own, out.data_ptr(),
+                        os[0] if rows > 1 else 0, os[1] if heads > 1 else 0,
+                        0 if lse is None else lse.data_ptr(), self._attn_at[1] or 0)
         sizes = (rows, heads, prefix_len, max_own)
         if sizes != self._attn_sizes:
             b = ctypes.c_size_t()
