@@ -20,7 +20,7 @@
 //    own;
 //  - sum: a token's products in the order of its choices, so that the result
 //    does not depend on who computed them (in down's launch where that has a
-//    workgroup per unit).
+//    workgroup per unit, or one wave of a workgroup per token tile).
 // Up and down are one scheme: a workgroup goes through consecutive units (a
 // token tile's rows, then the next tile's) with the tile's tokens kept in
 // registers, so that only weights are loaded, the next unit's while this one
@@ -427,6 +427,68 @@ __device__ void store_elem(char *to, float v) {
   *(typename T::elem *)to = (typename T::elem)v;
 }
 
+// Few token tiles: 16 rows of y per workgroup, a tile's products by one wave of
+// it, summed in its LDS.  KS steps of 32 per pass; EXACT: F is one pass and H whole
+// workgroups.
+constexpr int DOWN_FEW_THREADS = 512, DOWN_FEW_WAVES = DOWN_FEW_THREADS / 64, DOWN_FEW_TILES = 2 * DOWN_FEW_WAVES;
+constexpr int DOWN_FEW_PAIRS = 128;
+template <typename T, int KS, bool EXACT>
+__global__ __launch_bounds__(DOWN_FEW_THREADS, 2) void k_moe_down_few(Args a) {
+  __shared__ float part[DOWN_FEW_PAIRS][17];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
+  const int H = a.m.hidden, F = a.m.ffn, r0 = blockIdx.x * 16, k = a.m.topk;
+  const int passes = EXACT ? 1 : (F + KS * 32 - 1) / (KS * 32);
+  Tile tile = a.lists->tile[w];  // (there may be fewer: asked for beside their number)
+  const int n_tiles = a.lists->n_tiles;
+  for (int ti = w; ti < n_tiles; ti += DOWN_FEW_WAVES) {
+    if (ti != w) tile = a.lists->tile[ti];
+    const int n = min(col, (int)tile.count - 1);  // columns past the tokens repeat the last
+    const int pair = a.lists->pair[tile.start + n], r = EXACT ? r0 + col : min(r0 + col, H - 1);
+    const char *wp = (const char *)a.m.dev_down + 2 * ((int64_t)tile.expert * a.m.down_stride + (int64_t)r * F);
+    const int64_t h0 = 2 * (int64_t)(tile.start + n) * F;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int pass = 0; pass < passes; pass++) {
+      u32x4 av[KS];
+#pragma unroll
+      for (int s = 0; s < KS; s++) {
+        const int at = (pass * KS + s) * 32 + kg * 8;
+        av[s] = EXACT || at < F ? load16(wp + 2 * at) : ZERO4;
+      }
+      constexpr int HS = 8;  // steps of h at a time
+#pragma unroll
+      for (int s0 = 0; s0 < KS; s0 += HS) {
+        u32x4 hi[HS], lo[HS];
+#pragma unroll
+        for (int s = 0; s < HS; s++) {
+          const int at = (pass * KS + s0 + s) * 32 + kg * 8;
+          const bool on = EXACT || at < F;
+          hi[s] = on ? load16(a.h_hi + h0 + 2 * at) : ZERO4;
+          lo[s] = on ? load16(a.h_lo + h0 + 2 * at) : ZERO4;
+        }
+#pragma unroll
+        for (int s = 0; s < HS; s++) {
+          acc = T::mfma(av[s0 + s], hi[s], acc);
+          acc = T::mfma(av[s0 + s], lo[s], acc);
+        }
+      }
+    }
+    if (col < tile.count)
+#pragma unroll
+      for (int i = 0; i < 4; i++) part[pair][kg * 4 + i] = acc[i];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.tokens * 16; i += DOWN_FEW_THREADS) {
+    const int t = i >> 4, r = r0 + (i & 15);
+    if (!EXACT && r >= H) continue;
+    float y = 0.f;
+    for (int j = 0; j < k; j++) {
+      const int p = t * k + j;
+      if (used(a, p)) y += a.weights[p] * part[p][i & 15];
+    }
+    ((typename T::elem *)a.y)[t * a.ys + r] = (typename T::elem)y;
+  }
+}
+
 // KS steps of 32 per wave and pass, RB tiles of 16 rows per unit; EXACT: F is one
 // pass and H whole units.
 template <typename T, int KS, int RB, bool EXACT>
@@ -557,13 +619,21 @@ void down(const Args &a, int tiles, hipStream_t s) {
     k_moe_down<T, KS, RB, false><<<groups, THREADS, 0, s>>>(a);
 }
 
+template <typename T, int KS>
+void down_few(const Args &a, hipStream_t s) {
+  const int groups = (a.m.hidden + 15) / 16;
+  if (a.m.ffn == KS * 32 && a.m.hidden % 16 == 0)
+    k_moe_down_few<T, KS, true><<<groups, DOWN_FEW_THREADS, 0, s>>>(a);
+  else
+    k_moe_down_few<T, KS, false><<<groups, DOWN_FEW_THREADS, 0, s>>>(a);
+}
+
 template <typename T>
 hipError_t run(Args a, hipStream_t s) {
   const int pairs = a.tokens * a.m.topk;
   const int tiles = std::min(pairs, a.m.experts + pairs / 16);  // at most
   // A workgroup per unit: summed there, the layer is a launch shorter (one token of the 128-expert layer: 31.8 us, 33.0
-  // with it; 5 tokens of 20 small experts: 14.9, 16.9).  Where workgroups have several units, waiting for each one's
-  // stores would cost more.
+  // with it).  Where workgroups have several units, waiting for each one's stores would cost more.
   a.sum_in_down = (int64_t)tiles * ((a.m.hidden + 31) / 32) <= GROUPS;
   // A workgroup's four waves choose for four tokens side by side, which takes it 3 us, the route's hand-over from
   // workgroup to workgroup 5 (one token of the 128-expert layer: 30.8 us, 32.6 without it).
@@ -577,6 +647,15 @@ hipError_t run(Args a, hipStream_t s) {
   else if (up_steps <= 4) up<T, 4>(a, groups, s);
   else if (up_steps <= 8) up<T, 8>(a, groups, s);
   else up<T, 16>(a, groups, s);
+  // Up to 16 token tiles can be summed in the workgroups of 16 rows, but with few rows these leave CUs idle: 8 tiles of
+  // 4,096 x 1,536 83 us (92 with all units' workgroups and a launch for the sums), 6 of 512 x 256 13.0 (14.0), 15 of
+  // 328 x 104 13.7 (15.0); but 8 of 2,048 x 768 30.9 (30.5), 16 of them 47.5 (44.1).
+  if (tiles <= DOWN_FEW_TILES && pairs <= DOWN_FEW_PAIRS &&
+      (a.m.hidden >= 4096 || (int64_t)tiles * 16 * a.m.ffn <= 65536)) {
+    if (a.m.ffn <= 256) down_few<T, 8>(a, s);
+    else down_few<T, 24>(a, s);
+    return hipGetLastError();
+  }
   const int down_steps = ((a.m.ffn + 31) / 32 + WAVES - 1) / WAVES;
   if (down_steps <= 2) down<T, 2, 2>(a, tiles, s);
   else if (down_steps <= 4) down<T, 4, 2>(a, tiles, s);

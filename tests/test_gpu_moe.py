@@ -131,6 +131,18 @@ def test_layer_against_64_bits(torch, case, dtype):
     assert layer.get_status() == OK
 
 
+# few token tiles: whole passes over the inner axis, part of one, several; rows that end inside a workgroup
+@pytest.mark.parametrize("case", [(1, 16, 8, 4096, 768), (2, 6, 3, 4104, 1544), (3, 9, 5, 24, 264), (16, 2, 1, 40, 768),
+                                  (1, 8, 8, 4096, 256)], ids=lambda c: "-".join(map(str, c)))
+def test_few_token_tiles(torch, case):
+    T, E, k, H, F = case
+    say(f"moe few tiles {case}")
+    x, router, gate_up, down = make(torch, T, E, H, F, "bfloat16", seed=T + H)
+    layer, y, ids, w = run(torch, x, gate_up, down, k, router=router)
+    check(torch, y, reference(torch, x, gate_up, down, k, U["bfloat16"], router=router, ids=ids), ids, w)
+    assert layer.get_status() == OK
+
+
 def test_weights_over_all_experts(torch):
     x, router, gate_up, down = make(torch, 9, 12, 64, 32, "bfloat16", seed=2)
     _, y, ids, w = run(torch, x, gate_up, down, 3, router=router, renorm=False)
