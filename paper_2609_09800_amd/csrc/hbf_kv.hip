@@ -305,7 +305,8 @@ __device__ __forceinline__ void copy_part(const hbf_kv &kv, int plane, int src, 
              (int64_t)(len % kv.page_tokens) * kv.token_bytes, nt);
 }
 
-// PT pages per thread.  copy: the part-full pages too.
+// PT pages per thread.  copy: fork's rows and part-full pages too; else
+// k_kv_fork_copy's many workgroups do both.
 template <bool FORK, int PT>
 __global__ __launch_bounds__(ONE) void k_kv_one(hbf_kv kv, KvWs w, const int32_t *first, const int32_t *second, int n,
                                                 bool copy) {
@@ -353,9 +354,9 @@ __global__ __launch_bounds__(ONE) void k_kv_one(hbf_kv kv, KvWs w, const int32_t
     for (int i = t; i < n; i += ONE) kv.dev_lens[slot[i]] = len[i] + second[i];
     return;
   }
-  for (int i = t / ROW; i < n; i += ONE / ROW) share_row(kv, from[i], len[i], slot[i], t % ROW, ROW);
-  __syncthreads();
   if (copy) {
+    for (int i = t / ROW; i < n; i += ONE / ROW) share_row(kv, from[i], len[i], slot[i], t % ROW, ROW);
+    __syncthreads();
     for (int i = t >> 6; i < n * kv.planes; i += ONE / 64) {  // a wave each
       const int e = i / kv.planes;
       if (off[e + 1] != off[e])
@@ -363,6 +364,7 @@ __global__ __launch_bounds__(ONE) void k_kv_one(hbf_kv kv, KvWs w, const int32_t
                   64);
     }
   } else {
+    __syncthreads();
     for (int i = t; i < n; i += ONE) {
       w.len[i] = len[i];
       w.at[i] = held[i];
@@ -444,10 +446,13 @@ __global__ __launch_bounds__(THREADS) void k_kv_apply(hbf_kv kv, KvWs w, const i
   }
 }
 
-// The part-full pages of a fork: a plane of one child per workgroup.
-__global__ __launch_bounds__(THREADS) void k_kv_fork_copy(hbf_kv kv, KvWs w, const int32_t *parents) {
+// The part-full pages of a fork: a plane of one child per workgroup.  The first
+// plane's shares the row too, if `children` says whose.
+__global__ __launch_bounds__(THREADS) void k_kv_fork_copy(hbf_kv kv, KvWs w, const int32_t *parents,
+                                                          const int32_t *children) {
   if (!w.ctl->go) return;
   const int i = blockIdx.y;
+  if (children && blockIdx.x == 0) share_row(kv, parents[i], w.len[i], children[i], threadIdx.x, THREADS);
   if (w.need_off[i + 1] == w.need_off[i]) return;
   const int len = w.len[i];
   copy_part(kv, blockIdx.x, row_of(kv, kv.dev_tables, parents[i])[len / kv.page_tokens], w.at[i], len, THREADS);
@@ -722,12 +727,12 @@ int tiles_of(int pages) { return (pages + TILE - 1) / TILE; }
 
 template <bool FORK>
 hipError_t plan_apply(const hbf_kv &kv, const KvWs &w, const int32_t *first, const int32_t *second, int n,
-                      bool *copy /* done */, hipStream_t s) {
+                      bool *shared, bool *copy /* done */, hipStream_t s) {
   const int tiles = tiles_of(kv.pages);
   const size_t lds = (size_t)((kv.slots + 31) / 32) * 4;
   if (kv.pages <= SMALL_PAGES && kv.slots <= SMALL_ENTRIES && n <= SMALL_LIST &&
       (!FORK || (int64_t)n * kv.table_cols <= SMALL_ENTRIES)) {
-    *copy = FORK && (uint64_t)n * kv.planes * kv.page_tokens * kv.token_bytes <= SMALL_COPY;
+    *shared = *copy = FORK && (uint64_t)n * kv.planes * kv.page_tokens * kv.token_bytes <= SMALL_COPY;
     if (kv.pages <= ONE * 4)
       k_kv_one<FORK, 4><<<1, ONE, lds, s>>>(kv, w, first, second, n, *copy);
     else
@@ -735,6 +740,7 @@ hipError_t plan_apply(const hbf_kv &kv, const KvWs &w, const int32_t *first, con
     return hipGetLastError();
   }
   *copy = false;
+  *shared = true;
   k_kv_plan<FORK><<<tiles + 1 + (FORK ? n : 0), THREADS, lds, s>>>(kv, w, first, second, n, tiles);
   k_kv_apply<FORK><<<tiles + (FORK ? n : (n + THREADS - 1) / THREADS), THREADS, 0, s>>>(kv, w, first, second, n,
                                                                                         tiles);
@@ -752,18 +758,18 @@ hipError_t launch_kv_extend(const hbf_kv &kv, const int32_t *slots, const int32_
                             hipStream_t s) {
   KvWs w;
   carve(kv.dev_ws, kv.pages, ws_list, &w);
-  bool copied;
-  return plan_apply<false>(kv, w, slots, add, n, &copied, s);
+  bool shared, copied;
+  return plan_apply<false>(kv, w, slots, add, n, &shared, &copied, s);
 }
 
 hipError_t launch_kv_fork(const hbf_kv &kv, const int32_t *parents, const int32_t *children, int n, int ws_list,
                           hipStream_t s) {
   KvWs w;
   carve(kv.dev_ws, kv.pages, ws_list, &w);
-  bool copied;
-  const hipError_t e = plan_apply<true>(kv, w, parents, children, n, &copied, s);
+  bool shared, copied;
+  const hipError_t e = plan_apply<true>(kv, w, parents, children, n, &shared, &copied, s);
   if (e != hipSuccess || copied) return e;
-  k_kv_fork_copy<<<dim3(kv.planes, n), THREADS, 0, s>>>(kv, w, parents);
+  k_kv_fork_copy<<<dim3(kv.planes, n), THREADS, 0, s>>>(kv, w, parents, shared ? nullptr : children);
   return hipGetLastError();
 }
 
