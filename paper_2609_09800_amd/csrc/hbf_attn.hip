@@ -500,42 +500,48 @@ __device__ __forceinline__ int parts_of(const Args &a, int len, bool *bad) {
   const int own = *bad || len == 0 ? 0 : (int)(((uint32_t)len + (uint32_t)a.own_chunk - 1) / (uint32_t)a.own_chunk);
   return a.prefix_splits + own;
 }
-// V of a query's values, from d0 on, from its sums; none: it saw no token.  lead: the one thread that writes lse.
-template <typename T, int V>
-__device__ __forceinline__ void write_out(const Args &a, int row, int head, int d0, const float (&o)[V], float m, float l,
-                                          bool none, bool bad, bool lead) {
+// Four of a query's values, from d0 on, from its sums; none: it saw no token.  lead: the one thread that writes lse.
+template <typename T>
+__device__ __forceinline__ void write_out(const Args &a, int row, int head, int d0, f32x4 o, float m, float l, bool none,
+                                          bool bad, bool lead) {
   if (bad) {
     l = NAN;
     if (a.status && lead) *a.status = HBF_EINVAL;
   }
   none = none && !bad;
-  const float inv = none ? 0.f : 1.f / l;
+  o *= none ? 0.f : 1.f / l;
   typename T::elem *out = (typename T::elem *)a.at.dev_out + row * a.at.out_row_stride + head * a.at.out_head_stride + d0;
-#pragma unroll
-  for (int v = 0; v < V; v++) out[v] = (typename T::elem)(o[v] * inv);
+  *(u32x2 *)out = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
   if (a.at.dev_lse && lead) a.at.dev_lse[(int64_t)row * a.at.heads + head] = none ? -INFINITY : m * LN2 + logf(l);
 }
 
 // The running sums (m, l, o) take U parts in, relative to a first maximum, raised
 // as parts of larger ones come (NaN, a part of bad pages, stays).
-template <int U, int V>
-__device__ __forceinline__ void take_parts(const float2 (&ml)[U], const float (&p)[U][V], float &m, float &l,
-                                           float (&o)[V]) {
+template <int U>
+__device__ __forceinline__ void take_parts(const float2 (&ml)[U], const f32x4 (&p)[U], float &m, float &l, f32x4 &o) {
   float top = m;
 #pragma unroll
   for (int u = 0; u < U; u++) top = fmaxf(top, ml[u].x);
   const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
   m = top;
   l *= alpha;
-#pragma unroll
-  for (int v = 0; v < V; v++) o[v] *= alpha;
+  o *= alpha;
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
     l += f * ml[u].y;
-#pragma unroll
-    for (int v = 0; v < V; v++) o[v] += f * p[u][v];
+    o += f * p[u];
   }
+}
+// Parts n and above, of those that are u0 .. + step * (U - 1), are none.
+template <int U>
+__device__ __forceinline__ void leave_out(float2 (&ml)[U], f32x4 (&p)[U], int u0, int step, int n) {
+#pragma unroll
+  for (int u = 0; u < U; u++)
+    if (u0 + u * step >= n) {
+      ml[u] = make_float2(-INFINITY, 0.f);
+      p[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 }
 
 // All queries of one KV head by one workgroup, from parts that others of the
@@ -569,14 +575,10 @@ __device__ void join_here(const Args &a, int kv_head) {
   for (int r = 0; r < R; r++) {
     bool bad;
     const int n = parts_of(a, len[r], &bad);
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f}, p[U][4];
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      if (u >= n) ml[r][u] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-      for (int v = 0; v < 4; v++) p[u][v] = u < n ? x[r][u][v] : 0.f;
-    }
-    take_parts(ml[r], p, m, l, o);
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    leave_out(ml[r], x[r], 0, 1, n);
+    take_parts(ml[r], x[r], m, l, o);
     const int mm = query(r), row = mm / a.group;
     if (mm <= last) write_out<T>(a, row, kv_head * a.group + mm - row * a.group, d0, o, m, l, n == 0, bad, d0 == 0);
   }
@@ -657,69 +659,54 @@ __global__ __launch_bounds__(THREADS, 2) void k_attn(Args a) {
   end<T, D, HERE>(a, head);
 }
 
-// Join a query's parts by PER waves, each taking every PER-th part.
+// Join a query's parts by PER waves, D / 4 lanes a part.
 template <typename T, int D, int PER>
 __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
-  constexpr int V = D / 64;
-  __shared__ float so[JOIN_WAVES][D], sm[JOIN_WAVES], sl[JOIN_WAVES];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, pw = w % PER;
-  const int64_t qi = (int64_t)blockIdx.x * (JOIN_WAVES / PER) + w / PER;
-  if (PER < JOIN_WAVES && qi >= (int64_t)a.at.rows * a.at.heads) return;
+  constexpr int LANES = D / 4, ALL = JOIN_THREADS / LANES, GROUPS = ALL * PER / JOIN_WAVES;  // groups of lanes: all, a query's
+  constexpr int U = PER == 2 || PER == 1 && D == 128 ? 8 : 4;
+  __shared__ f32x4 so[JOIN_THREADS];
+  __shared__ float2 sml[ALL];
+  const int all = threadIdx.x / LANES, g = all % GROUPS, d0 = threadIdx.x % LANES * 4;
+  const int64_t stride = (int64_t)a.at.rows * a.at.heads;
+  const int64_t mine = (int64_t)blockIdx.x * (JOIN_WAVES / PER) + all / GROUPS, qi = min(mine, stride - 1);
   const int row = (int)(qi / a.at.heads), head = (int)(qi - (int64_t)row * a.at.heads);
   const int len = a.at.dev_own_len ? a.at.dev_own_len[row] : 0;
-  const int64_t stride = (int64_t)a.at.rows * a.at.heads;
-  float m = -INFINITY, l = 0.f, o[V];
-#pragma unroll
-  for (int v = 0; v < V; v++) o[v] = 0.f;
-  constexpr int U = 8;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float2 ml[U];
-  float p[U][V];
+  f32x4 p[U];
   auto load = [&](int i0, int end) {
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int i = i0 + u * PER;
+      const int i = i0 + u * GROUPS;
       ml[u] = i < end ? a.part_ml[i * stride + qi] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-      for (int v = 0; v < V; v++) p[u][v] = i < end ? a.part[(i * stride + qi) * D + lane * V + v] : 0.f;
+      p[u] = i < end ? *(const f32x4 *)(a.part + (i * stride + qi) * D + d0) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
-  load(pw, a.prefix_splits + a.own_splits);  // without waiting for the length: parts that are none are left out below
+  load(g, a.prefix_splits + a.own_splits);  // without waiting for the length: parts that are none are left out below
   bool bad;
   const int n = parts_of(a, len, &bad);
-#pragma unroll
-  for (int u = 0; u < U; u++)
-    if (pw + u * PER >= n) {
-      ml[u] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-      for (int v = 0; v < V; v++) p[u][v] = 0.f;
-    }
-  for (int i0 = pw; i0 < n; i0 += PER * U) {
-    if (i0 != pw) load(i0, n);
+  leave_out(ml, p, g, GROUPS, n);
+  for (int i0 = g; i0 < n; i0 += GROUPS * U) {
+    if (i0 != g) load(i0, n);
     take_parts(ml, p, m, l, o);
   }
-  if (PER > 1) {
+  so[threadIdx.x] = o;
+  if (d0 == 0) sml[all] = make_float2(m, l);
+  __syncthreads();
+  if (g || mine >= stride) return;
+  float2 parts[GROUPS];
+  f32x4 sums[GROUPS];
 #pragma unroll
-    for (int v = 0; v < V; v++) so[w][lane * V + v] = o[v];
-    sm[w] = m;
-    sl[w] = l;
-    __syncthreads();
-    static_assert(PER == 1 || PER == JOIN_WAVES, "a query's waves are a workgroup");
-    if (w) return;
-#pragma unroll
-    for (int i = 1; i < JOIN_WAVES; i++) m = fmaxf(m, sm[i]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    l = 0.f;
-#pragma unroll
-    for (int v = 0; v < V; v++) o[v] = 0.f;
-#pragma unroll
-    for (int i = 0; i < JOIN_WAVES; i++) {
-      const float f = __builtin_amdgcn_exp2f(sm[i] - ref);
-      l += f * sl[i];
-#pragma unroll
-      for (int v = 0; v < V; v++) o[v] += f * so[i][lane * V + v];
-    }
+  for (int i = 0; i < GROUPS; i++) {
+    parts[i] = sml[all + i];
+    sums[i] = so[threadIdx.x + i * LANES];
   }
-  write_out<T>(a, row, head, lane * V, o, m, l, n == 0, bad, lane == 0);
+  m = -INFINITY;
+  l = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+  take_parts(parts, sums, m, l, o);
+  write_out<T>(a, row, head, d0, o, m, l, n == 0, bad, d0 == 0);
 }
 
 // Sizes of a call: how the token axes are cut.
@@ -777,12 +764,15 @@ hipError_t run(const Args &a, hipStream_t s) {
     return hipGetLastError();
   }
   if (blocks > 0) k_attn<T, D, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
-  // a wave per query has the parts of two rounds of loads to wait for at most
+  // A wave per query where its parts are few and the waves fill the card: 512 queries in 9 parts took 16.4 us so, 15.9 by
+  // a workgroup each.
   const uint32_t queries = (uint32_t)a.at.rows * a.at.heads;
-  if (a.prefix_splits + a.own_splits <= 16 && queries >= 512)
+  if (a.prefix_splits + a.own_splits <= 16 && queries > 1024) {
     k_attn_join<T, D, 1><<<(queries + JOIN_WAVES - 1) / JOIN_WAVES, JOIN_THREADS, 0, s>>>(a);
-  else
-    k_attn_join<T, D, JOIN_WAVES><<<queries, JOIN_THREADS, 0, s>>>(a);
+  } else {
+    constexpr int PER = D == 128 ? 4 : 2;  // eight groups of lanes a query
+    k_attn_join<T, D, PER><<<(queries * PER + JOIN_WAVES - 1) / JOIN_WAVES, JOIN_THREADS, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
