@@ -764,7 +764,7 @@ hipError_t run(const Args &a, hipStream_t s) {
     return hipGetLastError();
   }
   if (blocks > 0) k_attn<T, D, false><<<(uint32_t)blocks, THREADS, 0, s>>>(a);
-  // A wave per query where its parts are few and the waves fill the card: 512 queries in 9 parts took 16.4 us so, 15.9 by
+  // A wave per query where its parts are few and the waves fill the card: 512 queries in up to 12 parts took 16.4 us so, 15.9 by
   // a workgroup each.
   const uint32_t queries = (uint32_t)a.at.rows * a.at.heads;
   if (a.prefix_splits + a.own_splits <= 16 && queries > 1024) {
