@@ -28,6 +28,7 @@
 // and take the operands' shape on the way through LDS: loaded straight into it,
 // in pieces of 64 bytes, they pass the CU's vector cache at half its rate
 // (28 bytes a clock measured), which bound both paths.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -60,7 +61,7 @@ struct Args {
   int prefix_blocks;    // workgroups of the prefix, before the own ones
   int own_splits, own_chunk, own_tiles;  // own_tiles: workgroups across a row's query heads of one KV head
   float *part;          // [splits][rows][heads][head_dim] sums of p v
-  float2 *part_ml;      // [splits][rows][heads] maximum (of s log2 e) and sum
+  float2 *part_ml;      // [splits][rows][heads] maximum (of q.k, its sign the scale's) and sum
   int32_t *status;
   uint32_t *ctl;        // a KV head's workgroups that are done, where the last one joins; else null
   uint32_t arrivals;    // workgroups per KV head
@@ -98,7 +99,9 @@ constexpr auto SUM_OP = [](float a, float b) { return a + b; };
 // collects the lane's own.  m is any number that keeps exp2 in range, the same
 // in a column's four lanes: it moves up, to the maximum so far, only where a
 // score passes it by more than LAZY / c (then p <= 2^LAZY otherwise), which
-// few steps do, and then what was summed before is scaled.
+// few steps do, and then what was summed before is scaled.  The difference comes
+// first and the factor after it: at scores of 2^28 the product s c alone is
+// rounded by more than exp2's range.
 constexpr float LAZY = 8.f;
 template <int QT, int U, int DT>
 __device__ __forceinline__ void softmax_step(f32x4 (&s)[QT][U], float c, float (&m)[QT], float (&l)[QT],
@@ -112,7 +115,7 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[QT][U], float c, float (
     for (int u = 0; u < U; u++)
 #pragma unroll
       for (int i = 0; i < 4; i++) mx[q] = fmaxf(mx[q], s[q][u][i]);
-    up |= mx[q] * c > m[q] * c + LAZY;
+    up |= (mx[q] - m[q]) * c > LAZY;  // (none seen, none here: NaN, false)
   }
   if (__any(up)) {
 #pragma unroll
@@ -127,12 +130,12 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[QT][U], float c, float (
   }
 #pragma unroll
   for (int q = 0; q < QT; q++) {
-    const float ref = m[q] == -INFINITY ? 0.f : -m[q] * c;  // nothing seen yet: every p is 0
+    const float ref = m[q] == -INFINITY ? 0.f : m[q];  // nothing seen yet: every p is 0
 #pragma unroll
     for (int u = 0; u < U; u++)
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        s[q][u][i] = __builtin_amdgcn_exp2f(fmaf(s[q][u][i], c, ref));
+        s[q][u][i] = __builtin_amdgcn_exp2f((s[q][u][i] - ref) * c);
         l[q] += s[q][u][i];
       }
   }
@@ -332,7 +335,7 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
 #pragma unroll
   for (int q = 0; q < QT; q++) {
     const float lq = across_rows(l[q], SUM_OP);
-    if (kg == 0) rml[w * 16 + col] = make_float2(m[q] * a.c, lq);
+    if (kg == 0) rml[w * 16 + col] = make_float2(m[q], lq);
 #pragma unroll
     for (int d = 0; d < DT; d++) *(f32x4 *)(ro + (w * 16 + col) * RS + d * 16 + kg * 4) = o[q][d];
     __syncthreads();
@@ -347,7 +350,7 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
       float f[WAVES];
 #pragma unroll
       for (int i = 0; i < WAVES; i++) {
-        f[i] = __builtin_amdgcn_exp2f(rml[i * 16 + n].x - ref);
+        f[i] = __builtin_amdgcn_exp2f((rml[i * 16 + n].x - ref) * a.c);
         sum += f[i] * rml[i * 16 + n].y;
       }
       const int64_t slot = part_slot(a, split, qq);
@@ -488,7 +491,7 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
     const int64_t slot = part_slot(a, split, qq);
 #pragma unroll
     for (int d = 0; d < DT; d++) *(f32x4 *)(a.part + slot * D + d * 16 + kg * 4) = o[q][d];
-    if (kg == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(m[q] * a.c, lq);
+    if (kg == 0) a.part_ml[slot] = any_bad ? make_float2(NAN, NAN) : make_float2(m[q], lq);
   }
 }
 
@@ -512,23 +515,24 @@ __device__ __forceinline__ void write_out(const Args &a, int row, int head, int 
   o *= none ? 0.f : 1.f / l;
   typename T::elem *out = (typename T::elem *)a.at.dev_out + row * a.at.out_row_stride + head * a.at.out_head_stride + d0;
   *(u32x2 *)out = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
-  if (a.at.dev_lse && lead) a.at.dev_lse[(int64_t)row * a.at.heads + head] = none ? -INFINITY : m * LN2 + logf(l);
+  if (a.at.dev_lse && lead) a.at.dev_lse[(int64_t)row * a.at.heads + head] = none ? -INFINITY : m * a.c * LN2 + logf(l);
 }
 
 // The running sums (m, l, o) take U parts in, relative to a first maximum, raised
 // as parts of larger ones come (NaN, a part of bad pages, stays).
 template <int U>
-__device__ __forceinline__ void take_parts(const float2 (&ml)[U], const f32x4 (&p)[U], float &m, float &l, f32x4 &o) {
+__device__ __forceinline__ void take_parts(float c, const float2 (&ml)[U], const f32x4 (&p)[U], float &m, float &l,
+                                           f32x4 &o) {
   float top = m;
 #pragma unroll
   for (int u = 0; u < U; u++) top = fmaxf(top, ml[u].x);
-  const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
+  const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f((m - ref) * c);
   m = top;
   l *= alpha;
   o *= alpha;
 #pragma unroll
   for (int u = 0; u < U; u++) {
-    const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
+    const float f = __builtin_amdgcn_exp2f((ml[u].x - ref) * c);
     l += f * ml[u].y;
     o += f * p[u];
   }
@@ -578,7 +582,7 @@ __device__ void join_here(const Args &a, int kv_head) {
     float m = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     leave_out(ml[r], x[r], 0, 1, n);
-    take_parts(ml[r], x[r], m, l, o);
+    take_parts(a.c, ml[r], x[r], m, l, o);
     const int mm = query(r), row = mm / a.group;
     if (mm <= last) write_out<T>(a, row, kv_head * a.group + mm - row * a.group, d0, o, m, l, n == 0, bad, d0 == 0);
   }
@@ -689,7 +693,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
   leave_out(ml, p, g, GROUPS, n);
   for (int i0 = g; i0 < n; i0 += GROUPS * U) {
     if (i0 != g) load(i0, n);
-    take_parts(ml, p, m, l, o);
+    take_parts(a.c, ml, p, m, l, o);
   }
   so[threadIdx.x] = o;
   if (d0 == 0) sml[all] = make_float2(m, l);
@@ -705,7 +709,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_attn_join(Args a) {
   m = -INFINITY;
   l = 0.f;
   o = f32x4{0.f, 0.f, 0.f, 0.f};
-  take_parts(parts, sums, m, l, o);
+  take_parts(a.c, parts, sums, m, l, o);
   write_out<T>(a, row, head, d0, o, m, l, n == 0, bad, d0 == 0);
 }
 
@@ -715,7 +719,8 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
   a.kv = kv;
   a.at = at;
   a.group = at.heads / kv.kv_heads;
-  a.c = std::max(fabsf(at.scale) * LOG2E, 1e-30f);  // (as flat as 0 is, and -infinity times it stays that)
+  // (1e-30: as flat as 0 is, and -infinity times it stays that)
+  a.c = std::min(std::max(fabsf(at.scale) * LOG2E, 1e-30f), FLT_MAX);
   a.flip = at.scale < 0 ? 0x80008000u : 0;
   // with M = ceil(2^k / d), k = 31 + ceil(log2 d): token * M / 2^k is at most token / 2^31 < 1 / d above token / d
   while ((1 << a.page_shift) < kv.page_tokens) a.page_shift++;
