@@ -517,8 +517,9 @@ int hbf_kv_get_status(const hbf_kv *kv, void *stream);
  *   out = sum_i exp(s[i] - lse) v[i],  lse = log sum_i exp(s[i]).
  * Query head j reads KV head j / (heads / kv_heads).  A row without any token
  * has out 0 and lse -infinity.  What lies behind a length is not looked at.
- * The probabilities are rounded to the call's 16-bit type before they meet V
- * (as fractions of the largest one met so far); nothing else is rounded
+ * The probabilities are rounded to the call's 16-bit type before they meet V,
+ * relative to a maximum that the largest so far passes by at most 2^8; those
+ * below 2^-32 of the largest may count as 0 there.  Nothing else is rounded
  * before the result. */
 typedef struct {
   const void *dev_k, *dev_v;  /* page 0, token 0, head 0; 16-byte aligned */

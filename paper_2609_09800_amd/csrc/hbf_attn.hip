@@ -95,15 +95,23 @@ constexpr auto MAX_OP = [](float a, float b) { return fmaxf(a, b); };
 constexpr auto SUM_OP = [](float a, float b) { return a + b; };
 
 // One step of the running softmax for QT queries per lane (columns): their
-// scores s of U tiles of 16 tokens become probabilities exp2((s - m) c), and l
+// scores s of U tiles of 16 tokens become probabilities exp2((s - m) c + SHIFT), and l
 // collects the lane's own.  m is any number that keeps exp2 in range, the same
 // in a column's four lanes: it moves up, to the maximum so far, only where a
 // score passes it by more than LAZY / c (then p <= 2^LAZY otherwise), which
 // few steps do, and then what was summed before is scaled.  The difference comes
 // first and the factor after it: at scores of 2^28 the product s c alone is
 // rounded by more than exp2's range.
+// p, l and o all carry the same 2^SHIFT.  A half's steps end at 2^-24: at the
+// maximum p is 2^7, at most 2^15 on the way up, and what rounds to 0 is below
+// 2^-32 of the maximum's (without the 2^7, 2^-25: thousands of such tokens, left
+// out of o but not of l, showed).  bfloat16 has float's range.
 constexpr float LAZY = 8.f;
-template <int QT, int U, int DT>
+template <typename T>
+constexpr float SHIFT = 0.f;
+template <>
+constexpr float SHIFT<Fp16> = 7.f;
+template <typename T, int QT, int U, int DT>
 __device__ __forceinline__ void softmax_step(f32x4 (&s)[QT][U], float c, float (&m)[QT], float (&l)[QT],
                                              f32x4 (&o)[QT][DT]) {
   float mx[QT];
@@ -135,7 +143,8 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[QT][U], float c, float (
     for (int u = 0; u < U; u++)
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        s[q][u][i] = __builtin_amdgcn_exp2f((s[q][u][i] - ref) * c);
+        const float d = s[q][u][i] - ref;
+        s[q][u][i] = __builtin_amdgcn_exp2f(SHIFT<T> == 0.f ? d * c : fmaf(d, c, SHIFT<T>));
         l[q] += s[q][u][i];
       }
   }
@@ -311,7 +320,7 @@ __device__ void few(const Args &a, const int32_t *pages, uint32_t t0, uint32_t t
 #pragma unroll
             for (int i = 0; i < 4; i++)
               if (base + u * 16 + kg * 4 + i >= t1) s[q][u][i] = -INFINITY;
-      softmax_step<QT, 2, DT>(s, a.c, m, l, o);
+      softmax_step<T, QT, 2, DT>(s, a.c, m, l, o);
       u32x4 p[QT];
 #pragma unroll
       for (int q = 0; q < QT; q++) p[q] = p_operand<T>(s[q][0], s[q][1]);
@@ -458,7 +467,7 @@ __device__ void many(const Args &a, uint32_t t0, uint32_t t1, int head, int spli
       for (int u = 0; u < U / 2; u++)
         vv2[d & 1][u] = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
     };
-    softmax_step<QT, U, DT>(s, a.c, m, l, o);
+    softmax_step<T, QT, U, DT>(s, a.c, m, l, o);
     u32x4 p[QT][U / 2];
 #pragma unroll
     for (int q = 0; q < QT; q++)
@@ -515,7 +524,7 @@ __device__ __forceinline__ void write_out(const Args &a, int row, int head, int 
   o *= none ? 0.f : 1.f / l;
   typename T::elem *out = (typename T::elem *)a.at.dev_out + row * a.at.out_row_stride + head * a.at.out_head_stride + d0;
   *(u32x2 *)out = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
-  if (a.at.dev_lse && lead) a.at.dev_lse[(int64_t)row * a.at.heads + head] = none ? -INFINITY : m * a.c * LN2 + logf(l);
+  if (a.at.dev_lse && lead) a.at.dev_lse[(int64_t)row * a.at.heads + head] = none ? -INFINITY : m * a.c * LN2 + logf(l * exp2f(-SHIFT<T>));
 }
 
 // The running sums (m, l, o) take U parts in, relative to a first maximum, raised

@@ -4,7 +4,8 @@ Scores here are exact in 32 bits, so that only what follows them is bounded:
 with u the 16-bit type's unit roundoff,
     |o - o64| <= u |o| + (u + 2 ds + (n + 16) 2^-23) sum p |v| + cut,  ds = (D + 8) 2^-23 max |s|,
 where ds bounds the rounding of the exponent (s - m) scale log2 e of scores that
-differ by a few, and is 0 where they are equal or too far apart to count.
+differ by a few, and is 0 where they are equal or too far apart to count; cut is
+what the type's range leaves out.
 """
 import math
 
@@ -51,3 +52,32 @@ def test_scores_of_any_size(torch, dtype, q_value, unit, low, high, shape):
     err = (out.cpu().double() - want).abs()
     assert bool((err <= u * want.abs() + (u + (n + 16) * 2.0 ** -23) * mag).all())
     assert bool(((lse.cpu().double() - want_lse).abs() <= (n + 16) * 2.0 ** -23 + 2.0 ** -22 * want_lse.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("every", [32, 64, 4096])
+@pytest.mark.parametrize("gap", [9.0, 14.0, 17.0, 17.5, 19.0, 21.5, 24.0])
+def test_many_small_probabilities(torch, gap, every, dtype):
+    """Tokens of no value take nearly all of the weight, and the others, each e^-gap of it, make the result.  What is
+    smaller than the type's steps is rounded to one: per token at most 2^-32 of the largest probability."""
+    for R, Hq, Hk, L, lens in ((1, 8, 1, 4099, [77]), (33, 8, 2, 4099, [0, 64, 300] * 11)):
+        say(f"attention small probabilities {gap} {every} {dtype} {R}")
+        pool, q, prefix, tables, ln = make(torch, R, Hq, Hk, 64, L, lens, 16, dtype, seed=33)
+        seen = torch.isfinite(pool[0, 0])
+        value = torch.rand(pool.shape[2:], generator=torch.Generator(device="cuda").manual_seed(34), device="cuda") * 500 + 500
+        pool[0, 0] = torch.where(seen, torch.zeros_like(pool[0, 0]), pool[0, 0])
+        pool[0, 1] = torch.where(seen, value.to(pool.dtype), pool[0, 1])
+        big = torch.arange(0, L, every, device="cuda")
+        page, token = prefix[big // 16].long(), big % 16
+        pool[0, 0, page, token, :, 0] = gap
+        pool[0, 1, page, token] = 0.0
+        q.zero_()
+        q[:, :, 0] = 1.0
+        kv, out, lse = run(torch, pool, q, prefix, L, tables, ln, scale=1.0)
+        assert kv.get_status() == OK
+        want, want_lse, mag, _ = reference(torch, pool[0], q, prefix, L, tables, ln, 1.0)
+        n, u, ds = L + max(lens), U[dtype], 72 * 2.0 ** -23 * gap
+        cut = 2.0 ** -32 * n * 1000 * torch.exp(gap - want_lse)[..., None] + 2.0 ** -25   # (and a half's own last step)
+        err = (out.cpu().double() - want).abs()
+        assert bool((err <= u * want.abs() + (u + 2 * ds + (n + 16) * 2.0 ** -23) * mag + cut).all())
+        assert bool(((lse.cpu().double() - want_lse).abs() <= ds + (n + 16) * 2.0 ** -23 + 2.0 ** -22 * want_lse.abs()).all())
