@@ -105,6 +105,7 @@ __device__ uint32_t block_scan(uint32_t v, uint32_t *total, uint32_t *lds /* [N 
 __device__ bool plan_done(KvCtl *ctl, uint32_t err) {
   __shared__ uint32_t last;
   if (err) atomicOr(&ctl->err, err);
+  stores_done();  // (of every wave: the barrier waits for no memory, the fence below for its own wave's)
   __syncthreads();
   if (threadIdx.x == 0) {
     __threadfence();
