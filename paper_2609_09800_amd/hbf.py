@@ -545,20 +545,36 @@ def _writable(t, what):
     return t
 
 
+class _Blocks:
+    """Device blocks of one object, and the streams that its calls used them
+    on: the allocator gives them away only once those are through with them."""
+
+    def __init__(self, *blocks):
+        self._blocks = blocks
+        self._on = {_raw(None)}   # the allocator knows the stream that they were made on
+
+    def use(self, raw, stream):
+        """A call on `stream` (None: the current one), whose number is `raw`, gets them."""
+        if raw not in self._on:
+            for t in self._blocks:
+                t.record_stream(stream if stream is not None else torch.cuda.current_stream())
+            self._on.add(raw)
+
+
 class _Scratch:
     """Device scratch that grows with the calls' needs."""
 
     def __init__(self):
-        self._t = None
-        self._stream = None   # the one that the block was made on
+        self._t = self._use = None
 
     def get(self, nbytes, device, stream):
         if self._t is None or self._t.numel() < nbytes:
-            # (the allocator takes the old block back once the streams it was used on are through with it)
-            self._t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-            self._stream = torch.cuda.current_stream(device).cuda_stream
-        if _raw(stream) != self._stream:
-            self._t.record_stream(stream if stream is not None else torch.cuda.current_stream(device))
+            # made on the call's stream: what was freed on another one may still be in use there
+            # (the allocator takes the old block back once the streams that it was used on are through with it)
+            with torch.cuda.stream(stream):
+                self._t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+                self._use = _Blocks(self._t)
+        self._use.use(_raw(stream), stream)
         return self._t
 
 
@@ -605,6 +621,7 @@ class KvPages:
         self._attn_status, self._attn_ctl = words[:1], words[64:]
         self._attn_args = hbf_attention()
         self._attn_at = (self._attn_status.data_ptr(), self._attn_ctl.data_ptr())
+        self._attn_words = _Blocks(words)
         self._kv = None
         if refs is None and tables is None and lens is None:
             return
@@ -626,38 +643,45 @@ class KvPages:
         self._ws = _zeroed(b.value, pool.device)
         self._kv.dev_ws = self._ws.data_ptr()
         self._kv_ref = ctypes.byref(self._kv)
+        self._kv_blocks = _Blocks(self._ws)
 
     def _desc(self):
         if self._kv is None:
             raise HbfError(HBF_EINVAL, "this KvPages was made without refs, tables and lens")
         return self._kv_ref
 
+    def _on(self, stream):
+        """A checked call's stream, as a number; the workspace is used on it."""
+        raw = _raw(stream)
+        self._kv_blocks.use(raw, stream)
+        return raw
+
     def extend(self, slots, add, stream=None):
         """Slot slots[i] grows by add[i] tokens (int32 device tensors [n])."""
         d = self._desc()
         n = _ints(slots, "slots")
         _ints(add, "add", n)
-        return self._lib.hbf_kv_extend(d, slots.data_ptr(), add.data_ptr(), n, self.max_list, _raw(stream))
+        return self._lib.hbf_kv_extend(d, slots.data_ptr(), add.data_ptr(), n, self.max_list, self._on(stream))
 
     def fork(self, parents, children, stream=None):
         """The empty slot children[i] gets parents[i]'s tokens (int32 [n])."""
         d = self._desc()
         n = _ints(parents, "parents")
         _ints(children, "children", n)
-        return self._lib.hbf_kv_fork(d, parents.data_ptr(), children.data_ptr(), n, self.max_list, _raw(stream))
+        return self._lib.hbf_kv_fork(d, parents.data_ptr(), children.data_ptr(), n, self.max_list, self._on(stream))
 
     def free(self, slots, stream=None):
         """Slots (int32 [n]) become empty and give their pages back."""
         d = self._desc()
         n = _ints(slots, "slots")
-        return self._lib.hbf_kv_free(d, slots.data_ptr(), n, _raw(stream))
+        return self._lib.hbf_kv_free(d, slots.data_ptr(), n, self._on(stream))
 
     def copy(self, src, dst, stream=None):
         """Pages dst[i] become copies of pages src[i] (int32 [n])."""
         d = self._desc()
         n = _ints(src, "src")
         _ints(dst, "dst", n)
-        return self._lib.hbf_kv_copy(d, src.data_ptr(), dst.data_ptr(), n, _raw(stream))
+        return self._lib.hbf_kv_copy(d, src.data_ptr(), dst.data_ptr(), n, self._on(stream))
 
     def compact(self, remap, tables_out=None, refs_out=None, stream=None):
         """Pages in use move to the front.  remap: int32 [pages]; tables_out
@@ -672,7 +696,7 @@ class KvPages:
                                        or tables_out.stride() != self.tables.stride()):
             raise HbfError(HBF_EINVAL, "tables_out: expected the shape, strides and type of tables")
         return self._lib.hbf_kv_compact(d, remap.data_ptr(), None if tables_out is None else tables_out.data_ptr(),
-                                        None if refs_out is None else refs_out.data_ptr(), _raw(stream))
+                                        None if refs_out is None else refs_out.data_ptr(), self._on(stream))
 
     def write(self, k, v, slots, pos, first_layer=0, stream=None):
         """Token pos[i] of slot slots[i] (int32 [n]) gets k[:, i] and v[:, i]:
@@ -690,7 +714,7 @@ class KvPages:
             raise HbfError(HBF_EINVAL, f"k, v: shapes {tuple(k.shape)}, {tuple(v.shape)}, expected "
                                        f"[layers, {n}, {self.kv_heads}, {self.head_dim}]")
         return self._lib.hbf_kv_write(d, int(first_layer), layers, k.data_ptr(), v.data_ptr(), slots.data_ptr(),
-                                      pos.data_ptr(), n, _raw(stream))
+                                      pos.data_ptr(), n, self._on(stream))
 
     def get_status(self, stream=None):
         """Synchronises; HBF_OK, HBF_EINVAL or HBF_ENOMEM since the last call
@@ -761,8 +785,9 @@ class KvPages:
                 return rc
             self._attn_sizes, self._attn_bytes = sizes, b.value
         ws = self._attn_ws.get(self._attn_bytes, self.pool.device, stream)
-        return self._lib.hbf_kv_attention(kv, at, self._attn_at[0], ws.data_ptr(), ws.numel(),
-                                          _raw(stream))
+        raw = _raw(stream)
+        self._attn_words.use(raw, stream)
+        return self._lib.hbf_kv_attention(kv, at, self._attn_at[0], ws.data_ptr(), ws.numel(), raw)
 
     def _layer(self, layer):
         """The library's description of one layer's pages."""
@@ -806,6 +831,7 @@ class MoeLayer:
                           _stride(gate_up, 0), _stride(down, 0))
         self._ws = _zeroed(self._bytes(max_tokens), gate_up.device)
         self._status = _zeroed(256, gate_up.device)[:4].view(torch.int32)
+        self._blocks = _Blocks(self._ws, self._status)
 
     def _bytes(self, tokens):
         b = ctypes.c_size_t()
@@ -829,9 +855,11 @@ class MoeLayer:
         for t, what, dt in ((ids, "ids", torch.int32), (weights, "weights", torch.float32)):
             if not _is(t, dt) or t.shape != (T, self.topk):
                 _dev(t, what, (str(dt).replace("torch.", ""),), shape=(T, self.topk))
+        raw = _raw(stream)
+        self._blocks.use(raw, stream)
         return self._lib.hbf_moe_layer(self._m, x.data_ptr(), _stride(x, 0), T, ids.data_ptr(), weights.data_ptr(),
                                        y.data_ptr(), _stride(y, 0), self._status.data_ptr(), self._ws.data_ptr(),
-                                       self._ws.numel(), _raw(stream))
+                                       self._ws.numel(), raw)
 
     def get_status(self, stream=None):
         """Synchronises; HBF_OK, or HBF_EINVAL if an id was out of range since
