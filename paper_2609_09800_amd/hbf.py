@@ -562,17 +562,24 @@ class _Blocks:
 
 
 class _Scratch:
-    """Device scratch that grows with the calls' needs."""
+    """Device scratch that grows with the calls' needs.  What it grew out of
+    stays as long as the object: a captured graph may write to it whenever it is
+    replayed.  Each block is at least twice the one before, so that what is kept
+    is less than the last."""
 
     def __init__(self):
         self._t = self._use = None
+        self._kept = []
 
     def get(self, nbytes, device, stream):
         if self._t is None or self._t.numel() < nbytes:
+            least = 256
+            if self._t is not None:
+                self._kept.append(self._t)
+                least = 2 * self._t.numel()
             # made on the call's stream: what was freed on another one may still be in use there
-            # (the allocator takes the old block back once the streams that it was used on are through with it)
             with torch.cuda.stream(stream):
-                self._t = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+                self._t = torch.empty(max(nbytes, least), dtype=torch.uint8, device=device)
                 self._use = _Blocks(self._t)
         self._use.use(_raw(stream), stream)
         return self._t
@@ -605,7 +612,8 @@ class KvPages:
     lens: int32 [slots].  All stay the caller's; a cache that only
     prefix_attention reads needs the pool alone.  max_list: the longest list
     that extend and fork will be given.  Calls on one object must be ordered
-    on one stream."""
+    on one stream, replays of captured ones among them, and the object must
+    live as long as a graph that captured its calls."""
 
     def __init__(self, pool, refs=None, tables=None, lens=None, max_list=1024):
         self._lib = _import_torch()
@@ -811,7 +819,8 @@ class MoeLayer:
     None where the caller chooses.  max_tokens: the most tokens of a call (its
     scratch is allocated here; HBF_ENOWORKSPACE beyond).  All bfloat16 or all float16.  renormalize:
     the chosen experts' weights sum to 1.  Calls on one object must be
-    ordered on one stream."""
+    ordered on one stream, replays of captured ones among them, and the object
+    must live as long as a graph that captured its calls."""
 
     def __init__(self, gate_up, down, topk, router=None, renormalize=True, max_tokens=64):
         self._lib = _import_torch()

@@ -107,3 +107,33 @@ def test_cache_pages(torch):
     assert refs.tolist() == [1, 1, 0, 1, 1, 0, 1, 1] + [0] * 32
     assert bool((pool[:, :, 6, 0] == 1).all()) and bool((pool[:, :, 7, 1] == 1).all())
     assert not any(bool(t.any()) for t in new)
+
+
+def test_a_graph_s_scratch_outlasts_larger_calls(torch):
+    """A captured call's scratch is nobody else's, however much scratch later calls of the object need."""
+    from paper_2609_09800_amd import hbf
+    attention.say("attention captured, then larger")
+    pool, q, prefix, tables, ln = attention.make(torch, 40, 8, 2, 64, 900, [0, 130] * 20, 16, seed=43)
+    small, one = q[:9].contiguous(), torch.empty_like(q[:9])
+    kv = hbf.KvPages(pool)
+    kv.prefix_attention(0, small, one, prefix, 300, tables[:9], ln[:9].contiguous())
+    own9 = ln[:9].contiguous()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        assert kv.prefix_attention(0, small, one, prefix, 300, tables[:9], own9) == OK
+    first = kv._attn_ws._t
+    size = first.numel()
+    del first
+    out = torch.empty_like(q)
+    assert kv.prefix_attention(0, q, out, prefix, 900, tables, ln) == OK
+    assert kv._attn_ws._t.numel() >= 2 * size
+    new = [torch.full((size,), 85, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for i in range(4):
+        small.copy_(q[:9] * (i + 1) / 2)
+        one.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(one, attention.run(torch, pool, small, prefix, 300, tables[:9], own9)[1])
+        assert all(bool((t == 85).all()) for t in new)
+    assert kv.get_status() == OK

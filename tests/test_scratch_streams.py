@@ -4,7 +4,9 @@ to be made on the call's stream, or the allocator has to be told of that stream,
 before the library gets its address.  (What goes wrong otherwise, memory in use
 given to somebody else, depends on timing.)"""
 import contextlib
+import gc
 import types
+import weakref
 
 import pytest
 
@@ -26,7 +28,8 @@ class Block:
     def __init__(self, notes, shape, dtype="int32"):
         self.notes, self.shape, self.dtype, self.device = notes, tuple(shape), dtype, None
         self.streams = [notes.current.cuda_stream]
-        notes.blocks.append(self)
+        notes.made += 1
+        self.address = 4096 * notes.made
 
     def numel(self):
         n = 1
@@ -44,7 +47,7 @@ class Block:
         return strides if d is None else strides[d]
 
     def data_ptr(self):
-        return 4096 * (1 + self.notes.blocks.index(self))
+        return self.address
 
     def is_contiguous(self):
         return True
@@ -61,7 +64,7 @@ class Block:
 
 @pytest.fixture
 def notes(monkeypatch):
-    d = types.SimpleNamespace(blocks=[], current=Stream(1), calls=[], need=300)
+    d = types.SimpleNamespace(made=0, current=Stream(1), calls=[], need=300)
 
     @contextlib.contextmanager
     def on(stream):
@@ -144,3 +147,20 @@ def test_a_moe_layer_s_blocks_are_known_on_every_stream(notes):
     x, y = Block(notes, (3, 64), "bf16"), Block(notes, (3, 64), "bf16")
     ids, weights = Block(notes, (3, 2)), Block(notes, (3, 2), "float32")
     known(notes, lambda: [layer._ws, layer._status], lambda stream: layer.forward(x, y, ids, weights, stream=stream))
+
+
+def test_scratch_that_a_graph_may_have_captured_is_kept(notes):
+    kv, call = attention(notes)
+    blocks, sizes = [], []
+    for length in range(64, 54, -1):   # a little more each time
+        notes.need = notes.need + 100
+        assert call(None, length) == hbf.HBF_OK
+        if not blocks or blocks[-1]() is not kv._attn_ws._t:
+            blocks.append(weakref.ref(kv._attn_ws._t))
+            sizes.append(kv._attn_ws._t.numel())
+    gc.collect()
+    assert len(blocks) > 1 and all(b() is not None for b in blocks)
+    assert sum(sizes[:-1]) < sizes[-1]
+    del kv, call
+    gc.collect()
+    assert all(b() is None for b in blocks)
