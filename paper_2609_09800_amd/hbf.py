@@ -598,6 +598,17 @@ def _zeroed(nbytes, device, zero=256):
     return t
 
 
+def _take_status(word, blocks, stream):
+    """A status word of those blocks, read and cleared in the order of `stream`
+    (None: the current one), so that a later call's error is not cleared with it."""
+    blocks.use(_raw(stream), stream)
+    with torch.cuda.stream(stream):
+        rc = int(word.item())
+        if rc != HBF_OK:
+            word.zero_()
+    return rc
+
+
 def _dtype_code(t):
     import torch
     return HBF_BF16 if t.dtype == torch.bfloat16 else HBF_FP16
@@ -731,11 +742,7 @@ class KvPages:
         if self._kv is not None:
             rc = self._lib.hbf_kv_get_status(self._desc(), _sp(stream))
         if rc == HBF_OK:
-            if stream is not None:
-                stream.synchronize()
-            rc = int(self._attn_status.item())
-            if rc != HBF_OK:
-                self._attn_status.zero_()
+            rc = _take_status(self._attn_status, self._attn_words, stream)
         return rc
 
     def prefix_attention(self, layer, q, out, prefix_pages, prefix_len, tables=None, own_lens=None, lse=None,
@@ -873,12 +880,7 @@ class MoeLayer:
     def get_status(self, stream=None):
         """Synchronises; HBF_OK, or HBF_EINVAL if an id was out of range since
         the last call."""
-        if stream is not None:
-            stream.synchronize()
-        rc = int(self._status.item())
-        if rc != HBF_OK:
-            self._status.zero_()
-        return rc
+        return _take_status(self._status, self._blocks, stream)
 
 
 def refresh_plan(params, blocks, pages_per_block):

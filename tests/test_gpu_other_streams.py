@@ -137,3 +137,24 @@ def test_a_graph_s_scratch_outlasts_larger_calls(torch):
         assert torch.equal(one, attention.run(torch, pool, small, prefix, 300, tables[:9], own9)[1])
         assert all(bool((t == 85).all()) for t in new)
     assert kv.get_status() == OK
+
+
+def test_an_error_after_the_status_was_taken_is_kept(torch):
+    from paper_2609_09800_amd import hbf
+    attention.say("status on another stream")
+    pool, q, prefix, tables, ln = attention.make(torch, 4, 8, 2, 64, 90, [20, 30, 16, 5], 16, seed=44)
+    kv = attention.run(torch, pool, q, prefix, 90, tables, ln)[0]
+    out, bad = torch.empty_like(q), ln.clone()
+    bad[1] = -1
+    x, router, gate_up, down = moe.make(torch, 3, 6, 64, 16, "bfloat16", seed=45)
+    layer = hbf.MoeLayer(gate_up, down, 2)
+    y, w = torch.empty_like(x), torch.ones((3, 2), device="cuda")
+    ids = torch.full((3, 2), 6, dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        assert kv.prefix_attention(0, q, out, prefix, 90, tables, bad, stream=s) == OK
+        assert layer.forward(x, y, ids, w, stream=s) == OK
+        assert kv.get_status(stream=s) == -1 and layer.get_status(stream=s) == -1
+    assert kv.get_status(stream=s) == OK and layer.get_status(stream=s) == OK
+    s.synchronize()

@@ -55,6 +55,13 @@ class Block:
     def record_stream(self, stream):
         self.streams.append(stream.cuda_stream)
 
+    def item(self):   # (waits for the current stream)
+        self.notes.status.append(("read", self.notes.current.cuda_stream))
+        return hbf.HBF_EINVAL
+
+    def zero_(self):
+        self.notes.status.append(("cleared", self.notes.current.cuda_stream))
+
     def view(self, dtype):
         return self
 
@@ -64,7 +71,7 @@ class Block:
 
 @pytest.fixture
 def notes(monkeypatch):
-    d = types.SimpleNamespace(made=0, current=Stream(1), calls=[], need=300)
+    d = types.SimpleNamespace(made=0, current=Stream(1), calls=[], need=300, status=[])
 
     @contextlib.contextmanager
     def on(stream):
@@ -164,3 +171,14 @@ def test_scratch_that_a_graph_may_have_captured_is_kept(notes):
     del kv, call
     gc.collect()
     assert all(b() is None for b in blocks)
+
+
+@pytest.mark.parametrize("given", [None, 6])
+def test_a_status_is_read_and_cleared_in_its_stream_s_order(notes, given):
+    """Cleared on another stream, the word could be cleared after the next call has set it."""
+    kv, _ = attention(notes)
+    layer = hbf.MoeLayer(Block(notes, (4, 32, 64), "bf16"), Block(notes, (4, 64, 16), "bf16"), 2)
+    for thing in (kv, layer):
+        notes.status.clear()
+        assert thing.get_status(stream=Stream(given) if given else None) == hbf.HBF_EINVAL
+        assert notes.status == [("read", given or 1), ("cleared", given or 1)]
