@@ -783,7 +783,7 @@ hipError_t launch_kv_free(const hbf_kv &kv, const int32_t *slots, int n, hipStre
 
 hipError_t launch_kv_copy(const hbf_kv &kv, const int32_t *src, const int32_t *dst, int n, hipStream_t s) {
   const int lds = (kv.pages + 31) / 32 * 4;
-  if (lds > 65536) {
+  if (lds + (int)sizeof(uint32_t) > 65536) {  // (and the word beside the bits)
     const hipError_t e = hipFuncSetAttribute((const void *)k_kv_copy_check,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, KV_MAX_PAGES / 8);
     if (e != hipSuccess) return e;
