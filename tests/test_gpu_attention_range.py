@@ -11,7 +11,7 @@ import math
 
 import pytest
 
-from test_gpu_kv_attention import OK, U, make, reference, run, say
+from test_gpu_kv_attention import EINVAL, OK, U, make, reference, run, say
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,15 @@ def test_many_small_probabilities(torch, gap, every, dtype):
         err = (out.cpu().double() - want).abs()
         assert bool((err <= u * want.abs() + (u + 2 * ds + (n + 16) * 2.0 ** -23) * mag + cut).all())
         assert bool(((lse.cpu().double() - want_lse).abs() <= ds + (n + 16) * 2.0 ** -23 + 2.0 ** -22 * want_lse.abs()).all())
+
+
+def test_scales_at_the_type_s_ends(torch):
+    """Past them: refused.  At them: the highest token alone; all alike."""
+    pool, q, prefix, tables, ln = make(torch, 2, 8, 2, 64, 90, [20, 30], 16, seed=35)
+    kv, out, lse = run(torch, pool, q, prefix, 90, tables, ln)
+    for scale in (1e39, -1e300, math.inf):
+        assert kv.prefix_attention(0, q, out, prefix, 90, tables, ln, scale=scale) == EINVAL
+    for scale in (3.4e38, 1e-44):
+        kv, out, lse = run(torch, pool, q, prefix, 90, tables, ln, scale=scale)
+        want = reference(torch, pool[0], q, prefix, 90, tables, ln, scale)[0]
+        assert bool(((out.cpu().double() - want).abs() <= U["bfloat16"] * (want.abs() + 4)).all())
