@@ -754,7 +754,11 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
     return (int)((tokens + *chunk - 1) / *chunk);
   };
   const double slots = SLOTS / (pre_work + own_work + 1e-9);
-  a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, a.few_q ? 1 : 4, slots * pre_work / pre_groups, &a.prefix_chunk);
+  // max_own is what the table's rows can hold, and a cache's are as wide as a sequence may grow, whatever they hold.
+  // Workgroups past a row's length end at once, but a prefix cut into too few parts is slow: against it, no more
+  // than 1,024 own tokens count.
+  const double pre_slots = SLOTS / (pre_work + std::min(own_work, own_groups * 1024. / own_step) + 1e-9);
+  a.prefix_splits = cut(at.prefix_len, pre_steps, pre_step, a.few_q ? 1 : 4, pre_slots * pre_work / pre_groups, &a.prefix_chunk);
   a.own_splits = cut(at.max_own, own_steps, own_step, 1, slots * own_work / std::max<int64_t>(1, own_groups), &a.own_chunk);
   // A KV head's last workgroup joins its queries where a thread can ask for their parts at once: a launch less, 3.4 us
   // of the host's time and 4 of the GPU's (7 rows of 3 queries over 1,003 tokens: 9.1 us, 11.9 with it; one row of 8
