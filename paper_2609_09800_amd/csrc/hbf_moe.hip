@@ -650,11 +650,15 @@ hipError_t run(Args a, hipStream_t s) {
   else if (up_steps <= 4) up<T, 4>(a, groups, s);
   else if (up_steps <= 8) up<T, 8>(a, groups, s);
   else up<T, 16>(a, groups, s);
-  // Up to 16 token tiles can be summed in the workgroups of 16 rows, but with few rows these leave CUs idle: 8 tiles of
-  // 4,096 x 1,536 83 us (92 with all units' workgroups and a launch for the sums), 6 of 512 x 256 13.0 (14.0), 15 of
-  // 328 x 104 13.7 (15.0); but 8 of 2,048 x 768 30.9 (30.5), 16 of them 47.5 (44.1).
+  // Up to 16 token tiles can be summed in the workgroups of 16 rows, but with few rows these leave CUs idle, and above 256
+  // channels a wave's weights are not one pass of its registers.  In us, so and by all units' workgroups:
+  //   rows x channels: 6 tiles     8 tiles     16 tiles       rows x channels: 6 tiles     8 tiles     16 tiles
+  //   512 x 256        13.3 13.8   15.9 17.1   19.6 19.6      2,048 x 256      16.3 17.9   19.9 22.8   24.9 26.2
+  //   512 x 512        16.0 15.0   19.9 18.5   25.5 21.3      2,048 x 512      20.8 21.4   25.4 26.1   35.8 33.8
+  //   1,024 x 256      14.2 15.0   17.5 18.9   21.4 22.0      2,048 x 768      23.0 24.4   30.4 30.1   47.5 44.1
+  //   1,024 x 512      18.0 16.9   22.1 21.3   28.6 25.1      4,096 x 1,536                83   92
   if (tiles <= DOWN_FEW_TILES && pairs <= DOWN_FEW_PAIRS &&
-      (a.m.hidden >= 4096 || (int64_t)tiles * 16 * a.m.ffn <= 65536)) {
+      (a.m.ffn <= 256 || a.m.hidden >= 4096 || (a.m.hidden >= 2048 && (int64_t)tiles * 16 * a.m.ffn <= 65536))) {
     if (a.m.ffn <= 256) down_few<T, 8>(a, s);
     else down_few<T, 24>(a, s);
     return hipGetLastError();
