@@ -540,7 +540,8 @@ typedef struct {
   const int32_t *dev_tables;  /* own pages of row r at r * table_stride; NULL where no row has own tokens */
   int64_t table_stride;
   const int32_t *dev_own_len; /* [rows] own tokens, 0 .. max_own; may be NULL if max_own is 0 */
-  int32_t max_own;            /* 0 without own tokens; rows of the table hold that many */
+  int32_t max_own;            /* 0 without own tokens; rows of the table hold that many.  Own tokens are cut into parts
+                                 for rows of this length: best the longest own_len, where the host knows it */
   void *dev_out;              /* [rows][heads][head_dim], strides as q's, 16-byte aligned */
   int64_t out_row_stride, out_head_stride;
   float *dev_lse;             /* [rows][heads], or NULL */

@@ -751,8 +751,11 @@ class KvPages:
         first prefix_len tokens of the pages prefix_pages (int32; None without
         prefix), shared by all rows, and each row's own_lens[r] tokens of the
         pages tables[r] (int32 [rows, entries], rows may be strided; e.g. the
-        columns behind the prefix of a cache's table).  out: as q; lse: float32
-        [rows, heads] or None; scale: 1 / sqrt(head_dim) if None."""
+        columns behind the prefix of a cache's table).  Work is cut for rows
+        that fill their columns: where the host knows that all of them are
+        shorter, it should pass no more columns than the longest needs (a
+        slice).  out: as q; lse: float32 [rows, heads] or None; scale:
+        1 / sqrt(head_dim) if None."""
         dtype = self.pool.dtype
         if not 0 <= layer < self.layers:
             raise HbfError(HBF_EINVAL, f"layer {layer}, the pool has {self.layers}")
