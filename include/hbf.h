@@ -566,7 +566,8 @@ int hbf_kv_attention(const hbf_kv_layer *kv, const hbf_attention *at, int32_t *d
  *   by the chosen ones' sum;
  *   h = silu(gate_e x) * (up_e x),  y = sum_j weight_j down_ej h.
  * h is held as the sum of two 16-bit words (in HBF_FP16 its magnitude is
- * limited to 65504 as an activation of that type is: beyond, infinity).
+ * limited to 65504 as an activation of that type is: beyond, infinity; and an
+ * infinite weight of down may give NaN where the sum is infinite).
  * Without a router the caller gives the choices: ids[t][j] an expert or -1
  * (none), and their weights; one expert may be named twice.  A logit that is
  * NaN counts as the lowest. */
