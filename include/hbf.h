@@ -560,6 +560,122 @@ int hbf_kv_attention_workspace_bytes(const hbf_kv_layer *kv, const hbf_attention
 int hbf_kv_attention(const hbf_kv_layer *kv, const hbf_attention *at, int32_t *dev_status, void *dev_ws,
                      size_t ws_bytes, void *stream);
 
+/* New tokens of one layer enter the cache.  Each head of q and k is divided by
+ * its root mean square and multiplied by the weights (where they are given):
+ *   y = x / sqrt(mean(x^2) + eps) * weight,
+ * then its pair i < pairs turns by the angle a = position * freqs[i]:
+ *   (y1, y2) -> (y1 cos a - y2 sin a, y1 sin a + y2 cos a),
+ * where pair i is the values i and i + pairs, or 2i and 2i + 1 with
+ * HBF_ROT_PAIRS; values from 2 pairs on stay.  v is not changed.  q goes to
+ * dev_q_out (which may be dev_q with its strides), k and v to the cache as in
+ * hbf_kv_write.  Angles are computed in 64 bits and the rest in 32; each
+ * result is rounded once. */
+#define HBF_ROT_PAIRS 1u
+typedef struct {
+  const void *dev_q, *dev_k, *dev_v;  /* [n][heads][head_dim], and [n][kv_heads][head_dim] twice: 16-byte aligned, strides
+                                         in elements, multiples of 8 */
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  void *dev_q_out;            /* as dev_q */
+  int64_t out_row_stride, out_head_stride;
+  int32_t n;                  /* 0 .. 2^20 */
+  int32_t heads, kv_heads;    /* 1 .. 1024 each */
+  int32_t head_dim;           /* 64 or 128; the cache's token_bytes are 2 * kv_heads * head_dim */
+  uint32_t dtype, flags;      /* HBF_BF16 / HBF_FP16; HBF_ROT_* */
+  const void *dev_q_weight, *dev_k_weight; /* [head_dim], 16-byte aligned; NULL: that norm is left out */
+  float eps;                  /* finite, >= 0 */
+  int32_t pairs;              /* 0 .. head_dim / 2, a multiple of 8 */
+  const double *dev_freqs;    /* [pairs] radians per position; may be NULL if pairs is 0 */
+  const int32_t *dev_slots, *dev_pos; /* [n] the token's slot and its place there */
+  const int32_t *dev_positions; /* [n] any values; NULL: dev_pos */
+} hbf_new_tokens;
+
+/* An entry whose slot, place (0 <= pos < length) or page is out of range is
+ * left out of the cache (HBF_EINVAL, sticky); its q_out is written.  Two
+ * entries of one token: undefined. */
+int hbf_kv_write_rotated(const hbf_kv *kv, int layer, const hbf_new_tokens *nt, void *stream);
+
+/* Attention of new tokens, one or a chunk of a prompt per row, over cache pages
+ * of one layer.  Row i's new tokens are queries starts[i] .. starts[i + 1] - 1
+ * and the last of slot slots[i]'s tokens, whose K and V are there already.
+ * With length L and n new ones, the t-th is at position p = L - n + t and sees
+ * the tokens j <= p; with a window only those of j > p - window, and those of
+ * j < sinks.  A query at p < 0 sees none: out 0, lse -infinity.  Scores,
+ * heads and roundings are as in hbf_kv_attention.  What a query does not see
+ * does not reach its result, infinities and NaN included.  Queries outside
+ * every row are left as they were.  A slot may be named by several rows.
+ * With dev_weights, weights[slot][KV head][j] grows by the sum of
+ * exp(s[j] - lse) over the row's queries that see j and the KV head's query
+ * heads, in 32 bits and an order that does not change; what no query sees is
+ * left as it was. */
+typedef struct {
+  const void *dev_q;          /* [tokens][heads][head_dim], 16-byte aligned, strides in elements, multiples of 8 */
+  int64_t q_row_stride, q_head_stride;
+  int32_t tokens;             /* 0 .. 2^20, tokens * heads <= 2^24 */
+  int32_t rows;               /* 0 .. 65535 */
+  int32_t heads;              /* a multiple of kv_heads, up to 1024 */
+  float scale;                /* finite */
+  const int32_t *dev_slots;   /* [rows] */
+  const int32_t *dev_starts;  /* [rows + 1], not decreasing, in [0, tokens] */
+  int32_t window, sinks;      /* >= 0; window 0: none (then sinks say nothing) */
+  void *dev_out;              /* [tokens][heads][head_dim], as dev_q, not overlapping it */
+  int64_t out_row_stride, out_head_stride;
+  float *dev_lse;             /* [tokens][heads], or NULL */
+  float *dev_weights;         /* slot s, KV head h at s * weights_slot_stride + h * weights_head_stride; or NULL */
+  int64_t weights_slot_stride, weights_head_stride;  /* in elements, >= 0 */
+  int32_t weights_tokens;     /* what a row of weights holds */
+  uint32_t *dev_ctl;          /* HBF_CHUNK_CTL_WORDS words, zero before the first call and kept by the calls from then on;
+                                 calls that share them must be ordered on one stream.  NULL: few long rows are not cut
+                                 into parts */
+} hbf_chunk;
+#define HBF_CHUNK_CTL_WORDS 2048u
+
+/* Device scratch of a call, in bytes (only sizes are looked at). */
+int hbf_kv_chunk_workspace_bytes(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch, size_t *bytes);
+
+/* The tables and lengths are the cache's; its counts, pool and workspace are
+ * not looked at.  dev_status (device, nullable): HBF_EINVAL is stored there if
+ * a slot or a length (longer than a row of weights, too) is out of range: the
+ * row's out and lse are NaN and its weights stay; if a page id that is read is
+ * outside [0, pages): the queries that see the page are NaN, other queries of the
+ * row may be, and such queries add nothing to weights; or if starts are not as
+ * above: outs, lse and weights are then unspecified.  Left as it was
+ * otherwise.  dev_ws: 256-byte aligned; a call's contents need not be kept. */
+int hbf_kv_chunk_attention(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch, int32_t *dev_status,
+                           void *dev_ws, size_t ws_bytes, void *stream);
+
+/* Sequences are cut down to their heaviest tokens.  Slot slots[i] of L tokens
+ * keeps min(L, keep[i]) of them, in every layer and KV head its own choice: the
+ * first `sinks`, the last `recent`, and of those between the ones with the
+ * largest weights (ties: the lowest position; NaN counts as the lowest).  With
+ * m = keep - recent, chosen tokens before m stay where they are, those from m
+ * on move, in order, to the places that are free before it, in order: the fewest moves.
+ * The last `recent` follow from m on, in their order.  The slot's length becomes
+ * keep, its pages behind that lose one count and their entries become -1.
+ * dev_kept[layer][i][head][j] receives the old position of the token that is at
+ * j now, -1 from the new length on.  weights follow their tokens; behind the new
+ * length, up to the old one, they become 0.  A slot of at most keep tokens
+ * stays as it is. */
+typedef struct {
+  const int32_t *dev_slots, *dev_keep; /* [n] */
+  int32_t n;                  /* 0 .. 65535; layers * n * kv_heads <= 2^22 */
+  int32_t kv_heads;           /* 1 .. 1024, each token_bytes / kv_heads, a multiple of 16 */
+  int32_t sinks, recent;      /* >= 0 */
+  const float *dev_weights;   /* layer l, slot s, head h at l * layer_stride + s * slot_stride + h * head_stride */
+  int64_t layer_stride, slot_stride, head_stride; /* in elements, >= 0 */
+  int32_t weights_tokens;     /* what a row of weights holds */
+  float *dev_weights_out;     /* as dev_weights, rows of listed slots up to their old length; NULL: in place */
+  int32_t *dev_kept;          /* [planes / 2][n][kv_heads][max_keep] */
+  int32_t max_keep;           /* 0 .. 2^24; layers * n * kv_heads * max_keep <= 2^40 */
+} hbf_eviction;
+
+/* Checks everything first; refused (HBF_EINVAL, sticky; nothing changes but
+ * dev_kept, which is unspecified then): a slot out of range or listed twice, a
+ * length out of range or longer than a row of weights, keep outside
+ * [0, max_keep], a slot to cut with keep < sinks + recent, an entry in use
+ * that is no page or a free one, a page that would be written, those of the
+ * places [sinks, keep) of a slot to cut, that others hold too. */
+int hbf_kv_evict(const hbf_kv *kv, const hbf_eviction *ev, void *stream);
+
 /* A mixture-of-experts layer for a few tokens, all of it:
  *   logits = x . router[e]  (fp32), the topk largest (ties: the lowest index),
  *   their weights: the softmax over all experts, with HBF_MOE_RENORM divided

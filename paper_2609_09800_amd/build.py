@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhbf.so")
 SOURCES = ["hbf_api.cpp", "hbf_kernels.hip", "hbf_gemv.hip", "hbf_cache.hip", "hbf_blocking.hip", "hbf_vmem.hip",
-           "hbf_layers.hip", "hbf_small.hip", "hbf_cache_chunk.hip", "hbf_ops_api.cpp", "hbf_kv.hip", "hbf_attn.hip", "hbf_moe.hip"]
+           "hbf_layers.hip", "hbf_small.hip", "hbf_cache_chunk.hip", "hbf_ops_api.cpp", "hbf_kv.hip", "hbf_attn.hip", "hbf_moe.hip",
+           "hbf_rotate.hip", "hbf_chunk.hip", "hbf_evict.hip"]
 ARCH = "gfx950"
 
 FLAGS = [

@@ -1,5 +1,5 @@
 // Declarations shared by the decode-layer operators (hbf_kv.hip, hbf_attn.hip,
-// hbf_moe.hip) and their host side (hbf_ops_api.cpp).
+// hbf_chunk.hip, hbf_evict.hip, hbf_rotate.hip, hbf_moe.hip) and their host side (hbf_ops_api.cpp).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -39,6 +39,12 @@ hipError_t launch_kv_write(const hbf_kv &kv, int layer0, int layers, const void 
 constexpr int ATTN_CTL_WORDS = 64;
 size_t attn_ws_bytes(const hbf_kv_layer &kv, const hbf_attention &at);
 hipError_t launch_attn(const hbf_kv_layer &kv, const hbf_attention &at, int32_t *status, void *ws, hipStream_t s);
+
+hipError_t launch_kv_write_rotated(const hbf_kv &kv, int layer, const hbf_new_tokens &nt, hipStream_t s);
+size_t chunk_ws_bytes(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch);
+hipError_t launch_chunk(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch, int32_t *status, void *ws,
+                        hipStream_t s);
+hipError_t launch_kv_evict(const hbf_kv &kv, const hbf_eviction &ev, hipStream_t s);
 
 constexpr int MOE_MAX_TOKENS = 128, MOE_MAX_TOPK = 32, MOE_MAX_EXPERTS = 1024, MOE_MAX_PAIRS = 2048;
 size_t moe_ws_bytes(const hbf_moe &m, int tokens);

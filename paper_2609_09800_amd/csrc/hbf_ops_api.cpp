@@ -41,8 +41,8 @@ int check_list(const void *a, const void *b, int n) {
   return HBF_OK;
 }
 
-int check_attention(const hbf_kv_layer *kv, const hbf_attention *at) {
-  if (!kv || !at) return HBF_EINVAL;
+// A layer's pages, as attention reads them.
+int check_layer(const hbf_kv_layer *kv) {
   if (!dtype_ok(kv->dtype) || (kv->head_dim != 64 && kv->head_dim != 128) || kv->kv_heads < 1 ||
       kv->kv_heads > 1024 || kv->pages < 1 || kv->pages > KV_MAX_PAGES || kv->page_tokens < 1 ||
       kv->page_tokens > 65536)
@@ -50,6 +50,13 @@ int check_attention(const hbf_kv_layer *kv, const hbf_attention *at) {
   if (kv->page_stride < 0 || kv->token_stride < 0 || kv->head_stride < 0 || kv->page_stride % 8 ||
       kv->token_stride % 8 || kv->head_stride % 8)
     return HBF_EINVAL;
+  return HBF_OK;
+}
+
+int check_attention(const hbf_kv_layer *kv, const hbf_attention *at) {
+  if (!kv || !at) return HBF_EINVAL;
+  const int rc = check_layer(kv);
+  if (rc) return rc;
   if (at->rows < 0 || at->rows > 65535 || at->heads < kv->kv_heads || at->heads > 1024 ||
       at->heads % kv->kv_heads || (int64_t)at->rows * at->heads > 1 << 22)
     return HBF_EINVAL;
@@ -57,6 +64,36 @@ int check_attention(const hbf_kv_layer *kv, const hbf_attention *at) {
   if (at->prefix_len < 0 || at->prefix_len > INT32_MAX || at->max_own < 0) return HBF_EINVAL;
   if (at->q_row_stride % 8 || at->q_head_stride % 8 || at->out_row_stride % 8 || at->out_head_stride % 8)
     return HBF_EINVAL;
+  return HBF_OK;
+}
+
+int check_chunk(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch) {
+  if (!layer || !ch) return HBF_EINVAL;
+  int rc = check_kv_sizes(kv);
+  if (rc || (rc = check_layer(layer))) return rc;
+  if (kv->page_tokens != layer->page_tokens) return HBF_EINVAL;
+  if (ch->tokens < 0 || ch->tokens > 1 << 20 || ch->rows < 0 || ch->rows > 65535 || ch->heads < layer->kv_heads ||
+      ch->heads > 1024 || ch->heads % layer->kv_heads || (int64_t)ch->tokens * ch->heads > 1 << 24)
+    return HBF_EINVAL;
+  if (!isfinite(ch->scale) || ch->window < 0 || ch->sinks < 0) return HBF_EINVAL;
+  if (ch->q_row_stride % 8 || ch->q_head_stride % 8 || ch->out_row_stride % 8 || ch->out_head_stride % 8)
+    return HBF_EINVAL;
+  if (ch->weights_slot_stride < 0 || ch->weights_head_stride < 0 || ch->weights_tokens < 0) return HBF_EINVAL;
+  return HBF_OK;
+}
+
+int check_new_tokens(const hbf_kv *kv, const hbf_new_tokens *nt) {
+  if (!nt || !dtype_ok(nt->dtype) || (nt->flags & ~HBF_ROT_PAIRS)) return HBF_EINVAL;
+  if (nt->head_dim != 64 && nt->head_dim != 128) return HBF_EINVAL;
+  if (nt->n < 0 || nt->n > 1 << 20 || nt->heads < 1 || nt->heads > 1024 || nt->kv_heads < 1 || nt->kv_heads > 1024 ||
+      kv->token_bytes != (uint64_t)nt->kv_heads * nt->head_dim * 2)
+    return HBF_EINVAL;
+  if (!isfinite(nt->eps) || nt->eps < 0 || nt->pairs < 0 || nt->pairs > nt->head_dim / 2 || nt->pairs % 8)
+    return HBF_EINVAL;
+  const int64_t strides[] = {nt->q_row_stride, nt->q_head_stride, nt->k_row_stride,   nt->k_head_stride,
+                             nt->v_row_stride, nt->v_head_stride, nt->out_row_stride, nt->out_head_stride};
+  for (int64_t s : strides)
+    if (s % 8) return HBF_EINVAL;
   return HBF_OK;
 }
 
@@ -166,6 +203,62 @@ int hbf_kv_attention(const hbf_kv_layer *kv, const hbf_attention *at, int32_t *s
   if (!ws || !aligned(ws, 256) || !aligned(at->dev_ctl, 4)) return HBF_EINVAL;
   if (ws_bytes < attn_ws_bytes(*kv, *at)) return HBF_ENOWORKSPACE;
   return status_of(launch_attn(*kv, *at, status, ws, (hipStream_t)stream));
+}
+
+int hbf_kv_write_rotated(const hbf_kv *kv, int layer, const hbf_new_tokens *nt, void *stream) {
+  int rc = check_kv(kv);
+  if (rc || (rc = check_new_tokens(kv, nt))) return rc;
+  if (layer < 0 || layer >= kv->planes / 2) return HBF_EINVAL;
+  if (nt->n == 0) return HBF_OK;
+  if (!nt->dev_q || !nt->dev_k || !nt->dev_v || !nt->dev_q_out || !aligned(nt->dev_q, 16) || !aligned(nt->dev_k, 16) ||
+      !aligned(nt->dev_v, 16) || !aligned(nt->dev_q_out, 16) || !aligned(nt->dev_q_weight, 16) ||
+      !aligned(nt->dev_k_weight, 16))
+    return HBF_EINVAL;
+  if ((nt->pairs > 0 && !nt->dev_freqs) || !aligned(nt->dev_freqs, 8) || !nt->dev_slots || !nt->dev_pos ||
+      !aligned(nt->dev_slots, 4) || !aligned(nt->dev_pos, 4) || !aligned(nt->dev_positions, 4))
+    return HBF_EINVAL;
+  return status_of(launch_kv_write_rotated(*kv, layer, *nt, (hipStream_t)stream));
+}
+
+int hbf_kv_chunk_workspace_bytes(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch, size_t *bytes) {
+  const int rc = check_chunk(kv, layer, ch);
+  if (rc) return rc;
+  if (!bytes) return HBF_EINVAL;
+  *bytes = chunk_ws_bytes(*kv, *layer, *ch);
+  return HBF_OK;
+}
+
+int hbf_kv_chunk_attention(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch, int32_t *status, void *ws,
+                           size_t ws_bytes, void *stream) {
+  const int rc = check_chunk(kv, layer, ch);
+  if (rc) return rc;
+  if (ch->rows == 0 || ch->tokens == 0) return HBF_OK;
+  if (!kv->dev_tables || !kv->dev_lens || !aligned(kv->dev_tables, 4) || !aligned(kv->dev_lens, 4)) return HBF_EINVAL;
+  if (!layer->dev_k || !layer->dev_v || !ch->dev_q || !ch->dev_out || !aligned(layer->dev_k, 16) ||
+      !aligned(layer->dev_v, 16) || !aligned(ch->dev_q, 16) || !aligned(ch->dev_out, 16) || !aligned(ch->dev_lse, 4) ||
+      !aligned(ch->dev_weights, 4) || !aligned(ch->dev_ctl, 4) || !aligned(status, 4))
+    return HBF_EINVAL;
+  if (!ch->dev_slots || !ch->dev_starts || !aligned(ch->dev_slots, 4) || !aligned(ch->dev_starts, 4)) return HBF_EINVAL;
+  if (!ws || !aligned(ws, 256)) return HBF_EINVAL;
+  if (ws_bytes < chunk_ws_bytes(*kv, *layer, *ch)) return HBF_ENOWORKSPACE;
+  return status_of(launch_chunk(*kv, *layer, *ch, status, ws, (hipStream_t)stream));
+}
+
+int hbf_kv_evict(const hbf_kv *kv, const hbf_eviction *ev, void *stream) {
+  const int rc = check_kv(kv);
+  if (rc) return rc;
+  if (!ev || kv->planes % 2 || ev->n < 0 || ev->n > KV_MAX_LIST || ev->kv_heads < 1 || ev->kv_heads > 1024 ||
+      kv->token_bytes % (16 * (uint64_t)ev->kv_heads) || ev->sinks < 0 || ev->recent < 0 || ev->weights_tokens < 0 ||
+      ev->max_keep < 0 || ev->max_keep > 1 << 24 || ev->layer_stride < 0 || ev->slot_stride < 0 || ev->head_stride < 0)
+    return HBF_EINVAL;
+  const int64_t groups = (int64_t)(kv->planes / 2) * ev->n * ev->kv_heads;
+  if (groups > 1 << 22 || groups * ev->max_keep > (int64_t)1 << 40) return HBF_EINVAL;
+  if (ev->n == 0) return HBF_OK;
+  if (!ev->dev_slots || !ev->dev_keep || !ev->dev_weights || (ev->max_keep > 0 && !ev->dev_kept) ||
+      !aligned(ev->dev_slots, 4) || !aligned(ev->dev_keep, 4) || !aligned(ev->dev_weights, 4) ||
+      !aligned(ev->dev_weights_out, 4) || !aligned(ev->dev_kept, 4))
+    return HBF_EINVAL;
+  return status_of(launch_kv_evict(*kv, *ev, (hipStream_t)stream));
 }
 
 int hbf_moe_workspace_bytes(const hbf_moe *moe, int tokens, size_t *bytes) {

@@ -39,12 +39,15 @@ EXPORTED = [
     "hbf_kv_workspace_bytes", "hbf_kv_extend", "hbf_kv_fork", "hbf_kv_free", "hbf_kv_copy", "hbf_kv_compact",
     "hbf_kv_write", "hbf_kv_get_status", "hbf_kv_attention_workspace_bytes", "hbf_kv_attention",
     "hbf_moe_workspace_bytes", "hbf_moe_layer",
+    "hbf_kv_write_rotated", "hbf_kv_chunk_workspace_bytes", "hbf_kv_chunk_attention", "hbf_kv_evict",
 ]
 HBF_NOALLOC_SCRATCH_BYTES = 64 << 20
 REFRESH_PENDING = -1
 HBF_BF16 = 0
 HBF_FP16 = 1
 HBF_MOE_RENORM = 1
+HBF_ROT_PAIRS = 1
+HBF_CHUNK_CTL_WORDS = 2048
 
 
 class hbf_params(ctypes.Structure):
@@ -85,6 +88,42 @@ class hbf_attention(ctypes.Structure):
 
 
 _pack_attention = struct.Struct("@PqqiifPqPqPiPqqPP").pack_into   # its fields, in order
+
+
+class hbf_new_tokens(ctypes.Structure):
+    _fields_ = [("dev_q", ctypes.c_void_p), ("dev_k", ctypes.c_void_p), ("dev_v", ctypes.c_void_p),
+                ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("k_row_stride", ctypes.c_int64),
+                ("k_head_stride", ctypes.c_int64), ("v_row_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+                ("dev_q_out", ctypes.c_void_p), ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("n", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+                ("dev_q_weight", ctypes.c_void_p), ("dev_k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("pairs", ctypes.c_int32), ("dev_freqs", ctypes.c_void_p), ("dev_slots", ctypes.c_void_p),
+                ("dev_pos", ctypes.c_void_p), ("dev_positions", ctypes.c_void_p)]
+
+
+_pack_new_tokens = struct.Struct("@PPPqqqqqqPqqiiiiIIPPfiPPPP").pack_into
+
+
+class hbf_chunk(ctypes.Structure):
+    _fields_ = [("dev_q", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("tokens", ctypes.c_int32), ("rows", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("dev_slots", ctypes.c_void_p), ("dev_starts", ctypes.c_void_p),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("dev_out", ctypes.c_void_p),
+                ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64), ("dev_lse", ctypes.c_void_p),
+                ("dev_weights", ctypes.c_void_p), ("weights_slot_stride", ctypes.c_int64),
+                ("weights_head_stride", ctypes.c_int64), ("weights_tokens", ctypes.c_int32), ("dev_ctl", ctypes.c_void_p)]
+
+
+_pack_chunk = struct.Struct("@PqqiiifPPiiPqqPPqqiP").pack_into
+
+
+class hbf_eviction(ctypes.Structure):
+    _fields_ = [("dev_slots", ctypes.c_void_p), ("dev_keep", ctypes.c_void_p), ("n", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("dev_weights", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("weights_tokens", ctypes.c_int32),
+                ("dev_weights_out", ctypes.c_void_p), ("dev_kept", ctypes.c_void_p), ("max_keep", ctypes.c_int32)]
 
 
 class hbf_moe(ctypes.Structure):
@@ -152,6 +191,12 @@ def load_library(path=LIB_PATH):
                                               ctypes.POINTER(ctypes.c_size_t)], i32),
         "hbf_kv_attention": ([ctypes.POINTER(hbf_kv_layer), ctypes.POINTER(hbf_attention), vp, vp, ctypes.c_size_t,
                               vp], i32),
+        "hbf_kv_write_rotated": ([ctypes.POINTER(hbf_kv), i32, ctypes.POINTER(hbf_new_tokens), vp], i32),
+        "hbf_kv_chunk_workspace_bytes": ([ctypes.POINTER(hbf_kv), ctypes.POINTER(hbf_kv_layer),
+                                          ctypes.POINTER(hbf_chunk), ctypes.POINTER(ctypes.c_size_t)], i32),
+        "hbf_kv_chunk_attention": ([ctypes.POINTER(hbf_kv), ctypes.POINTER(hbf_kv_layer), ctypes.POINTER(hbf_chunk),
+                                    vp, vp, ctypes.c_size_t, vp], i32),
+        "hbf_kv_evict": ([ctypes.POINTER(hbf_kv), ctypes.POINTER(hbf_eviction), vp], i32),
         "hbf_moe_workspace_bytes": ([ctypes.POINTER(hbf_moe), i32, ctypes.POINTER(ctypes.c_size_t)], i32),
         "hbf_moe_layer": ([ctypes.POINTER(hbf_moe), vp, i64, i32, vp, vp, vp, i64, vp, vp, ctypes.c_size_t, vp],
                           i32),
@@ -545,6 +590,10 @@ def _writable(t, what):
     return t
 
 
+def _same_layout(t, like):
+    return getattr(t, "is_cuda", False) and t.dtype == like.dtype and t.shape == like.shape and t.stride() == like.stride()
+
+
 class _Blocks:
     """Device blocks of one object, and the streams that its calls used them
     on: the allocator gives them away only once those are through with them."""
@@ -636,10 +685,13 @@ class KvPages:
         self.layers, _, self.pages, self.page_tokens, self.kv_heads, self.head_dim = pool.shape
         self._attn_ws = _Scratch()
         self._attn_sizes, self._attn_bytes, self._layers = None, 0, {}
-        words = _zeroed(512, pool.device, 512).view(torch.int32)
-        self._attn_status, self._attn_ctl = words[:1], words[64:]
-        self._attn_args = hbf_attention()
+        self._chunk_sizes, self._chunk_bytes = None, 0
+        nbytes = 512 + 4 * HBF_CHUNK_CTL_WORDS
+        words = _zeroed(nbytes, pool.device, nbytes).view(torch.int32)
+        self._attn_status, self._attn_ctl, self._chunk_ctl = words[:1], words[64:], words[128:]
+        self._attn_args, self._chunk_args, self._new_args = hbf_attention(), hbf_chunk(), hbf_new_tokens()
         self._attn_at = (self._attn_status.data_ptr(), self._attn_ctl.data_ptr())
+        self._chunk_at = self._chunk_ctl.data_ptr()
         self._attn_words = _Blocks(words)
         self._kv = None
         if refs is None and tables is None and lens is None:
@@ -806,6 +858,135 @@ class KvPages:
         raw = _raw(stream)
         self._attn_words.use(raw, stream)
         return self._lib.hbf_kv_attention(kv, at, self._attn_at[0], ws.data_ptr(), ws.numel(), raw)
+
+    def write_rotated(self, layer, q, k, v, slots, pos, freqs, q_out, q_weight=None, k_weight=None, eps=1e-6,
+                      positions=None, interleaved=False, stream=None):
+        """New tokens of one layer enter the cache: q [n, heads, head_dim] is
+        normed (with q_weight [head_dim]; None: not) and turned to q_out (which
+        may be q), k [n, kv_heads, head_dim] likewise and v as it is go to token
+        pos[i] of slot slots[i] (int32 [n]).  Rows and heads may be strided, as
+        views of one projection's output are.  freqs: float64, radians per
+        position of each pair that turns (a multiple of 8, up to head_dim / 2);
+        pair i is the values i and i + len(freqs), interleaved: 2 i and 2 i + 1.
+        positions: int32 [n], pos if None."""
+        d = self._desc()
+        dtype = self.pool.dtype
+        if not 0 <= layer < self.layers:
+            raise HbfError(HBF_EINVAL, f"layer {layer}, the pool has {self.layers}")
+        n = _ints(slots, "slots")
+        _ints(pos, "pos", n)
+        if positions is not None:
+            _ints(positions, "positions", n)
+        for t, what in ((q, "q"), (k, "k"), (v, "v"), (q_out, "q_out")):
+            if not _is(t, dtype) or t.dim() != 3:
+                _strided(t, what, (dtype,), 3)
+        _writable(q_out, "q_out")
+        heads, dim, kv_shape = q.shape[1], self.head_dim, (n, self.kv_heads, self.head_dim)
+        if q.shape != (n, heads, dim) or q_out.shape != q.shape or k.shape != kv_shape or v.shape != kv_shape:
+            raise HbfError(HBF_EINVAL, f"q, k, v, q_out: shapes {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}, "
+                                       f"{tuple(q_out.shape)}, expected [{n}, heads, {dim}] and {list(kv_shape)}")
+        for t, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None and (not _is(t, dtype) or t.shape != (dim,)):
+                _dev(t, what, (str(dtype).replace("torch.", ""),), shape=(dim,))
+        if not _is(freqs, torch.float64):
+            _dev(freqs, "freqs", ("float64",))
+        qs, ks, vs, os = q.stride(), k.stride(), v.stride(), q_out.stride()
+        row = n > 1
+        nt = self._new_args
+        _pack_new_tokens(nt, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), qs[0] if row else 0,
+                         qs[1] if heads > 1 else 0, ks[0] if row else 0, ks[1] if self.kv_heads > 1 else 0,
+                         vs[0] if row else 0, vs[1] if self.kv_heads > 1 else 0, q_out.data_ptr(),
+                         os[0] if row else 0, os[1] if heads > 1 else 0, n, heads, self.kv_heads, dim,
+                         HBF_BF16 if dtype is torch.bfloat16 else HBF_FP16, HBF_ROT_PAIRS if interleaved else 0,
+                         0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
+                         eps, freqs.numel(), freqs.data_ptr(), slots.data_ptr(), pos.data_ptr(),
+                         0 if positions is None else positions.data_ptr())
+        return self._lib.hbf_kv_write_rotated(d, layer, nt, self._on(stream))
+
+    def attention(self, layer, q, out, slots, starts, lse=None, weights=None, scale=None, window=0, sinks=0,
+                  stream=None):
+        """Causal attention of new tokens over the cache.  Row i's queries are
+        q[starts[i]:starts[i + 1]] (q: [tokens, heads, head_dim]; starts: int32
+        [rows + 1], slots: int32 [rows]), the last tokens of slot slots[i], whose
+        K and V are in the cache already: one per row in a decode step, more for
+        a chunk of a prompt, also in one call.  window > 0: a query sees the
+        last `window` tokens up to its own, and the first `sinks`.  out: as q
+        (not q itself); lse: float32 [tokens, heads] or None; weights: float32
+        [slots, kv_heads, tokens] (slots and heads may be strided) or None:
+        each cached token's grows by the probabilities that the row's queries
+        gave it.  What lies behind starts[rows] is left as it was."""
+        d = self._desc()
+        dtype = self.pool.dtype
+        if not 0 <= layer < self.layers:
+            raise HbfError(HBF_EINVAL, f"layer {layer}, the pool has {self.layers}")
+        if not _is(q, dtype) or q.dim() != 3:
+            _strided(q, "q", (dtype,), 3)
+        if not _is(out, dtype):
+            _writable(_strided(out, "out", (dtype,), 3), "out")
+        shape = q.shape
+        tokens, heads, dim = shape
+        if dim != self.head_dim or out.shape != shape:
+            raise HbfError(HBF_EINVAL, f"q, out: shapes {tuple(shape)}, {tuple(out.shape)}, expected "
+                                       f"[tokens, heads, {self.head_dim}]")
+        rows = _ints(slots, "slots")
+        _ints(starts, "starts", rows + 1)
+        if lse is not None and (not _is(lse, torch.float32) or lse.shape != shape[:2]):
+            _dev(lse, "lse", ("float32",), shape=(tokens, heads))
+        ws, held = (0, 0), 0
+        if weights is not None:
+            self._check_weights(weights, "weights", (self.tables.shape[0], self.kv_heads))
+            ws, held = (_stride(weights, 0), _stride(weights, 1)), weights.shape[2]
+        kv = self._layer(layer)
+        qs, os = q.stride(), out.stride()
+        at = self._chunk_args
+        _pack_chunk(at, 0, q.data_ptr(), qs[0] if tokens > 1 else 0, qs[1] if heads > 1 else 0, tokens, rows, heads,
+                    dim ** -0.5 if scale is None else scale, slots.data_ptr(), starts.data_ptr(), int(window),
+                    int(sinks), out.data_ptr(), os[0] if tokens > 1 else 0, os[1] if heads > 1 else 0,
+                    0 if lse is None else lse.data_ptr(), 0 if weights is None else weights.data_ptr(), *ws,
+                    min(held, (1 << 31) - 1), self._chunk_at or 0)
+        sizes = (tokens, rows, heads, weights is None)
+        if sizes != self._chunk_sizes:
+            b = ctypes.c_size_t()
+            rc = self._lib.hbf_kv_chunk_workspace_bytes(d, kv, at, ctypes.byref(b))
+            if rc != HBF_OK:
+                return rc
+            self._chunk_sizes, self._chunk_bytes = sizes, b.value
+        scratch = self._attn_ws.get(self._chunk_bytes, self.pool.device, stream)
+        raw = _raw(stream)
+        self._attn_words.use(raw, stream)
+        return self._lib.hbf_kv_chunk_attention(d, kv, at, self._attn_at[0], scratch.data_ptr(), scratch.numel(), raw)
+
+    def _check_weights(self, t, what, lead):
+        """Accumulated weights: float32 [*lead, tokens], tokens contiguous."""
+        if not isinstance(t, _Tensor) or not t.is_cuda or t.dtype is not torch.float32 \
+                or tuple(t.shape[:-1]) != lead or (t.shape[-1] > 1 and t.stride(-1) != 1):
+            raise HbfError(HBF_EINVAL, f"{what}: expected float32 {[*lead, 'tokens']} in GPU memory, tokens contiguous")
+        _writable(t, what)
+
+    def evict(self, slots, keep, weights, kept, sinks=0, recent=0, weights_out=None, stream=None):
+        """Slot slots[i] is cut down to keep[i] tokens (int32 [n]), in every
+        layer and KV head its own: the first `sinks`, the last `recent`, and
+        those of the largest weights between.  weights: float32 [layers, slots,
+        kv_heads, tokens] (as attention's, for each layer; all but the tokens
+        may be strided) follow their tokens, in place or to weights_out (shaped
+        and strided alike).  kept: int32 [layers, n, kv_heads, max_keep],
+        max_keep at least the largest keep, receives each place's token's old
+        position, -1 behind them."""
+        d = self._desc()
+        n = _ints(slots, "slots")
+        _ints(keep, "keep", n)
+        self._check_weights(weights, "weights", (self.layers, self.tables.shape[0], self.kv_heads))
+        if weights_out is not None and (not _same_layout(weights_out, weights)):
+            raise HbfError(HBF_EINVAL, "weights_out: expected the shape, strides and type of weights")
+        if not _is(kept, _int32) or kept.dim() != 4 or kept.shape[:3] != (self.layers, n, self.kv_heads):
+            _dev(kept, "kept", _I32)
+            raise HbfError(HBF_EINVAL, f"kept: shape {tuple(kept.shape)}, expected "
+                                       f"[{self.layers}, {n}, {self.kv_heads}, max_keep]")
+        ev = hbf_eviction(slots.data_ptr(), keep.data_ptr(), n, self.kv_heads, int(sinks), int(recent),
+                          weights.data_ptr(), _stride(weights, 0), _stride(weights, 1), _stride(weights, 2),
+                          min(weights.shape[3], (1 << 31) - 1), None if weights_out is None else weights_out.data_ptr(),
+                          kept.data_ptr(), kept.shape[3])
+        return self._lib.hbf_kv_evict(d, ev, self._on(stream))
 
     def _layer(self, layer):
         """The library's description of one layer's pages."""
