@@ -33,8 +33,11 @@ namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int FEW_TILE = 32;   // tokens of a wave's step where queries are few
-constexpr int MANY_TILE = 64;  // tokens staged where they are many
-constexpr int MANY_Q = 128, FEW_Q = 16;  // queries per tile
+constexpr int MANY_TILE = 64;  // tokens staged at a time where they are many
+constexpr int HALF = 32;       // tokens of a step there
+constexpr int RING = 4;        // staged tiles
+constexpr int MANY_Q = 256;    // queries of a tile there
+constexpr int MANY_WAVES = MANY_Q / 32, MANY_THREADS = 64 * MANY_WAVES;
 
 struct Args {
   hbf_kv kv;
@@ -43,9 +46,10 @@ struct Args {
   int group;          // query heads per KV head
   float c;            // |scale| * log2(e), not 0
   uint32_t flip;      // sign bits of two 16-bit values if the scale is negative
+  uint32_t window;    // of positions, or all of them
   uint32_t page_mul;  // token / page_tokens = token * page_mul >> page_shift, for tokens below 2^31
   int page_shift;
-  int tile_q, tile_shift;  // queries per tile, FEW_Q or MANY_Q, and its logarithm
+  int tile_q, tile_shift;  // queries per tile, 16, 32 or MANY_Q, and its logarithm
   int slots;          // places for tiles: tokens * group / tile_q + rows
   int splits;         // most parts of a tile
   int part_steps;     // least steps of a part
@@ -121,7 +125,7 @@ __device__ __forceinline__ View view_of(const Args &a, const Row &r, int q0, int
   return v;
 }
 __device__ __forceinline__ bool sees(const Args &a, int p, int token) {
-  return token <= p && (a.ch.window == 0 || token > p - a.ch.window || token < a.ch.sinks);
+  return (token <= p) & (((uint32_t)p - (uint32_t)token < a.window) | (token < a.ch.sinks));
 }
 // Whether every query of the tile sees all of x .. x + n - 1 (which are below total).
 __device__ __forceinline__ bool all_see(const Args &a, const View &v, uint32_t x, uint32_t n) {
@@ -187,27 +191,12 @@ struct Stage : Places<D, NT> {
   }
 };
 
-// The same share loaded past the registers, straight into LDS; there after loads_done().
-template <int D, int NT>
-struct StageLds : Places<D, NT> {
-  using P = Places<D, NT>;
-  // To tokens first .. of a tile (past x1: its last one again).
-  __device__ __forceinline__ void load(const Args &a, const View &vw, uint32_t x, uint32_t x1, int head, uint32_t kt,
-                                       uint32_t vt, int first) {
-    const int lane = threadIdx.x & 63;
-    const int64_t at = P::place(a, vw, x, x1, head);
-    int64_t row[P::PASSES];
-#pragma unroll
-    for (int j = 0; j < P::PASSES; j++) row[j] = from_lane(at, j * P::AT_ONCE + lane / P::LANES);
-#pragma unroll
-    for (int j = 0; j < P::PASSES; j++) {
-      const int t = first + j * P::AT_ONCE;  // of the wave's first lanes
-      const int mine = t + lane / P::LANES, piece = lane % P::LANES * 16;
-      to_lds((const char *)a.layer.dev_k + row[j] + (piece ^ (k_at<D>(mine, 0) - mine * (D * 2))), kt + t * (D * 2));
-      to_lds((const char *)a.layer.dev_v + row[j] + (piece ^ (v_at<D>(mine, 0) - mine * (D * 2))), vt + t * (D * 2));
-    }
-  }
-};
+// Byte offset of 16-byte piece `piece` of a token in a staged tile of V whose
+// readers take four pieces of 4 tokens in one cycle.
+template <int D>
+__device__ __forceinline__ int v4_at(int token, int piece) {
+  return token * (D * 2) + ((piece ^ (D == 128 ? (token & 3) << 2 : (token >> 1 & 1) << 2)) << 4);
+}
 
 // The tile that a workgroup works on.
 struct Tile {
@@ -240,53 +229,55 @@ __device__ __forceinline__ void load_query(const Args &a, Query q, int kgroup, u
   }
 }
 
-// Four of a query's values, from d0 on, from its sums; none: it sees no token.
-// lead: the one thread that writes lse.
+// What a query's sums are multiplied with: 1 / l, or 0 where it sees no token, or
+// NaN where it met a bad page.
+__device__ __forceinline__ float one_over(Query q, float l, bool bad) { return bad ? NAN : q.pos < 0 ? 0.f : 1.f / l; }
+// Four of a query's values, from d0 on.
 template <typename T>
-__device__ __forceinline__ void write_out(const Args &a, Query q, int d0, f32x4 o, float m, float l, bool bad, bool lead) {
-  const bool none = q.pos < 0 && !bad;
-  if (bad) l = NAN;
-  o *= none ? 0.f : 1.f / l;
+__device__ __forceinline__ void write_out(const Args &a, Query q, int d0, f32x4 o) {
   typename T::elem *out = (typename T::elem *)a.ch.dev_out + q.token * a.ch.out_row_stride + q.head * a.ch.out_head_stride + d0;
   *(u32x2 *)out = u32x2{pack2<T>(o[0], o[1]), pack2<T>(o[2], o[3])};
-  if (!lead) return;
+}
+// A query's lse, and what its weights are computed from; by one thread.
+template <typename T>
+__device__ __forceinline__ void write_sums(const Args &a, Query q, float m, float l, bool bad) {
   const int64_t at = (int64_t)q.token * a.ch.heads + q.head;
+  const bool none = q.pos < 0 && !bad;
   const float sum = l * exp2f(-SHIFT<T>);
-  if (a.ch.dev_lse) a.ch.dev_lse[at] = none ? -INFINITY : m * a.c * LN2 + logf(sum);
+  if (a.ch.dev_lse) a.ch.dev_lse[at] = bad ? NAN : none ? -INFINITY : m * a.c * LN2 + logf(sum);
   // a query in error or that sees nothing gives no weight
   if (a.query_ml) a.query_ml[at] = bad || none ? make_float2(0.f, 0.f) : make_float2(m, 1.f / sum);
 }
 
 // A step's products with V one by one, in 32 bits: a value that a query does not see
-// must not meet its 0.  s: the lane's probabilities; pos: its queries' positions.
+// must not meet its 0.  p: the lane's probabilities as they are multiplied otherwise;
+// pos: its queries' positions; at: U * 512 bytes of LDS of the wave's own.
 template <typename T, int D, int QT, int U>
-__device__ void products_one_by_one(const Args &a, const View &v, const char *vt, uint32_t x, uint32_t x1,
-                                    const f32x4 (&s)[QT][U], const int (&pos)[QT], f32x4 (&o)[QT][D / 16]) {
+__device__ __forceinline__ void products_one_by_one(const Args &a, const View &v, const char *vt, uint32_t x, uint32_t x1,
+                                                    const u32x4 (&p)[QT][U / 2], const int (&pos)[QT],
+                                                    f32x4 (&o)[QT][D / 16], char *at) {
+  typedef typename T::elem e4 __attribute__((ext_vector_type(4)));
   const int lane = threadIdx.x & 63, col = lane & 15, kg = lane >> 4;
 #pragma unroll
-  for (int u = 0; u < U; u++)
+  for (int q = 0; q < QT; q++) {
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int u = 0; u < U; u++)  // [tokens / 4][16 queries][4 tokens]
+      *(u32x2 *)(at + ((u * 4 + kg) * 16 + col) * 8) = u32x2{p[q][u / 2][u % 2 * 2], p[q][u / 2][u % 2 * 2 + 1]};
+    wave_lds_fence();
 #pragma unroll 1
-      for (int g = 0; g < 4; g++) {
-        const int t = u * 16 + g * 4 + i;
-        if (x + t >= x1) break;
-        const int token = (int)v.token(x + t);
+    for (int t = 0; t < U * 16 && x + t < x1; t++) {
+      if (!sees(a, pos[q], (int)v.token(x + t))) continue;
+      const float w = (float)*(const typename T::elem *)(at + ((t >> 2) * 16 + col) * 8 + (t & 3) * 2);
 #pragma unroll
-        for (int q = 0; q < QT; q++) {
-          const float p = __shfl(s[q][u][i], g * 16 + col);
-          if (!sees(a, pos[q], token)) continue;
+      for (int d = 0; d < D / 16; d++) {
+        const int n = d * 16 + kg * 4;
+        const e4 e = *(const e4 *)(vt + v_at<D>(t, n / 8) + (n % 8) * 2);
 #pragma unroll
-          for (int d = 0; d < D / 16; d++) {
-            const int at = d * 16 + kg * 4;
-            const u32x2 w = *(const u32x2 *)(vt + v_at<D>(t, at / 8) + (at % 8) * 2);
-            typedef typename T::elem e4 __attribute__((ext_vector_type(4)));
-            const e4 e = __builtin_bit_cast(e4, w);
-#pragma unroll
-            for (int k = 0; k < 4; k++) o[q][d][k] = fmaf(p, (float)e[k], o[q][d][k]);
-          }
-        }
+        for (int k = 0; k < 4; k++) o[q][d][k] = fmaf(w, (float)e[k], o[q][d][k]);
       }
+    }
+    wave_lds_fence();
+  }
 }
 // Whether 16 bytes hold a value that is not finite.
 template <typename T>
@@ -307,7 +298,8 @@ __device__ __forceinline__ int64_t part_at(const Args &a, const Tile &t, int spl
 // a time, U parts of each asked for at once.
 template <typename T, int D>
 __device__ void join(const Args &a, const Tile &t) {
-  constexpr int LANES = D / 4, AT_ONCE = THREADS / LANES, R = 2, U = 8;
+  constexpr int LANES = D / 4, R = 2, U = 8;
+  const int AT_ONCE = blockDim.x / LANES;
   const int d0 = threadIdx.x % LANES * 4, mine = threadIdx.x / LANES;
   for (int i0 = mine; i0 < t.q1 - t.q0; i0 += AT_ONCE * R) {
     float m[R], l[R];
@@ -341,7 +333,9 @@ __device__ void join(const Args &a, const Tile &t) {
 #pragma unroll
     for (int r = 0; r < R; r++) {
       const Query q = query_of(a, t, i0 + r * AT_ONCE);
-      if (q.head >= 0) write_out<T>(a, q, d0, o[r], m[r], l[r], bad[r], d0 == 0);
+      if (q.head < 0) continue;
+      write_out<T>(a, q, d0, o[r] * one_over(q, l[r], bad[r]));
+      if (d0 == 0) write_sums<T>(a, q, m[r], l[r], bad[r]);
     }
   }
 }
@@ -356,18 +350,18 @@ __device__ void end_part(const Args &a, const Tile &t) {
 
 // ------------------------------------------------------------ few queries
 
-// A tile of at most 16 QT queries, one per column: each wave takes 32 tokens at a
-// time through LDS of its own, the next ones' loads in flight; the waves meet
-// once, at the end.
-template <typename T, int D, int QT>
-__device__ void few(const Args &a, const Tile &t, char *lds) {
+// 16 QT queries of a tile, from i0 on, one per column: each of W waves takes 32 tokens
+// at a time through LDS of its own, the next ones' loads in flight; the waves
+// meet once, at the end.
+template <typename T, int D, int QT, int W>
+__device__ __forceinline__ void few(const Args &a, const Tile &t, int i0, char *lds) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   constexpr int KS = D / 32, DT = D / 16;
   u32x4 qv[QT][KS];
   int pos[QT];
 #pragma unroll
   for (int q = 0; q < QT; q++) {
-    const Query qq = query_of(a, t, q * 16 + col);
+    const Query qq = query_of(a, t, i0 + q * 16 + col);
     pos[q] = qq.head < 0 ? t.view.p1 : qq.pos;
     load_query<T, D>(a, qq, kg, qv[q]);
   }
@@ -385,7 +379,7 @@ __device__ void few(const Args &a, const Tile &t, char *lds) {
   const uint32_t x1 = t.x1;
   uint32_t x = t.x0 + w * FEW_TILE;
   Stage<D, FEW_TILE> st;
-  constexpr uint32_t STEP = WAVES * FEW_TILE;
+  constexpr uint32_t STEP = W * FEW_TILE;
   if (x < x1) {
     st.find(a, t.view, pages, x, x1);
     st.load(a, t.view, x, x1, t.head);
@@ -429,17 +423,17 @@ __device__ void few(const Args &a, const Tile &t, char *lds) {
               if (xx >= x1 || !sees(a, pos[q], token)) s[q][u][i] = -INFINITY;
           }
       softmax_step<T, QT, 2, DT>(s, a.c, m, l, o);
-      if (odd) {
-        products_one_by_one<T, D, QT, 2>(a, t.view, vt, x, x1, s, pos, o);
-      } else {
-        u32x4 p[QT];
+      u32x4 p[QT][1];
 #pragma unroll
-        for (int q = 0; q < QT; q++) p[q] = p_operand<T>(s[q][0], s[q][1]);
+      for (int q = 0; q < QT; q++) p[q][0] = p_operand<T>(s[q][0], s[q][1]);
+      if (odd) {  // (in the wave's own K, which is done with)
+        products_one_by_one<T, D, QT, 2>(a, t.view, vt, x, x1, p, pos, o, kt);
+      } else {
 #pragma unroll
         for (int d = 0; d < DT; d++) {
           const u32x4 v = v_operand<D>(vt, kg * 4, 16 + kg * 4, d, lane);
 #pragma unroll
-          for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q], o[q][d]);
+          for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][0], o[q][d]);
         }
       }
       wave_lds_fence();
@@ -449,8 +443,8 @@ __device__ void few(const Args &a, const Tile &t, char *lds) {
   }
   // the waves' parts become one: 16 queries at a time through LDS
   constexpr int RS = D + 4;  // a query's row, padded against bank conflicts
-  float *ro = (float *)lds;  // [WAVES][16][RS], then the maxima and sums
-  float2 *rml = (float2 *)(lds + WAVES * 16 * RS * 4);
+  float *ro = (float *)lds;  // [W][16][RS], then the maxima and sums
+  float2 *rml = (float2 *)(lds + W * 16 * RS * 4);
   const bool any_bad = __syncthreads_or(st.bad);
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
 #pragma unroll
@@ -460,193 +454,316 @@ __device__ void few(const Args &a, const Tile &t, char *lds) {
 #pragma unroll
     for (int d = 0; d < DT; d++) *(f32x4 *)(ro + (w * 16 + col) * RS + d * 16 + kg * 4) = o[q][d];
     __syncthreads();
-    constexpr int PER = THREADS / 16;  // threads per query
+    constexpr int PER = W * 64 / 16;  // threads per query
     const int n = threadIdx.x / PER, d0 = threadIdx.x % PER * 4;
-    const Query qq = query_of(a, t, q * 16 + n);
+    const Query qq = query_of(a, t, i0 + q * 16 + n);
     if (qq.head >= 0) {
       float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < WAVES; i++) mx = fmaxf(mx, rml[i * 16 + n].x);
+      for (int i = 0; i < W; i++) mx = fmaxf(mx, rml[i * 16 + n].x);
       const float ref = mx == -INFINITY ? 0.f : mx;
-      float f[WAVES];
+      float f[W];
 #pragma unroll
-      for (int i = 0; i < WAVES; i++) {
+      for (int i = 0; i < W; i++) {
         f[i] = __builtin_amdgcn_exp2f((rml[i * 16 + n].x - ref) * a.c);
         sum += f[i] * rml[i * 16 + n].y;
       }
-      const int64_t at = t.parts > 1 ? part_at(a, t, t.split, q * 16 + n) : 0;
+      const int64_t at = t.parts > 1 ? part_at(a, t, t.split, i0 + q * 16 + n) : 0;
 #pragma unroll
       for (int d = d0; d < D; d += PER * 4) {
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < WAVES; i++) v += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
+        for (int i = 0; i < W; i++) v += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
         if (t.parts > 1) hand_over((f32x4 *)(a.part + at * D + d), v);
-        else write_out<T>(a, qq, d, v, mx, sum, any_bad, d == 0);
+        else write_out<T>(a, qq, d, v * one_over(qq, sum, any_bad));
       }
+      if (d0 == 0 && t.parts == 1) write_sums<T>(a, qq, mx, sum, any_bad);
       if (d0 == 0 && t.parts > 1) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum));
     }
     __syncthreads();
   }
-  if (t.parts > 1) end_part<T, D>(a, t);
 }
 
 // ------------------------------------------------------------ many queries
 
-// A tile of up to MANY_Q queries: 64 tokens staged for four waves of 32 queries each.
+// op over the two lanes that hold the same column of a 32 x 32 tile, in both of them.
+template <typename F>
+__device__ __forceinline__ float across_halves(float x, F op) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t a = both[0], b = both[1];
+  return op(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+
+// A tile of up to MANY_Q queries, 32 for each of eight waves, two on each SIMD, and 64
+// tokens staged for all of them.  Steps of 32 tokens are one ahead of each other:
+// while the scores of step h become probabilities on the vector units, the matrix
+// cores multiply h - 1's probabilities with V, then K of h + 1 with the queries.
 template <typename T, int D>
-__device__ void many(const Args &a, const Tile &t, char *lds) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
-  static_assert(MANY_Q == 32 * WAVES, "queries per wave");
-  constexpr int KS = D / 32, DT = D / 16, QT = 2, U = MANY_TILE / 16;
-  constexpr int TILE_BYTES = MANY_TILE * D * 2;
-  constexpr int NT = MANY_TILE / WAVES;  // tokens of a tile that a wave stages
-  constexpr uint32_t STEP = MANY_TILE;
-  const int32_t *pages = t.row.pages;
-  const uint32_t lds0 = lds_address(lds), x1 = t.x1;
-  StageLds<D, NT> st;
-  st.find(a, t.view, pages, t.x0 + w * NT, x1);
-  u32x4 qv[QT][KS];
-  int pos[QT];
-#pragma unroll
-  for (int q = 0; q < QT; q++) {
-    const Query qq = query_of(a, t, w * 32 + q * 16 + col);
-    pos[q] = qq.head < 0 ? t.view.p1 : qq.pos;
-    load_query<T, D>(a, qq, kg, qv[q]);
+struct Many {
+  static constexpr int KS = D / 16, DT = D / 32;
+  static constexpr int TILE_BYTES = MANY_TILE * D * 2;      // of K, then as much of V
+  static constexpr int NT = MANY_TILE / MANY_WAVES;         // tokens of a tile that a wave stages
+  static constexpr int GROUP = 64 / NT;                     // tiles whose places it looks up at a time, a lane a token
+  static constexpr int LANES = D / 8, AT_ONCE = 64 / LANES, PASSES = NT / AT_ONCE;
+  const Args &a;
+  const Tile &t;
+  char *lds;
+  uint32_t lds0;
+  int lane, w, col, hf;
+  int page = 0, pos;
+  bool bad = false, odd = false;
+  int64_t at;       // bytes to the row of this lane's token of the group
+  u32x4 qv[KS], p[2], kk[KS], vv[DT][2];
+  f32x16 o[DT];
+  float m = -INFINITY, l = 0.f;
+
+  __device__ __forceinline__ Many(const Args &a, const Tile &t, char *lds) : a(a), t(t), lds(lds) {
+    lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 31, hf = lane >> 5;
+    lds0 = lds_address(lds);
   }
-  st.load(a, t.view, t.x0 + w * NT, x1, t.head, lds0, lds0 + TILE_BYTES, w * NT);
-  f32x4 o[QT][DT];
-  float m[QT], l[QT];
+  __device__ __forceinline__ void load_queries() {
+    const Query qq = query_of(a, t, w * 32 + col);
+    const bool none = qq.head < 0;
+    pos = none ? t.view.p1 : qq.pos;
+    const char *from = (const char *)a.ch.dev_q + 2 * (none ? 0 : qq.token * a.ch.q_row_stride + qq.head * a.ch.q_head_stride);
 #pragma unroll
-  for (int q = 0; q < QT; q++) {
-    m[q] = -INFINITY;
-    l[q] = 0.f;
+    for (int k = 0; k < KS; k++) {
+      const u32x4 v = *(const u32x4 *)(from + (k * 16 + hf * 8) * 2) ^ a.flip;
+      qv[k] = none ? u32x4{0, 0, 0, 0} : v;
+    }
 #pragma unroll
-    for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) o[d][i] = 0.f;
   }
-  st.find(a, t.view, pages, t.x0 + STEP + w * NT, x1);
-  loads_done();
-  __syncthreads();
-  int cur = 0;
-  for (uint32_t x = t.x0;;) {
-    char *kt = lds + cur * 2 * TILE_BYTES, *vt = kt + TILE_BYTES;
-    const bool whole = x1 - x >= MANY_TILE && all_see(a, t.view, x, MANY_TILE);
-    bool odd = false;
-    if (!whole) {  // 0 * infinity must not reach the sums: no V behind the last token, and see what is before it
-      for (int i = threadIdx.x * 16; i < TILE_BYTES; i += THREADS * 16) {
-        u32x4 *at = (u32x4 *)(vt + i);
-        if (x + i / (D * 2) >= x1) *at = u32x4{0, 0, 0, 0};
-        else odd |= not_finite<T>(*at);
+  // This lane's token of the tiles from `tile` on (past the part: its last one).
+  __device__ __forceinline__ uint32_t token(int tile) const {
+    return t.view.token(min(t.x0 + (tile + lane / NT) * MANY_TILE + w * NT + lane % NT, t.x1 - 1));
+  }
+  __device__ __forceinline__ void find(int tile) { page = t.row.pages[page_index(a, token(tile))]; }
+  __device__ __forceinline__ void place(int tile) {
+    if (page < 0 || page >= a.layer.pages) {  // noted; page 0 is read instead
+      bad = true;
+      page = 0;
+    }
+    const uint32_t tok = token(tile), in_page = tok - page_index(a, tok) * (uint32_t)a.layer.page_tokens;
+    at = 2 * (page * a.layer.page_stride + in_page * a.layer.token_stride + t.head * a.layer.head_stride);
+  }
+  // A tile on its way to LDS: 2 PASSES loads of the wave.
+  __device__ __forceinline__ void stage(int tile) {
+    if (tile % GROUP == 0 && tile > 0) {
+      place(tile);
+      find(tile + GROUP);
+    }
+    const uint32_t kt = lds0 + tile % RING * 2 * TILE_BYTES, vt = kt + TILE_BYTES;
+    int64_t row[PASSES];
+#pragma unroll
+    for (int j = 0; j < PASSES; j++) row[j] = from_lane(at, tile % GROUP * NT + j * AT_ONCE + lane / LANES);
+#pragma unroll
+    for (int j = 0; j < PASSES; j++) {
+      const int first = w * NT + j * AT_ONCE;  // of the wave's first lanes
+      const int mine = first + lane / LANES, piece = lane % LANES * 16;
+      to_lds((const char *)a.layer.dev_k + row[j] + (piece ^ (k_at<D>(mine, 0) - mine * (D * 2))), kt + first * (D * 2));
+      to_lds((const char *)a.layer.dev_v + row[j] + (piece ^ (v4_at<D>(mine, 0) - mine * (D * 2))), vt + first * (D * 2));
+    }
+  }
+  __device__ __forceinline__ void read_k(int tile, int first) {
+    const char *kt = lds + tile % RING * 2 * TILE_BYTES;
+#pragma unroll
+    for (int k = 0; k < KS; k++) kk[k] = *(const u32x4 *)(kt + k_at<D>(first + col, k * 2 + hf));
+  }
+  __device__ __forceinline__ void read_v(int tile, int first) {
+    const char *vt = lds + tile % RING * 2 * TILE_BYTES + TILE_BYTES;
+    const int i = lane & 15, half = (i & 1) << 3, r = first + hf * 4 + (i >> 2);
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int k = 0; k < 2; k++) {
+        const int piece = d * 4 + ((lane >> 4 & 1) << 1) + ((i & 3) >> 1);
+        const u32x2 x = read_transposed(vt + v4_at<D>(r + k * 16, piece) + half);
+        const u32x2 y = read_transposed(vt + v4_at<D>(r + k * 16 + 8, piece) + half);
+        vv[d][k] = u32x4{x[0], x[1], y[0], y[1]};
       }
-      odd = __syncthreads_or(odd);
+  }
+  __device__ __forceinline__ void scores(f32x16 &s) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) s[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; k++) s = T::mfma32(kk[k], qv[k], s);
+  }
+  __device__ __forceinline__ void add_values() {
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+#pragma unroll
+      for (int d = 0; d < DT; d++) o[d] = T::mfma32(vv[d][k], p[k], o[d]);
+  }
+  __device__ __forceinline__ void nothing_pending() {
+    p[0] = p[1] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int d = 0; d < DT; d++) vv[d][0] = vv[d][1] = u32x4{0, 0, 0, 0};
+  }
+  // Whether every query sees all of tile i.
+  __device__ __forceinline__ bool whole(int i) const {
+    const uint32_t x = t.x0 + i * MANY_TILE;
+    return t.x1 - x >= MANY_TILE && all_see(a, t.view, x, MANY_TILE);
+  }
+  // Scores of the tokens from x on that their query does not see, or that are none.
+  __device__ __forceinline__ void mask(f32x16 &s, uint32_t x) const {
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      const uint32_t xx = x + (i / 4) * 8 + hf * 4 + i % 4;
+      s[i] = (xx < t.x1) & sees(a, pos, (int)t.view.token(xx)) ? s[i] : -INFINITY;
     }
-    // Operands come from LDS one group of products ahead of their use: left to
-    // itself the compiler waits for each group's reads right before it.
-    u32x4 kk[2][KS];
-    auto read_k = [&](int u) {
+  }
+  // A tile that is not whole: whether its V holds what is not finite (0 * infinity would reach the sums).
+  __device__ __forceinline__ void look(int tile) {
+    const char *vt = lds + tile % RING * 2 * TILE_BYTES + TILE_BYTES;
+#pragma unroll 1
+    for (int i = threadIdx.x * 16; i < TILE_BYTES; i += MANY_THREADS * 16) odd |= not_finite<T>(*(const u32x4 *)(vt + i));
+  }
+  // The running maximum takes the scores in, as in softmax_step.  PENDING: of the
+  // step before, probabilities and values wait in p and vv; they are relative to the old maximum.
+  template <bool PENDING>
+  __device__ __forceinline__ void maximum(const f32x16 &s) {
+    float mx = s[0];
 #pragma unroll
-      for (int k = 0; k < KS; k++) kk[u & 1][k] = *(const u32x4 *)(kt + k_at<D>(u * 16 + col, k * 4 + kg));
-    };
-    f32x4 s[QT][U];
-    read_k(0);
+    for (int i = 1; i < 16; i++) mx = fmaxf(mx, s[i]);
+    if (__any((mx - m) * a.c > LAZY)) {  // (none seen, none here: NaN, false)
+      if (PENDING) add_values();
+      const float top = fmaxf(m, across_halves(mx, MAX_OP));
+      const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.c);
+      m = top;
+      l *= alpha;
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      if (u + 1 < U) read_k(u + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < KS; k++)
-#pragma unroll
-        for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk[u & 1][k], qv[q][k], s[q][u]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int d = 0; d < DT; d++) o[d] *= alpha;
+      if (PENDING) nothing_pending();
     }
-    const bool more = x1 - x > STEP;
-    if (more) {  // the next step's tile, here so that its addresses are found beside the products
-      const uint32_t next = lds0 + (cur ^ 1) * 2 * TILE_BYTES;
-      st.load(a, t.view, x + STEP + w * NT, x1, t.head, next, next + TILE_BYTES, w * NT);
-      if (x1 - x > 2 * STEP) st.find(a, t.view, pages, x + 2 * STEP + w * NT, x1);
+  }
+  // Of 16 tokens of the step, k = 0 or 1.
+  __device__ __forceinline__ void probabilities(const f32x16 &s, int k) {
+    const float ref = m == -INFINITY ? 0.f : m;  // nothing seen yet: every p is 0
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const float d = s[k * 8 + i] - ref;
+      e[i] = __builtin_amdgcn_exp2f(SHIFT<T> == 0.f ? d * a.c : fmaf(d, a.c, SHIFT<T>));
+      l += e[i];
     }
-    if (!whole)
+    p[k] = u32x4{pack2<T>(e[0], e[1]), pack2<T>(e[2], e[3]), pack2<T>(e[4], e[5]), pack2<T>(e[6], e[7])};
+  }
+  // One step, of tokens first .. of a tile: its scores are in s and its maximum is
+  // known; the next one's (there are more), of a tile that is `whole` or not, go to sn.
+  __device__ __forceinline__ void step(const f32x16 &s, f32x16 &sn, int tile, int first, bool more, bool whole) {
+    const int next = first ? tile + 1 : tile;
+    read_k(next, HALF - first);
+    add_values();
+    probabilities(s, 0);
+    scores(sn);
+    read_v(tile, first);
+    probabilities(s, 1);
+    // a product, what it needs from LDS, some of the vector units' work, and so on: left to itself the compiler puts
+    // most of the products side by side
 #pragma unroll
-      for (int u = 0; u < U; u++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const uint32_t xx = x + u * 16 + kg * 4 + i;
-          const int token = (int)t.view.token(xx);
-#pragma unroll
-          for (int q = 0; q < QT; q++)
-            if (xx >= x1 || !sees(a, pos[q], token)) s[q][u][i] = -INFINITY;
-        }
-    u32x4 vv[2][U / 2];
-    auto read_v = [&](int d) {
-#pragma unroll
-      for (int u = 0; u < U / 2; u++)
-        vv[d & 1][u] = v_operand<D>(vt, u * 32 + kg * 4, u * 32 + 16 + kg * 4, d, lane);
-    };
-    softmax_step<T, QT, U, DT>(s, a.c, m, l, o);
-    if (odd) {
-      products_one_by_one<T, D, QT, U>(a, t.view, vt, x, x1, s, pos, o);
-    } else {
-      u32x4 p[QT][U / 2];
-#pragma unroll
-      for (int q = 0; q < QT; q++)
-#pragma unroll
-        for (int u = 0; u < U / 2; u++) p[q][u] = p_operand<T>(s[q][2 * u], s[q][2 * u + 1]);
-      read_v(0);
-#pragma unroll
-      for (int d = 0; d < DT; d++) {
-        if (d + 1 < DT) read_v(d + 1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < U / 2; u++)
-#pragma unroll
-          for (int q = 0; q < QT; q++) o[q][d] = T::mfma(vv[d & 1][u], p[q][u], o[q][d]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+    for (int z = 0; z < KS + 2 * DT; z++) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
     }
-    if (!more) break;
-    x += STEP;
-    loads_done();
+    if (!more) return;
+    if (!whole) mask(sn, t.x0 + next * MANY_TILE + HALF - first);
+    maximum<true>(sn);
+  }
+  // Waits until at most `tiles` (0 .. 2) of the staged tiles are on their way.
+  __device__ __forceinline__ void arrived(int tiles) {
+    constexpr int N = 2 * PASSES;
+    if (tiles <= 0) loads_left<0>();
+    else if (tiles == 1) loads_left<N>();
+    else loads_left<2 * N>();
     __syncthreads();
-    cur ^= 1;
   }
-  const bool any_bad = __syncthreads_or(st.bad);
-  if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
-#pragma unroll
-  for (int q = 0; q < QT; q++) {
-    const int i = w * 32 + q * 16 + col;
-    const Query qq = query_of(a, t, i);
-    const float lq = across_rows(l[q], SUM_OP);
-    if (qq.head < 0) continue;
-    if (t.parts > 1) {
-      const int64_t at = part_at(a, t, t.split, i);
-#pragma unroll
-      for (int d = 0; d < DT; d++) hand_over((f32x4 *)(a.part + at * D + d * 16 + kg * 4), o[q][d]);
-      if (kg == 0) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(m[q], lq));
-    } else {
-#pragma unroll
-      for (int d = 0; d < DT; d++) write_out<T>(a, qq, d * 16 + kg * 4, o[q][d], m[q], lq, any_bad, d == 0 && kg == 0);
+  // All of the part's tokens.
+  __device__ __forceinline__ void run() {
+    const int n = (int)((t.x1 - t.x0 + MANY_TILE - 1) / MANY_TILE);
+    find(0);
+    place(0);
+    find(GROUP);
+    for (int i = 0; i < min(n, RING - 1); i++) stage(i);
+    load_queries();
+    nothing_pending();
+    f32x16 sa, sb;
+    arrived(min(n, RING - 1) - 1);
+    bool now = whole(0);
+    if (!now) look(0);
+    read_k(0, 0);
+    scores(sa);
+    if (!now) mask(sa, t.x0);
+    maximum<false>(sa);
+    for (int i = 0; i < n; i++) {
+      step(sa, sb, i, 0, true, now);
+      // the next tile is there, and one more goes where all are done with
+      arrived(n - 2 - i);
+      if (i + RING - 1 < n) stage(i + RING - 1);
+      const bool more = i + 1 < n;
+      now = more && whole(i + 1);
+      if (more && !now) look(i + 1);
+      step(sb, sa, i, HALF, more, now);
     }
+    add_values();
   }
-  if (t.parts > 1) end_part<T, D>(a, t);
+};
+
+// Returns whether the tile has to be done again, the slow way.
+template <typename T, int D>
+__device__ __forceinline__ bool many(const Args &a, const Tile &t, char *lds) {
+  Many<T, D> z(a, t, lds);
+  constexpr int DT = D / 32;
+  z.run();
+  if (__syncthreads_or(z.odd)) return true;
+  const bool any_bad = __syncthreads_or(z.bad);
+  if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
+  const int i = z.w * 32 + z.col;
+  const Query qq = query_of(a, t, i);
+  const float l = across_halves(z.l, SUM_OP);
+  if (qq.head < 0) return false;
+  auto four = [&](int d, int g) { return f32x4{z.o[d][g * 4], z.o[d][g * 4 + 1], z.o[d][g * 4 + 2], z.o[d][g * 4 + 3]}; };
+  if (t.parts > 1) {
+    const int64_t at = part_at(a, t, t.split, i);
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) hand_over((f32x4 *)(a.part + at * D + d * 32 + g * 8 + z.hf * 4), four(d, g));
+    if (z.hf == 0) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(z.m, l));
+  } else {
+    const float f = one_over(qq, l, any_bad);
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) write_out<T>(a, qq, d * 32 + g * 8 + z.hf * 4, four(d, g) * f);
+    if (z.hf == 0) write_sums<T>(a, qq, z.m, l, any_bad);
+  }
+  return false;
 }
 
-template <int D>
+template <int D, int W>
+constexpr int few_bytes() {  // K and V of each wave; or the waves' join
+  return W * FEW_TILE * D * 4 > W * 16 * ((D + 4) * 4 + 8) ? W * FEW_TILE * D * 4 : W * 16 * ((D + 4) * 4 + 8);
+}
+template <int D, int QT>
 constexpr int lds_bytes() {
-  const int many_b = 4 * MANY_TILE * D * 2;    // K and V, twice
-  const int few_b = WAVES * FEW_TILE * D * 4;  // K and V of each wave; the waves' join is smaller
-  return many_b > few_b ? many_b : few_b;
+  return QT ? few_bytes<D, WAVES>() : std::max(RING * 2 * MANY_TILE * D * 2, few_bytes<D, MANY_WAVES>());
 }
 
-// MANY: tiles of MANY_Q queries; rows that have few in theirs take the other way all the same.
-template <typename T, int D, bool MANY>
-__global__ __launch_bounds__(THREADS, 2) void k_chunk(Args a) {
-  __shared__ __align__(16) char lds[lds_bytes<D>()];
+// Tiles of 16 QT queries, or of MANY_Q (QT = 0).
+template <typename T, int D, int QT>
+__global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chunk(Args a) {
+  __shared__ __align__(16) char lds[lds_bytes<D, QT>()];
   const int kv_heads = a.layer.kv_heads;
   uint32_t b = blockIdx.x;
   if (b == 0) {  // starts that decrease or leave the queries
     bool bad = false;
-    for (int i = threadIdx.x; i < a.ch.rows; i += THREADS) {
+    for (int i = threadIdx.x; i < a.ch.rows; i += blockDim.x) {
       const int s = a.ch.dev_starts[i], e = a.ch.dev_starts[i + 1];
       bad |= s < 0 || e < s || e > a.ch.tokens;
     }
@@ -664,15 +781,16 @@ __global__ __launch_bounds__(THREADS, 2) void k_chunk(Args a) {
   t.q0 = (int)q0;
   t.q1 = (int)min(n, q0 + a.tile_q);
   t.view = view_of(a, t.row, t.q0, t.q1);
-  const bool is_few = !MANY || t.q1 - t.q0 <= 2 * FEW_Q;
-  const uint32_t step = is_few ? WAVES * FEW_TILE : MANY_TILE;
+  constexpr uint32_t step = QT ? WAVES * FEW_TILE : MANY_TILE;
   const uint32_t steps = t.row.ok ? (t.view.total + step - 1) / step : 0;
   if (steps == 0) {  // nothing is seen, or the row is in error
     if (t.split) return;
     if (!t.row.ok && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
-    for (int j = threadIdx.x; j < (t.q1 - t.q0) * (D / 4); j += THREADS) {
+    for (int j = threadIdx.x; j < (t.q1 - t.q0) * (D / 4); j += blockDim.x) {
       Query q = query_of(a, t, j / (D / 4));
-      write_out<T>(a, q, j % (D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, 0.f, 0.f, !t.row.ok, j % (D / 4) == 0);
+      const float v = t.row.ok ? 0.f : NAN;
+      write_out<T>(a, q, j % (D / 4) * 4, f32x4{v, v, v, v});
+      if (j % (D / 4) == 0) write_sums<T>(a, q, 0.f, 0.f, !t.row.ok);
     }
     return;
   }
@@ -682,9 +800,12 @@ __global__ __launch_bounds__(THREADS, 2) void k_chunk(Args a) {
   if (t.split >= t.parts) return;
   t.x0 = (uint32_t)t.split * each * step;
   t.x1 = min(t.view.total, t.x0 + each * step);
-  if (!MANY || t.q1 - t.q0 <= FEW_Q) few<T, D, 1>(a, t, lds);
-  else if (is_few) few<T, D, 2>(a, t, lds);
-  else many<T, D>(a, t, lds);
+  if constexpr (QT) {
+    few<T, D, QT, WAVES>(a, t, 0, lds);
+  } else if (many<T, D>(a, t, lds)) {
+    for (int i = 0; i < t.q1 - t.q0; i += 16) few<T, D, 1, MANY_WAVES>(a, t, i, lds);
+  }
+  if (t.parts > 1) end_part<T, D>(a, t);
 }
 
 // ------------------------------------------------------------ weights
@@ -791,19 +912,21 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   // (1e-30: as flat as 0 is, and -infinity times it stays that)
   a.c = std::min(std::max(fabsf(ch.scale) * LOG2E, 1e-30f), FLT_MAX);
   a.flip = ch.scale < 0 ? 0x80008000u : 0;
+  a.window = ch.window ? (uint32_t)ch.window : UINT32_MAX;
   // with M = ceil(2^k / d), k = 31 + ceil(log2 d): token * M / 2^k is at most token / 2^31 < 1 / d above token / d
   while ((1 << a.page_shift) < layer.page_tokens) a.page_shift++;
   a.page_shift += 31;
   a.page_mul = (uint32_t)(((uint64_t(1) << a.page_shift) + layer.page_tokens - 1) / layer.page_tokens);
   const int64_t queries = (int64_t)ch.tokens * a.group;
-  a.tile_q = queries > (int64_t)FEW_Q * std::max(ch.rows, 1) ? MANY_Q : FEW_Q;
-  a.tile_shift = a.tile_q == MANY_Q ? 7 : 4;
+  const int64_t rows = std::max(ch.rows, 1);
+  a.tile_shift = queries <= 16 * rows ? 4 : queries <= 32 * rows ? 5 : 8;
+  a.tile_q = 1 << a.tile_shift;
   a.slots = (int)(queries >> a.tile_shift) + ch.rows;
   // Parts, so that about 1,024 workgroups have work if all rows are long; a tile takes as many as its length gives work for.
   const int64_t groups = (int64_t)a.slots * layer.kv_heads, longest = (int64_t)kv.table_cols * kv.page_tokens;
-  a.part_steps = a.tile_q == FEW_Q ? 2 : 4;
-  const int64_t steps = longest / ((a.tile_q == FEW_Q ? WAVES * FEW_TILE : MANY_TILE) * a.part_steps) + 1;
-  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(steps, 1024 / groups));
+  a.part_steps = a.tile_q == MANY_Q ? 4 : 2;
+  const int64_t steps = longest / ((a.tile_q == MANY_Q ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
+  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(steps, (a.tile_q == MANY_Q ? 256 : 1024) / groups));
   return a;
 }
 
@@ -827,8 +950,9 @@ size_t carve(Args &a, char *ws) {
 template <typename T, int D>
 hipError_t run(const Args &a, hipStream_t s) {
   const uint32_t blocks = (uint32_t)((int64_t)a.slots * a.layer.kv_heads * a.splits);
-  if (a.tile_q == MANY_Q) k_chunk<T, D, true><<<blocks, THREADS, 0, s>>>(a);
-  else k_chunk<T, D, false><<<blocks, THREADS, 0, s>>>(a);
+  if (a.tile_q == 16) k_chunk<T, D, 1><<<blocks, THREADS, 0, s>>>(a);
+  else if (a.tile_q == 32) k_chunk<T, D, 2><<<blocks, THREADS, 0, s>>>(a);
+  else k_chunk<T, D, 0><<<blocks, MANY_THREADS, 0, s>>>(a);
   if (a.ch.dev_weights) {
     const int64_t groups = (int64_t)a.ch.rows * a.layer.kv_heads;
     const int64_t longest = std::min<int64_t>((int64_t)a.kv.table_cols * a.kv.page_tokens, a.ch.weights_tokens);

@@ -8,6 +8,7 @@
 namespace hbf {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -22,6 +23,12 @@ struct Bf16 {
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
   }
+  // D[32 x 32] += A[32 x 16] B[16 x 32]: lane l holds A's row l % 32 and B's
+  // column l % 32 at k = 8 (l / 32) .. + 7, and of D's column l % 32 the rows
+  // 8 (i / 4) + 4 (l / 32) + i % 4, i < 16.
+  static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
 };
 struct Fp16 {
   typedef _Float16 elem;
@@ -29,6 +36,9 @@ struct Fp16 {
   typedef _Float16 x2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
   }
 };
 
@@ -131,6 +141,11 @@ __device__ __forceinline__ void to_lds(const void *from, uint32_t to) {
                : "memory", "m0");
 }
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All but the wave's last N are there.
+template <int N>
+__device__ __forceinline__ void loads_left() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
 // What the lanes of one wave have written to LDS is read by others of it: the
 // LDS serves a wave's accesses in order, so only the compiler is held.
