@@ -39,11 +39,15 @@ constexpr int RING = 4;        // staged tiles
 constexpr int MANY_Q = 256;    // queries of a tile there
 constexpr int MANY_WAVES = MANY_Q / 32, MANY_THREADS = 64 * MANY_WAVES;
 
+constexpr float LARGE = 1 << 22;  // of a score, times c: beyond, its rounding shows in exp2
+
 struct Args {
   hbf_kv kv;
   hbf_kv_layer layer;
   hbf_chunk ch;
   int group;          // query heads per KV head
+  uint32_t group_mul;  // query / group = query * group_mul >> group_shift, for queries below 2^31
+  int group_shift;
   float c;            // |scale| * log2(e), not 0
   uint32_t flip;      // sign bits of two 16-bit values if the scale is negative
   uint32_t window;    // of positions, or all of them
@@ -56,9 +60,13 @@ struct Args {
   float *part;        // [slots][kv_heads][splits][tile_q][head_dim] sums of p v
   float2 *part_ml;    // [slots][kv_heads][splits][tile_q] maximum (of q.k, its sign the scale's) and sum
   float2 *query_ml;   // [tokens][heads] the same of each query, 1 / sum; with weights only
+  float *part_w;      // [WEIGH_GROUPS][512] sums of a split's queries
   int32_t *status;
 };
 
+__device__ __forceinline__ int token_of(const Args &a, int query) {  // of a row's
+  return (int)((uint64_t)(uint32_t)query * a.group_mul >> a.group_shift);
+}
 __device__ __forceinline__ uint32_t page_index(const Args &a, uint32_t token) {
   return (uint32_t)((uint64_t)token * a.page_mul >> a.page_shift);
 }
@@ -114,8 +122,8 @@ struct View {
 };
 __device__ __forceinline__ View view_of(const Args &a, const Row &r, int q0, int q1) {
   View v;
-  v.p0 = r.len - r.n + q0 / a.group;
-  v.p1 = r.len - r.n + (q1 - 1) / a.group;
+  v.p0 = r.len - r.n + token_of(a, q0);
+  v.p1 = r.len - r.n + token_of(a, q1 - 1);
   v.first = v.lo = 0;
   if (a.ch.window > 0 && (int64_t)v.p0 - a.ch.window >= a.ch.sinks) {
     v.first = (uint32_t)a.ch.sinks;
@@ -214,7 +222,7 @@ struct Query {
 };
 __device__ __forceinline__ Query query_of(const Args &a, const Tile &t, int i) {
   if (!t.has(i)) return Query{0, -1, 0};
-  const int q = t.q0 + i, tok = q / a.group;
+  const int q = t.q0 + i, tok = token_of(a, q);
   return Query{t.row.start + tok, t.head * a.group + q - tok * a.group, t.row.len - t.row.n + tok};
 }
 
@@ -516,7 +524,7 @@ struct Many {
   int64_t at;       // bytes to the row of this lane's token of the group
   u32x4 qv[KS], p[2], kk[KS], vv[DT][2];
   f32x16 o[DT];
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, ref = 0.f, l = 0.f;
 
   __device__ __forceinline__ Many(const Args &a, const Tile &t, char *lds) : a(a), t(t), lds(lds) {
     lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 31, hf = lane >> 5;
@@ -622,8 +630,10 @@ struct Many {
 #pragma unroll 1
     for (int i = threadIdx.x * 16; i < TILE_BYTES; i += MANY_THREADS * 16) odd |= not_finite<T>(*(const u32x4 *)(vt + i));
   }
-  // The running maximum takes the scores in, as in softmax_step.  PENDING: of the
-  // step before, probabilities and values wait in p and vv; they are relative to the old maximum.
+  // The running maximum takes the scores in, as in softmax_step: a probability is
+  // exp2(s c + ref) with ref = SHIFT - m c, rounded; o and l are relative to ref as it is, so that its rounding
+  // cancels, but for scores so large that it passes exp2's range: these go the slow way.  PENDING: of the step
+  // before, probabilities and values wait in p and vv; they are relative to the old maximum.
   template <bool PENDING>
   __device__ __forceinline__ void maximum(const f32x16 &s) {
     float mx = s[0];
@@ -632,22 +642,27 @@ struct Many {
     if (__any((mx - m) * a.c > LAZY)) {  // (none seen, none here: NaN, false)
       if (PENDING) add_values();
       const float top = fmaxf(m, across_halves(mx, MAX_OP));
-      const float alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * a.c);
+      const float now = top == -INFINITY ? 0.f : fmaf(-top, a.c, SHIFT<T>);  // nothing seen yet: every p is exp2(-infinity)
+      odd |= fabsf(now) > LARGE;
+      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(now - ref);  // (0: nothing is summed yet)
       m = top;
+      ref = now;
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < DT; d++) o[d] *= alpha;
       if (PENDING) nothing_pending();
     }
   }
+  // What o and l are multiplied with to be relative to the maximum itself.
+  __device__ __forceinline__ float to_maximum() const {
+    return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fmaf(-m, a.c, SHIFT<T> - ref));
+  }
   // Of 16 tokens of the step, k = 0 or 1.
   __device__ __forceinline__ void probabilities(const f32x16 &s, int k) {
-    const float ref = m == -INFINITY ? 0.f : m;  // nothing seen yet: every p is 0
     float e[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      const float d = s[k * 8 + i] - ref;
-      e[i] = __builtin_amdgcn_exp2f(SHIFT<T> == 0.f ? d * a.c : fmaf(d, a.c, SHIFT<T>));
+      e[i] = __builtin_amdgcn_exp2f(fmaf(s[k * 8 + i], a.c, ref));
       l += e[i];
     }
     p[k] = u32x4{pack2<T>(e[0], e[1]), pack2<T>(e[2], e[3]), pack2<T>(e[4], e[5]), pack2<T>(e[6], e[7])};
@@ -668,7 +683,7 @@ struct Many {
     for (int z = 0; z < KS + 2 * DT; z++) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
       __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
     }
     if (!more) return;
@@ -725,7 +740,7 @@ __device__ __forceinline__ bool many(const Args &a, const Tile &t, char *lds) {
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
   const int i = z.w * 32 + z.col;
   const Query qq = query_of(a, t, i);
-  const float l = across_halves(z.l, SUM_OP);
+  const float fix = z.to_maximum(), l = across_halves(z.l, SUM_OP);
   if (qq.head < 0) return false;
   auto four = [&](int d, int g) { return f32x4{z.o[d][g * 4], z.o[d][g * 4 + 1], z.o[d][g * 4 + 2], z.o[d][g * 4 + 3]}; };
   if (t.parts > 1) {
@@ -733,15 +748,15 @@ __device__ __forceinline__ bool many(const Args &a, const Tile &t, char *lds) {
 #pragma unroll
     for (int d = 0; d < DT; d++)
 #pragma unroll
-      for (int g = 0; g < 4; g++) hand_over((f32x4 *)(a.part + at * D + d * 32 + g * 8 + z.hf * 4), four(d, g));
-    if (z.hf == 0) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(z.m, l));
+      for (int g = 0; g < 4; g++) hand_over((f32x4 *)(a.part + at * D + d * 32 + g * 8 + z.hf * 4), four(d, g) * fix);
+    if (z.hf == 0) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(z.m, l * fix));
   } else {
     const float f = one_over(qq, l, any_bad);
 #pragma unroll
     for (int d = 0; d < DT; d++)
 #pragma unroll
       for (int g = 0; g < 4; g++) write_out<T>(a, qq, d * 32 + g * 8 + z.hf * 4, four(d, g) * f);
-    if (z.hf == 0) write_sums<T>(a, qq, z.m, l, any_bad);
+    if (z.hf == 0) write_sums<T>(a, qq, z.m, l * fix, any_bad);
   }
   return false;
 }
@@ -902,6 +917,261 @@ __global__ __launch_bounds__(THREADS) void k_weigh(Args a, int blocks) {
   }
 }
 
+// The same for rows of many queries.  A workgroup holds 512 tokens' K in
+// registers, 64 a wave, and meets 64 queries at a time, which all waves read from
+// LDS.  A block's queries are cut into `splits` as far as the card has room; the last
+// split to finish adds their sums up, in order.
+constexpr int BLOCK = 64 * MANY_WAVES, Q_TILE = 64, Q_RING = 3;
+constexpr int WEIGH_GROUPS = 256;      // workgroups: one for each CU
+constexpr int WEIGH_ROWS = 512;        // most rows that it takes; more go the way of few queries
+
+template <typename T, int D>
+struct Weigh {
+  static constexpr int KS = D / 16, TILE_BYTES = Q_TILE * D * 2;
+  static constexpr int LANES = D / 8, AT_ONCE = 64 / LANES, NT = Q_TILE / MANY_WAVES, PASSES = NT / AT_ONCE;
+  const Args &a;
+  char *lds;
+  uint32_t lds0;
+  int lane, w, col, hf;
+  u32x4 kk[2][KS];
+  f32x16 sum[2];
+  uint32_t j0, j1;  // this wave's tokens
+  bool seen;
+
+  __device__ __forceinline__ Weigh(const Args &a, char *lds) : a(a), lds(lds) {
+    lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 31, hf = lane >> 5;
+    lds0 = lds_address(lds);
+  }
+  // K of the wave's tokens, by way of its own part of the LDS.
+  __device__ __forceinline__ void load_k(const int32_t *pages, int len, int head) {
+    View all;
+    all.first = all.lo = 0;
+    Places<D, 64> pl;
+    const uint32_t x1 = max(j1, j0 + 1), last = (uint32_t)len;  // (a wave without tokens reads some of the row's)
+    pl.find(a, all, pages, min(j0, last - 1), min(x1, last));
+    const int64_t at = pl.place(a, all, min(j0, last - 1), min(x1, last), head);
+    const uint32_t to = lds0 + w * 32 * D * 2;
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+#pragma unroll
+      for (int j = 0; j < 32 / AT_ONCE; j++) {
+        const int mine = j * AT_ONCE + lane / LANES;
+        to_lds((const char *)a.layer.dev_k + from_lane(at, t * 32 + mine) +
+                   (lane % LANES * 16 ^ (k_at<D>(mine, 0) - mine * (D * 2))), to + j * AT_ONCE * D * 2);
+      }
+      loads_done();
+#pragma unroll
+      for (int k = 0; k < KS; k++) kk[t][k] = *(const u32x4 *)(lds + w * 32 * D * 2 + k_at<D>(col, k * 2 + hf)) ^ a.flip;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before the next are on their way)
+    }
+  }
+  // Queries base .. of [.., q1) of the row (past them: the last one again) on their way to LDS.
+  __device__ __forceinline__ void stage(int start, int head, int base, int q1, int buf) {
+#pragma unroll
+    for (int j = 0; j < PASSES; j++) {
+      const int first = w * NT + j * AT_ONCE, mine = first + lane / LANES;
+      const int q = min(base + mine, q1 - 1), tok = token_of(a, q);
+      const char *row = (const char *)a.ch.dev_q +
+                        2 * ((start + tok) * a.ch.q_row_stride + (head * a.group + q - tok * a.group) * a.ch.q_head_stride);
+      to_lds(row + (lane % LANES * 16 ^ (k_at<D>(mine, 0) - mine * (D * 2))), lds0 + buf * TILE_BYTES + first * D * 2);
+    }
+  }
+  __device__ __forceinline__ float2 sums_of(int start, int head, int q, int q1) const {
+    if (q >= q1) return make_float2(0.f, 0.f);
+    const int tok = token_of(a, q);
+    return a.query_ml[(start + tok) * a.ch.heads + head * a.group + q - tok * a.group];
+  }
+  // 32 tokens' scores with the queries of qv.
+  __device__ __forceinline__ f32x16 scores(const u32x4 (&k)[KS], const u32x4 (&qv)[KS]) {
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; i++) s = T::mfma32(k[i], qv[i], s);
+    return s;
+  }
+  // Their weights exp2((s - m) c) / l, as ml = (-m c, 1 / l); of a tile that is not WHOLE, ml = (m, 1 / l), and only
+  // those whose bit (16 r + e) the lane's query sees.
+  template <bool WHOLE>
+  __device__ __forceinline__ void add(const f32x16 &s, int r, float2 ml, uint32_t sees) {
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      if (WHOLE) {
+        sum[r][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e], a.c, ml.x)), ml.y, sum[r][e]);
+      } else {
+        const float p = __builtin_amdgcn_exp2f((s[e] - ml.x) * a.c) * ml.y;
+        sum[r][e] += __int_as_float(__float_as_int(p) & __builtin_amdgcn_sbfe((int)sees, r * 16 + e, 1));
+      }
+    }
+  }
+  // Bits 0 .. n - 1.
+  static __device__ __forceinline__ uint64_t first_bits(int n) { return n <= 0 ? 0 : ~uint64_t(0) >> (64 - min(n, 64)); }
+  // What a query at `pos` sees of the wave's tokens, a bit for each of this lane's scores.
+  __device__ __forceinline__ uint32_t seen_bits(int pos) const {
+    const int behind = a.ch.window == 0 ? 0 : (int)max((int64_t)pos - a.ch.window + 1 - j0, (int64_t)0);  // tokens before the window
+    uint64_t v = first_bits(min(pos + 1, (int)j1) - (int)j0) & (~first_bits(behind) | first_bits(a.ch.sinks - (int)j0));
+    v >>= 4 * hf;  // scores of 4 tokens of each 8
+    auto pack = [](uint32_t x) {
+      x &= 0x0f0f0f0f;
+      x = (x | x >> 4) & 0x00ff00ff;
+      return (x | x >> 8) & 0xffff;
+    };
+    return pack((uint32_t)v) | pack((uint32_t)(v >> 32)) << 16;
+  }
+  // One staged tile: products of 32 tokens and 32 queries, each beside the vector units' work on the one before.
+  template <bool WHOLE>
+  __device__ __forceinline__ void tile(const char *qt, const float2 (&ml)[2], const uint32_t (&sees)[2]) {
+    u32x4 qv[KS];
+    auto read = [&](int u) {
+#pragma unroll
+      for (int k = 0; k < KS; k++) qv[k] = *(const u32x4 *)(qt + k_at<D>(u * 32 + col, k * 2 + hf));
+    };
+    read(0);
+    f32x16 x = scores(kk[0], qv);
+    f32x16 y = scores(kk[1], qv);
+    add<WHOLE>(x, 0, ml[0], sees[0]);
+    read(1);
+    x = scores(kk[0], qv);
+    add<WHOLE>(y, 1, ml[0], sees[0]);
+    y = scores(kk[1], qv);
+    add<WHOLE>(x, 0, ml[1], sees[1]);
+    add<WHOLE>(y, 1, ml[1], sees[1]);
+  }
+  // Queries q0 .. q1 - 1 of a row that starts at query `start`, at position p.
+  __device__ __forceinline__ void meet(int start, int p, int head, int q0, int q1) {
+    const int n = (q1 - q0 + Q_TILE - 1) / Q_TILE;
+    __syncthreads();  // (all are done with the LDS)
+    stage(start, head, q0, q1, 0);
+    if (n > 1) stage(start, head, q0 + Q_TILE, q1, 1);
+    float2 ml[2] = {sums_of(start, head, q0 + col, q1), sums_of(start, head, q0 + 32 + col, q1)};
+    for (int i = 0, buf = 0; i < n; i++, buf = buf + 1 == Q_RING ? 0 : buf + 1) {
+      const int base = q0 + i * Q_TILE, last = min(base + Q_TILE, q1) - 1;
+      float2 now[2] = {ml[0], ml[1]};
+      loads_done();
+      __syncthreads();
+      asm volatile("" : "+v"(now[0].x), "+v"(now[0].y), "+v"(now[1].x), "+v"(now[1].y));  // (waited for here, not behind the next loads)
+      if (i + 2 < n) stage(start, head, base + 2 * Q_TILE, q1, buf == 0 ? Q_RING - 1 : buf - 1);
+      if (i + 1 < n) {
+        ml[0] = sums_of(start, head, base + Q_TILE + col, q1);
+        ml[1] = sums_of(start, head, base + Q_TILE + 32 + col, q1);
+      }
+      const int pa = p + token_of(a, base), pb = p + token_of(a, last);  // positions of the first and the last
+      // (all that follows is of one wave: no barrier)
+      if (j0 >= j1 || (int)j0 > pb) continue;
+      if (a.ch.window > 0 && (int)j0 >= a.ch.sinks && (int64_t)j1 - 1 <= (int64_t)pa - a.ch.window) continue;
+      seen = true;
+      uint32_t sees[2] = {0, 0};
+      // where every query sees every token and none is to be left out, nothing is compared
+      const float far = fmaxf(fabsf(now[0].x), fabsf(now[1].x)) * a.c;
+      if (j1 - j0 == 64 && (int)j1 - 1 <= pa && !__any(now[0].y == 0.f || now[1].y == 0.f || far > LARGE) &&
+          (a.ch.window == 0 || (int)j1 <= a.ch.sinks || (int64_t)j0 > (int64_t)pb - a.ch.window)) {
+#pragma unroll
+        for (int u = 0; u < 2; u++) {  // -m c is rounded: what it is off by goes to the factor
+          const float ref = -now[u].x * a.c;
+          now[u].y *= __builtin_amdgcn_exp2f(-fmaf(now[u].x, a.c, ref));
+          now[u].x = ref;
+        }
+        tile<true>(lds + buf * TILE_BYTES, now, sees);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+          sees[u] = now[u].y == 0.f ? 0 : seen_bits(p + token_of(a, min(base + u * 32 + col, last)));
+        tile<false>(lds + buf * TILE_BYTES, now, sees);
+      }
+    }
+  }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(MANY_THREADS, 1) void k_weigh_many(Args a) {
+  using Z = Weigh<T, D>;
+  constexpr int LDS = Q_RING * Z::TILE_BYTES > MANY_WAVES * 32 * D * 2 ? Q_RING * Z::TILE_BYTES : MANY_WAVES * 32 * D * 2;
+  __shared__ __align__(16) char lds[LDS];
+  __shared__ int row_blocks[WEIGH_ROWS], slots[WEIGH_ROWS];
+  __shared__ uint32_t scan[MANY_THREADS / 64];
+  static_assert(WEIGH_ROWS == MANY_THREADS, "a row a thread");
+  const int kv_heads = a.layer.kv_heads;
+  // The blocks of rows whose slot no row before names.
+  int units, splits = 1;
+  {
+    const int i = threadIdx.x;
+    int mine = 0;
+    slots[i] = i < a.ch.rows ? a.ch.dev_slots[i] : -1;
+    __syncthreads();
+    if (i < a.ch.rows) {
+      const Row r = get_row(a, i);
+      mine = r.ok ? (int)(((uint32_t)r.len + BLOCK - 1) / BLOCK) : 0;
+      for (int j = 0; j < i; j++)
+        if (slots[j] == slots[i]) mine = 0;
+    }
+    uint32_t total;
+    row_blocks[i] = (int)block_scan<MANY_THREADS>((uint32_t)mine, &total, scan);
+    __syncthreads();
+    units = (int)min((uint64_t)total * kv_heads, (uint64_t)INT32_MAX / 64);
+    if (a.part_w) splits = max(1, min((int)gridDim.x / max(units, 1), 64));
+  }
+  for (int u = blockIdx.x; u < units * splits; u += gridDim.x) {
+    const int split = u / units, unit = u - split * units, head = unit % kv_heads, b = unit / kv_heads;
+    int i0 = 0;  // the last row whose first block is at most b
+    for (int hi = a.ch.rows; hi - i0 > 1;) {
+      const int mid = (i0 + hi) >> 1;
+      if (row_blocks[mid] <= b) i0 = mid; else hi = mid;
+    }
+    i0 = __builtin_amdgcn_readfirstlane(i0);
+    const int slot = __builtin_amdgcn_readfirstlane(slots[i0]);
+    const uint32_t base = (uint32_t)__builtin_amdgcn_readfirstlane(b - row_blocks[i0]) * BLOCK;
+    const int len = a.kv.dev_lens[slot];  // (in range, or the row has no blocks)
+    Z z(a, lds);
+    z.j0 = min(base + z.w * 64, (uint32_t)len);
+    z.j1 = min(base + z.w * 64 + 64, (uint32_t)len);
+    __syncthreads();  // (all are done with the LDS)
+    z.load_k(row_of(a.kv, a.kv.dev_tables, slot), len, head);
+#pragma unroll
+    for (int r = 0; r < 2; r++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) z.sum[r][e] = 0.f;
+    z.seen = false;
+    const int end = (int)min(base + BLOCK, (uint32_t)len);
+#pragma unroll 1
+    for (int i = i0; i < a.ch.rows; i++) {
+      if (__builtin_amdgcn_readfirstlane(slots[i]) != slot) continue;
+      int start = a.ch.dev_starts[i], n = a.ch.dev_starts[i + 1] - start;
+      if (start < 0 || n < 0 || n > a.ch.tokens || start > a.ch.tokens - n) n = 0;  // (refused elsewhere)
+      const int p = len - n;  // the first query's position
+      // the queries that may see one of the block's tokens
+      const int t0 = max(0, (int)base - p);
+      int t1 = n;
+      if (a.ch.window > 0 && (int)base >= a.ch.sinks) t1 = (int)min((int64_t)n, (int64_t)end - 1 + a.ch.window - p);
+      if (t0 >= t1) continue;
+      const int q0 = t0 * a.group, q1 = t1 * a.group;
+      const int each = ((q1 - q0 + Q_TILE - 1) / Q_TILE + splits - 1) / splits * Q_TILE;
+      if (split * each < q1 - q0) z.meet(start, p, head, q0 + split * each, min(q1, q0 + (split + 1) * each));
+    }
+    // a token's sum over the lanes that hold its scores; then every split's
+    float mine = 0.f;  // lane's of a half: the one of r = col / 16, e = col % 16
+#pragma unroll
+    for (int r = 0; r < 2; r++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const float v = sum_of_half(z.sum[r][e]);
+        mine = z.col == r * 16 + e ? v : mine;
+      }
+    float *out = a.ch.dev_weights + slot * a.ch.weights_slot_stride + head * a.ch.weights_head_stride;
+    const uint32_t at = z.col / 16 * 32 + z.col % 16 / 4 * 8 + z.hf * 4 + z.col % 4;
+    if (splits == 1) {
+      if (z.seen && z.j0 + at < z.j1) out[z.j0 + at] += mine;
+      continue;
+    }
+    hand_over(a.part_w + (int64_t)u * BLOCK + z.w * 64 + at, z.seen ? mine : 0.f);
+    stores_done();
+    if (!last_of(a.ch.dev_ctl + unit, (uint32_t)splits)) continue;
+    const uint32_t j = base + threadIdx.x;
+    float v = 0.f;
+    for (int k = 0; k < splits; k++) v += handed(a.part_w + ((int64_t)k * units + unit) * BLOCK + threadIdx.x);
+    if (j < (uint32_t)len && v != 0.f) out[j] += v;  // (NaN too; a token that nobody sees has 0)
+  }
+}
+
 // Sizes of a call.
 Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   Args a{};
@@ -913,10 +1183,15 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   a.c = std::min(std::max(fabsf(ch.scale) * LOG2E, 1e-30f), FLT_MAX);
   a.flip = ch.scale < 0 ? 0x80008000u : 0;
   a.window = ch.window ? (uint32_t)ch.window : UINT32_MAX;
-  // with M = ceil(2^k / d), k = 31 + ceil(log2 d): token * M / 2^k is at most token / 2^31 < 1 / d above token / d
-  while ((1 << a.page_shift) < layer.page_tokens) a.page_shift++;
-  a.page_shift += 31;
-  a.page_mul = (uint32_t)(((uint64_t(1) << a.page_shift) + layer.page_tokens - 1) / layer.page_tokens);
+  // with M = ceil(2^k / d), k = 31 + ceil(log2 d): x * M / 2^k is at most x / 2^31 < 1 / d above x / d
+  auto by = [](int d, uint32_t *mul, int *shift) {
+    for (*shift = 0; (1 << *shift) < d; ++*shift) {
+    }
+    *shift += 31;
+    *mul = (uint32_t)(((uint64_t(1) << *shift) + d - 1) / d);
+  };
+  by(layer.page_tokens, &a.page_mul, &a.page_shift);
+  by(a.group, &a.group_mul, &a.group_shift);
   const int64_t queries = (int64_t)ch.tokens * a.group;
   const int64_t rows = std::max(ch.rows, 1);
   a.tile_shift = queries <= 16 * rows ? 4 : queries <= 32 * rows ? 5 : 8;
@@ -943,7 +1218,10 @@ size_t carve(Args &a, char *ws) {
     a.part = (float *)take(n * a.layer.head_dim * 4);
     a.part_ml = (float2 *)take(n * 8);
   }
-  if (a.ch.dev_weights) a.query_ml = (float2 *)take((size_t)a.ch.tokens * a.ch.heads * 8);
+  if (a.ch.dev_weights) {
+    a.query_ml = (float2 *)take((size_t)a.ch.tokens * a.ch.heads * 8);
+    if (a.tile_q == MANY_Q && a.ch.dev_ctl) a.part_w = (float *)take((size_t)WEIGH_GROUPS * BLOCK * 4);
+  }
   return std::max(o, size_t(256));
 }
 
@@ -956,6 +1234,10 @@ hipError_t run(const Args &a, hipStream_t s) {
   if (a.ch.dev_weights) {
     const int64_t groups = (int64_t)a.ch.rows * a.layer.kv_heads;
     const int64_t longest = std::min<int64_t>((int64_t)a.kv.table_cols * a.kv.page_tokens, a.ch.weights_tokens);
+    if (a.tile_q == MANY_Q && a.ch.rows <= WEIGH_ROWS) {
+      k_weigh_many<T, D><<<WEIGH_GROUPS, MANY_THREADS, 0, s>>>(a);
+      return hipGetLastError();
+    }
     const int64_t most = longest / (WAVES * WEIGH_TILE) + 1;
     const int each = (int)std::max<int64_t>(1, std::min<int64_t>(most, 4096 / groups));
     k_weigh<T, D><<<(uint32_t)(groups * each), THREADS, 0, s>>>(a, each);
