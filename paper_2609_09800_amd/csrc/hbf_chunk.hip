@@ -171,7 +171,7 @@ __device__ __forceinline__ int64_t from_lane(int64_t v, int lane) {
   return (int64_t)((uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32 | (uint32_t)__shfl((int)v, lane));
 }
 
-template <int D, int NT>
+template <int D, int NT, bool V = true>
 struct Stage : Places<D, NT> {
   using P = Places<D, NT>;
   u32x4 k[P::PASSES], v[P::PASSES];
@@ -182,8 +182,9 @@ struct Stage : Places<D, NT> {
 #pragma unroll
     for (int j = 0; j < P::PASSES; j++) {
       const int64_t mine = from_lane(at, j * P::AT_ONCE + lane / P::LANES) + lane % P::LANES * 16;
-      k[j] = *(const u32x4 *)((const char *)a.layer.dev_k + mine);
-      v[j] = *(const u32x4 *)((const char *)a.layer.dev_v + mine);
+      // (past the caches' order: one tile holds all of a row's queries as a rule, and nobody else reads them)
+      k[j] = __builtin_nontemporal_load((const u32x4 *)((const char *)a.layer.dev_k + mine));
+      if (V) v[j] = __builtin_nontemporal_load((const u32x4 *)((const char *)a.layer.dev_v + mine));
     }
   }
   // To tiles of K and V.  What lies behind the last token may be anything: 0 * NaN
@@ -194,7 +195,7 @@ struct Stage : Places<D, NT> {
     for (int j = 0; j < P::PASSES; j++) {
       const int t = j * P::AT_ONCE + lane / P::LANES;
       *(u32x4 *)(kt + k_at<D>(t, lane % P::LANES)) = k[j];
-      *(u32x4 *)(vt + v_at<D>(t, lane % P::LANES)) = x + t < x1 ? v[j] : u32x4{0, 0, 0, 0};
+      if (V) *(u32x4 *)(vt + v_at<D>(t, lane % P::LANES)) = x + t < x1 ? v[j] : u32x4{0, 0, 0, 0};
     }
   }
 };
@@ -825,95 +826,130 @@ __global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chu
 
 // ------------------------------------------------------------ weights
 
-// What a row's queries gave each token: a wave takes 64 tokens, as the rows of the
-// operand, in registers, and meets 16 queries at a time; the sums of a token stay
-// in the four lanes that hold its scores until the end.  A slot's rows are taken
+// What a row's queries gave each token: a wave takes 32 tokens at a time, through LDS of
+// its own, the next ones on their way, and meets 16 queries at a time; a token's
+// sum over the lanes that hold its scores is taken once.  A slot's rows are taken
 // by the first of them, one after another.
-constexpr int WEIGH_TILE = 64;
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS) void k_weigh(Args a, int blocks) {
-  constexpr int KS = D / 32, U = WEIGH_TILE / 16;
+__global__ __launch_bounds__(THREADS, 3) void k_weigh(Args a, int blocks) {
+  constexpr int KS = D / 32, NT = FEW_TILE;
+  __shared__ __align__(16) char lds[WAVES * NT * D * 2];
+  __shared__ int after;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   int b = blockIdx.x;
   const int head = b % a.layer.kv_heads;
   b /= a.layer.kv_heads;
   const int i0 = b % a.ch.rows, block = b / a.ch.rows;
   const int slot = a.ch.dev_slots[i0];
+  if (threadIdx.x == 0) after = i0;
   bool before = false;
-  for (int j = threadIdx.x; j < i0; j += THREADS) before |= a.ch.dev_slots[j] == slot;
+  int last = i0;
+  for (int j = threadIdx.x; j < a.ch.rows; j += THREADS)
+    if (a.ch.dev_slots[j] == slot) {
+      before |= j < i0;
+      last = max(last, j);
+    }
   if (__syncthreads_or(before)) return;
+  if (last > i0) atomicMax(&after, last);
+  __syncthreads();
+  last = __builtin_amdgcn_readfirstlane(after);
   const Row first = get_row(a, i0);
   if (!first.ok) return;
+  const uint32_t len = (uint32_t)first.len, step = (uint32_t)blocks * WAVES * NT;
+  char *kt = lds + w * NT * D * 2;
+  float *out = a.ch.dev_weights + slot * a.ch.weights_slot_stride + head * a.ch.weights_head_stride;
   View all;
   all.first = all.lo = 0;
-  all.total = first.len;
-  for (uint32_t j0 = ((uint32_t)block * WAVES + w) * WEIGH_TILE; j0 < (uint32_t)first.len;
-       j0 += (uint32_t)blocks * WAVES * WEIGH_TILE) {
-    const uint32_t j1 = min(j0 + WEIGH_TILE, (uint32_t)first.len);
-    Places<D, WEIGH_TILE> pl;
-    pl.find(a, all, first.pages, j0, j1);
-    const int64_t at = pl.place(a, all, j0, j1, head);
-    u32x4 kk[U][KS];
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const char *p = (const char *)a.layer.dev_k + from_lane(at, u * 16 + col) + kg * 16;
-#pragma unroll
-      for (int k = 0; k < KS; k++) kk[u][k] = *(const u32x4 *)(p + k * 64);
+  all.total = len;
+  // The queries, 16 of a row from q0 on: theirs of this lane's column, and the row's own.
+  struct Queries {
+    u32x4 v[KS];
+    float2 ml;
+    int pos;
+  };
+  auto load = [&](const Tile &t, int q0) {
+    Queries z;
+    const Query q = query_of(a, t, q0 + col);
+    load_query<T, D>(a, q, kg, z.v);
+    z.ml = q.head < 0 ? make_float2(0.f, 0.f) : a.query_ml[(int64_t)q.token * a.ch.heads + q.head];
+    z.pos = q.pos;
+    return z;
+  };
+  auto tile_of = [&](int i) {
+    Tile t;
+    t.row = get_row(a, i);
+    t.head = head;
+    t.q0 = 0;
+    t.q1 = t.row.n * a.group;
+    return t;
+  };
+  const Tile own = tile_of(i0);
+  const bool one = last == i0 && own.q1 <= 16;  // as a rule: they are loaded once
+  Queries mine = load(own, 0);
+  uint32_t x = ((uint32_t)block * WAVES + w) * NT;
+  if (x >= len) return;  // (a whole wave; no barrier follows)
+  Stage<D, NT, false> st;
+  st.find(a, all, first.pages, x, len);
+  st.load(a, all, x, len, head);
+  st.find(a, all, first.pages, min(x + step, len - 1), len);
+  while (true) {
+    const bool more = len - x > step;
+    const uint32_t x1 = min(x + NT, len);
+    // lane col < 8 of a group of 16 answers for token x + 16 (col / 4) + 4 kg + col % 4
+    const uint32_t at = x + (col >> 2 & 1) * 16 + kg * 4 + (col & 3);
+    const bool writes = col < 8 && at < x1;
+    const float old = writes ? out[at] : 0.f;
+    st.store(kt, nullptr, x, len);
+    wave_lds_fence();
+    if (more) {
+      st.load(a, all, x + step, len, head);
+      st.find(a, all, first.pages, min(x + 2 * step, len - 1), len);
     }
-    f32x4 sum[U];
-#pragma unroll
-    for (int u = 0; u < U; u++) sum[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 sum[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     bool seen = false;
-    for (int i = i0; i < a.ch.rows; i++) {
-      if (a.ch.dev_slots[i] != slot) continue;
-      Tile t;
-      t.row = get_row(a, i);
-      t.head = head;
-      const int p = t.row.len - t.row.n;  // the first query's position
-      // tokens [t0, t1) may see one of these
-      int t0 = max(0, (int)j0 - p), t1 = t.row.n;
-      if (a.ch.window > 0 && (int)j0 >= a.ch.sinks) t1 = (int)min((int64_t)t1, (int64_t)j1 - 1 + a.ch.window - p);
-      if (t0 >= t1) continue;
-      t.q0 = t0 * a.group;
-      t.q1 = t1 * a.group;
-      // where every query sees every token, no positions are compared
-      const bool whole = j1 - j0 == WEIGH_TILE && (int)j1 - 1 <= p + t0 &&
-                         (a.ch.window == 0 || (int)j1 <= a.ch.sinks || (int)j0 > p + t1 - 1 - a.ch.window);
-      seen = true;
-      for (int q0 = 0; q0 < t.q1 - t.q0; q0 += 16) {
-        const Query q = query_of(a, t, q0 + col);
-        u32x4 qv[KS];
-        load_query<T, D>(a, q, kg, qv);
-        const float2 ml = q.head < 0 ? make_float2(0.f, 0.f) : a.query_ml[(int64_t)q.token * a.ch.heads + q.head];
-        f32x4 s[U];
+    auto meet = [&](const Queries &z) {
+      f32x4 s[2];
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-          s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < 2; u++) {
+        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int k = 0; k < KS; k++) s[u] = T::mfma(kk[u][k], qv[k], s[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const int token = (int)j0 + u * 16 + kg * 4 + j;
-            const bool skip = ml.y == 0.f || (!whole && (token >= (int)j1 || !sees(a, q.pos, token)));
-            sum[u][j] += skip ? 0.f : __builtin_amdgcn_exp2f((s[u][j] - ml.x) * a.c) * ml.y;
-          }
+        for (int k = 0; k < KS; k++) s[u] = T::mfma(*(const u32x4 *)(kt + k_at<D>(u * 16 + col, k * 4 + kg)), z.v[k], s[u]);
       }
-    }
-    if (!seen) continue;
-    float *out = a.ch.dev_weights + slot * a.ch.weights_slot_stride + head * a.ch.weights_head_stride;
 #pragma unroll
-    for (int u = 0; u < U; u++)
+      for (int u = 0; u < 2; u++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const uint32_t j = x + u * 16 + kg * 4 + i;
+          const float p = __builtin_amdgcn_exp2f((s[u][i] - z.ml.x) * a.c) * z.ml.y;
+          sum[u][i] += (z.ml.y != 0.f) & (j < x1) & sees(a, z.pos, (int)j) ? p : 0.f;
+        }
+    };
+    for (int i = i0; i <= last; i++) {
+      if (i > i0 && a.ch.dev_slots[i] != slot) continue;
+      const Tile t = i == i0 ? own : tile_of(i);
+      const int p = t.row.len - t.row.n;  // the first query's position
+      // queries of tokens [t0, t1) may see one of these
+      const int t0 = max(0, (int)x - p);
+      int t1 = t.row.n;
+      if (a.ch.window > 0 && (int)x >= a.ch.sinks) t1 = (int)min((int64_t)t1, (int64_t)x1 - 1 + a.ch.window - p);
+      if (t0 >= t1) continue;
+      seen = true;
+      if (one) meet(mine);
+      else
+        for (int q0 = t0 * a.group & ~15; q0 < t1 * a.group; q0 += 16) meet(load(t, q0));
+    }
+    float v = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; u++)
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        float v = sum[u][i];
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) v += __shfl_xor(v, d);
-        const uint32_t j = j0 + u * 16 + kg * 4 + i;
-        if (col == 0 && j < j1) out[j] += v;
+        const float all16 = sum_of_row(sum[u][i]);
+        v = col == u * 4 + i ? all16 : v;
       }
+    if (writes && seen) out[at] = old + v;
+    wave_lds_fence();
+    if (!more) break;
+    x += step;
   }
 }
 
@@ -1194,14 +1230,18 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   by(a.group, &a.group_mul, &a.group_shift);
   const int64_t queries = (int64_t)ch.tokens * a.group;
   const int64_t rows = std::max(ch.rows, 1);
-  a.tile_shift = queries <= 16 * rows ? 4 : queries <= 32 * rows ? 5 : 8;
+  const int64_t longest = (int64_t)kv.table_cols * kv.page_tokens;
+  // Small calls of many queries: their tiles of 256, in parts of 256 tokens, leave most of the card idle.
+  const bool idle = ((queries >> 8) + ch.rows) * layer.kv_heads * (longest / 256 + 1) < 256;
+  a.tile_shift = queries <= 16 * rows ? 4 : queries <= 32 * rows || idle ? 5 : 8;
   a.tile_q = 1 << a.tile_shift;
   a.slots = (int)(queries >> a.tile_shift) + ch.rows;
-  // Parts, so that about 1,024 workgroups have work if all rows are long; a tile takes as many as its length gives work for.
-  const int64_t groups = (int64_t)a.slots * layer.kv_heads, longest = (int64_t)kv.table_cols * kv.page_tokens;
+  // Parts, so that a card's worth of workgroups have work if all rows are long, twice that where rows of different
+  // lengths have to be packed; a tile takes as many as its length gives work for.
+  const int64_t groups = (int64_t)a.slots * layer.kv_heads;
   a.part_steps = a.tile_q == MANY_Q ? 4 : 2;
   const int64_t steps = longest / ((a.tile_q == MANY_Q ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
-  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(steps, (a.tile_q == MANY_Q ? 256 : 1024) / groups));
+  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(steps, (a.tile_q == MANY_Q ? 256 : groups < 128 ? 512 : 1024) / groups));
   return a;
 }
 
@@ -1238,8 +1278,8 @@ hipError_t run(const Args &a, hipStream_t s) {
       k_weigh_many<T, D><<<WEIGH_GROUPS, MANY_THREADS, 0, s>>>(a);
       return hipGetLastError();
     }
-    const int64_t most = longest / (WAVES * WEIGH_TILE) + 1;
-    const int each = (int)std::max<int64_t>(1, std::min<int64_t>(most, 4096 / groups));
+    const int64_t most = longest / (WAVES * FEW_TILE) + 1;
+    const int each = (int)std::max<int64_t>(1, std::min<int64_t>(most, 2048 / groups));
     k_weigh<T, D><<<(uint32_t)(groups * each), THREADS, 0, s>>>(a, each);
   }
   return hipGetLastError();

@@ -29,6 +29,7 @@ struct Args {
   hbf_eviction ev;
   KvCtl *ctl;
   int layers, moves;   // workgroups of the moves per layer, entry and head
+  int lasts;           // of the last tokens, per plane and entry
   int64_t head_bytes;
 };
 
@@ -61,58 +62,84 @@ __device__ __forceinline__ uint32_t key_of(float w) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// The k-th largest key (k >= 1) of the n weights, and how many equal ones are among the k.
-__device__ uint32_t kth_key(const float *w, int n, uint32_t k, uint32_t *equal) {
-  __shared__ uint32_t bins[256], found, rest;
+// The k-th largest (k >= 1) of the workgroup's keys, and how many equal ones are
+// among the k.  each(f): f(key) for the thread's own.
+template <typename F>
+__device__ uint32_t kth_key(F each, uint32_t k, uint32_t *equal) {
+  __shared__ uint32_t bins[256], found, rest, lds[WAVES];
+  static_assert(THREADS == 256, "a bin a thread");
   uint32_t prefix = 0;
 #pragma unroll 1
   for (int shift = 24; shift >= 0; shift -= 8) {
     bins[threadIdx.x] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-      const uint32_t key = key_of(w[i]);
+    each([&](uint32_t key) {
       if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&bins[key >> shift & 255], 1u);
-    }
+    });
     __syncthreads();
-    // the bin that holds it: those above have fewer than k, with it at least k
-    uint32_t c = bins[255 - threadIdx.x];
-    const uint32_t mine = c;
-    __shared__ uint32_t waves[WAVES];
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t y = __shfl_up(c, d);
-      if ((int)(threadIdx.x & 63) >= d) c += y;
-    }
-    if ((threadIdx.x & 63) == 63) waves[threadIdx.x >> 6] = c;
-    __syncthreads();
-    for (int i = 0; i < (int)(threadIdx.x >> 6); i++) c += waves[i];
-    if (c >= k && c - mine < k) {
+    // the bin that holds it, from the highest down: those above have fewer than k, with it at least k
+    uint32_t total;
+    const uint32_t mine = bins[255 - threadIdx.x], before = block_scan<THREADS>(mine, &total, lds);
+    if (before < k && before + mine >= k) {
       found = 255 - threadIdx.x;
-      rest = k - (c - mine);
+      rest = k - before;
     }
     __syncthreads();
     prefix = prefix << 8 | found;
     k = rest;
-    __syncthreads();
   }
   *equal = k;
   return prefix;
 }
 
-// One layer's and head's choice for entry i: dev_kept.
-__device__ void choose(const Args &a, const Entry &e, int layer, int i, int head) {
-  int32_t *kept = kept_of(a, layer, i, head);
-  const int t = threadIdx.x, end = e.cut ? e.keep : e.len;
-  for (int j = t; j < a.ev.max_keep; j += THREADS) {
-    if (j >= end) kept[j] = -1;
-    else if (!e.cut || j < a.ev.sinks) kept[j] = j;
-    else if (j >= e.keep - a.ev.recent) kept[j] = j + (e.len - e.keep);
+// The choice between s0 and mid, of which m - s0 stay: up to FEW_KEYS weights are
+// read once, into registers, 16 neighbours a thread.
+constexpr int KEYS = 16, FEW_KEYS = THREADS * KEYS;
+__device__ void choose_few(const float *w, int s0, int m, int mid, int32_t *kept) {
+  __shared__ uint32_t lds[WAVES];
+  __shared__ int32_t holes[FEW_KEYS / 2];  // (as many as movers)
+  const int first = s0 + threadIdx.x * KEYS, n = min(max(mid - first, 0), KEYS);
+  uint32_t key[KEYS], equal, total;
+#pragma unroll
+  for (int u = 0; u < KEYS; u++) key[u] = key_of(w[min(first + u, mid - 1)]);
+  const uint32_t least = kth_key([&](auto f) {
+#pragma unroll
+    for (int u = 0; u < KEYS; u++)
+      if (u < n) f(key[u]);
+  }, (uint32_t)(m - s0), &equal);
+  uint32_t ties = 0, in = 0, count = 0;
+#pragma unroll
+  for (int u = 0; u < KEYS; u++) ties += u < n && key[u] == least;
+  uint32_t rank = block_scan<THREADS>(ties, &total, lds);
+  // movers before this thread's in the high half, free places in the low one
+#pragma unroll
+  for (int u = 0; u < KEYS; u++) {
+    const bool tie = key[u] == least, chosen = u < n && (key[u] > least || (tie && rank < equal));
+    rank += u < n && tie;
+    in |= (uint32_t)chosen << u;
+    if (u < n) count += first + u < m ? !chosen : (uint32_t)chosen << 16;
   }
-  const int s0 = a.ev.sinks, m = e.keep - a.ev.recent, mid = e.len - a.ev.recent;
-  if (!e.cut || m == s0) return;
-  const float *w = a.ev.dev_weights + weights_at(a, layer, e.slot, head);
+  const uint32_t before = block_scan<THREADS>(count, &total, lds);
+  uint32_t hole = before & 0xffff, mover = before >> 16;
+#pragma unroll
+  for (int u = 0; u < KEYS; u++) {
+    if (u >= n || first + u >= m) continue;
+    if (in >> u & 1) kept[first + u] = first + u;
+    else holes[hole++] = first + u;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < KEYS; u++)
+    if (u < n && first + u >= m && (in >> u & 1)) kept[holes[mover++]] = first + u;
+}
+
+// The same for any number, read anew by each step.
+__device__ void choose_many(const float *w, int s0, int m, int mid, int32_t *kept) {
+  const int t = threadIdx.x;
   uint32_t equal;
-  const uint32_t least = kth_key(w + s0, mid - s0, (uint32_t)(m - s0), &equal);
+  const uint32_t least = kth_key([&](auto f) {
+    for (int i = s0 + t; i < mid; i += THREADS) f(key_of(w[i]));
+  }, (uint32_t)(m - s0), &equal);
   // In position order: those above the least, and the first `equal` of those equal to it.
   __shared__ uint32_t lds[WAVES];
   __shared__ int32_t holes[HOLES];
@@ -161,6 +188,22 @@ __device__ void choose(const Args &a, const Entry &e, int layer, int i, int head
     });
     __syncthreads();
   }
+}
+
+// One layer's and head's choice for entry i: dev_kept.
+__device__ void choose(const Args &a, const Entry &e, int layer, int i, int head) {
+  int32_t *kept = kept_of(a, layer, i, head);
+  const int end = e.cut ? e.keep : e.len;
+  for (int j = threadIdx.x; j < a.ev.max_keep; j += THREADS) {
+    if (j >= end) kept[j] = -1;
+    else if (!e.cut || j < a.ev.sinks) kept[j] = j;
+    else if (j >= e.keep - a.ev.recent) kept[j] = j + (e.len - e.keep);
+  }
+  const int s0 = a.ev.sinks, m = e.keep - a.ev.recent, mid = e.len - a.ev.recent;
+  if (!e.cut || m == s0) return;
+  const float *w = a.ev.dev_weights + weights_at(a, layer, e.slot, head);
+  if (mid - s0 <= FEW_KEYS) choose_few(w, s0, m, mid, kept);
+  else choose_many(w, s0, m, mid, kept);
 }
 
 // Workgroups 0 .. n-1 check a row each, the next one that no slot is listed twice;
@@ -261,49 +304,59 @@ __global__ __launch_bounds__(THREADS) void k_evict_move(Args a) {
   }
 }
 
-// The last tokens of one plane, all heads together, and (beside the planes) a
-// layer's weights of them and behind.
+// The last tokens: of one plane, all heads together, LAST_BYTES a workgroup where
+// the new places are before the old ones, and else by one workgroup, some at a
+// time from the front.  And, a workgroup a head, a layer's weights of them and behind.
+constexpr int LAST_U = 8, LAST_BYTES = THREADS * LAST_U * 16;
 __global__ __launch_bounds__(THREADS) void k_evict_last(Args a) {
   if (!a.ctl->go) return;
   int b = blockIdx.x;
-  const int what = b % 3;  // K, V, weights
-  b /= 3;
+  const int each = 2 * a.lasts + a.ev.kv_heads, what = b % each;  // K's parts, V's, weights
+  b /= each;
   const int i = b % a.ev.n, layer = b / a.ev.n;
   const Entry e = get_entry(a, i);
   if (!e.cut) return;
   const int m = e.keep - a.ev.recent, by = e.len - e.keep;
-  if (what == 2) {
-    for (int head = 0; head < a.ev.kv_heads; head++) {
-      const int64_t wat = weights_at(a, layer, e.slot, head);
-      for (int j0 = m; j0 < e.len; j0 += THREADS) {  // (place j + by is read before any later step writes it)
-        const int j = j0 + threadIdx.x;
-        const float v = j < e.keep ? a.ev.dev_weights[wat + j + by] : 0.f;
+  if (what >= 2 * a.lasts) {
+    const int64_t wat = weights_at(a, layer, e.slot, what - 2 * a.lasts);
+    const float *from = a.ev.dev_weights + wat;
+    float *to = a.ev.dev_weights_out + wat;
+    const bool over = to == from;  // (then place j + by, which becomes something else in this step or a later one, is read first)
+    for (int j0 = m; j0 < e.len; j0 += THREADS) {
+      const int j = j0 + threadIdx.x;
+      const float v = j < e.keep ? from[j + by] : 0.f;
+      if (over) {
         loads_done();
         __syncthreads();
-        if (j < e.len) a.ev.dev_weights_out[wat + j] = v;
-        __syncthreads();
       }
+      if (j < e.len) to[j] = v;
     }
     return;
   }
-  char *plane = (char *)a.kv.dev_pool + (uint64_t)(2 * layer + what) * a.kv.plane_stride;
+  const int kv = what / a.lasts, part = what % a.lasts;
+  char *plane = (char *)a.kv.dev_pool + (uint64_t)(2 * layer + kv) * a.kv.plane_stride;
   const int32_t *row = row_of(a.kv, a.kv.dev_tables, e.slot);
   const uint32_t pieces = (uint32_t)(a.kv.token_bytes / 16);
   const uint64_t all = (uint64_t)a.ev.recent * pieces;
-  constexpr int U = 8;
-  for (uint64_t x0 = 0; x0 < all; x0 += THREADS * U) {
-    u32x4 v[U];
+  const bool over = by < a.ev.recent;
+  if (over && part) return;
+  for (uint64_t x0 = (uint64_t)part * THREADS * LAST_U; x0 < all; x0 += (uint64_t)(over ? 1 : a.lasts) * THREADS * LAST_U) {
+    const int j0 = (int)(x0 / pieces);  // the first piece is `rest` of token j0
+    const uint32_t rest = (uint32_t)(x0 - (uint64_t)j0 * pieces);
+    u32x4 v[LAST_U];
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const uint64_t x = x0 + u * THREADS + threadIdx.x;
-      if (x < all) v[u] = *(const u32x4 *)(plane + token_at(a, row, m + by + (int)(x / pieces)) + x % pieces * 16);
+    for (int u = 0; u < LAST_U; u++) {
+      const uint32_t x = rest + u * THREADS + threadIdx.x, j = x / pieces;
+      if (x0 + x - rest < all) v[u] = *(const u32x4 *)(plane + token_at(a, row, m + by + j0 + (int)j) + (x - j * pieces) * 16);
     }
-    loads_done();  // (of every wave, before any stores: the barrier waits for no memory)
-    __syncthreads();
+    if (over) {
+      loads_done();  // (of every wave, before any stores: the barrier waits for no memory)
+      __syncthreads();
+    }
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const uint64_t x = x0 + u * THREADS + threadIdx.x;
-      if (x < all) *(u32x4 *)(plane + token_at(a, row, m + (int)(x / pieces)) + x % pieces * 16) = v[u];
+    for (int u = 0; u < LAST_U; u++) {
+      const uint32_t x = rest + u * THREADS + threadIdx.x, j = x / pieces;
+      if (x0 + x - rest < all) *(u32x4 *)(plane + token_at(a, row, m + j0 + (int)j) + (x - j * pieces) * 16) = v[u];
     }
   }
 }
@@ -336,7 +389,9 @@ hipError_t launch_kv_evict(const hbf_kv &kv, const hbf_eviction &ev, hipStream_t
   a.moves = (int)std::max<int64_t>(1, std::min<int64_t>((ev.max_keep + MOVE_TILE - 1) / MOVE_TILE, (1 << 14) / groups));
   k_evict_plan<<<(uint32_t)(ev.n + 1 + groups), THREADS, (size_t)((kv.slots + 31) / 32) * 4, s>>>(a);
   k_evict_move<<<(uint32_t)(groups * a.moves), THREADS, 0, s>>>(a);
-  k_evict_last<<<(uint32_t)((int64_t)a.layers * ev.n * 3), THREADS, 0, s>>>(a);
+  const int64_t entries = (int64_t)a.layers * ev.n, bytes = (int64_t)ev.recent * kv.token_bytes;
+  a.lasts = (int)std::max<int64_t>(1, std::min<int64_t>((bytes + LAST_BYTES - 1) / LAST_BYTES, (1 << 14) / entries));
+  k_evict_last<<<(uint32_t)(entries * (2 * a.lasts + ev.kv_heads)), THREADS, 0, s>>>(a);
   k_evict_end<<<(uint32_t)ev.n, THREADS, 0, s>>>(a);
   return hipGetLastError();
 }

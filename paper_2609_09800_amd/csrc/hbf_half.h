@@ -76,19 +76,23 @@ __device__ __forceinline__ V across_wave(V x, F op) {
   return __builtin_bit_cast(V, u);
 }
 
-// The sum over each half of the wave, in its lanes.
-__device__ __forceinline__ float sum_of_half(float x) {
+// The sum over each 16 lanes of the wave, in each of them; over each half of it.
+__device__ __forceinline__ float sum_of_row(float x) {
   uint32_t u = __builtin_bit_cast(uint32_t, x);
-  auto join = [&](uint32_t a, uint32_t b) {
-    u = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+  auto join = [&](uint32_t b) {
+    u = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, u) + __builtin_bit_cast(float, b));
   };
-  join(u, __builtin_amdgcn_update_dpp(0, u, 0xb1, 0xf, 0xf, true));   // quad_perm 1,0,3,2
-  join(u, __builtin_amdgcn_update_dpp(0, u, 0x4e, 0xf, 0xf, true));   // quad_perm 2,3,0,1
-  join(u, __builtin_amdgcn_update_dpp(0, u, 0x141, 0xf, 0xf, true));  // row_half_mirror
-  join(u, __builtin_amdgcn_update_dpp(0, u, 0x140, 0xf, 0xf, true));  // row_mirror
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  join(a[0], a[1]);
+  join(__builtin_amdgcn_update_dpp(0, u, 0xb1, 0xf, 0xf, true));   // quad_perm 1,0,3,2
+  join(__builtin_amdgcn_update_dpp(0, u, 0x4e, 0xf, 0xf, true));   // quad_perm 2,3,0,1
+  join(__builtin_amdgcn_update_dpp(0, u, 0x141, 0xf, 0xf, true));  // row_half_mirror
+  join(__builtin_amdgcn_update_dpp(0, u, 0x140, 0xf, 0xf, true));  // row_mirror
   return __builtin_bit_cast(float, u);
+}
+__device__ __forceinline__ float sum_of_half(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, sum_of_row(x));
+  const auto both = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t a = both[0], b = both[1];
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
 }
 
 // op over the four lanes that hold the same column of a tile (l % 16), in each of them.
