@@ -190,14 +190,337 @@ CASES = [
 ]
 
 
+
+# Tables that could hold far more: calls of many queries are then cut into tiles of 256, and else, so small, of 32.
+@pytest.mark.parametrize("cols", [0, 5000])
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
-def test_against_64_bits(torch, case, dtype):
+def test_against_64_bits(torch, case, dtype, cols):
     heads, kv_heads, dim, new, lens, page, window, sinks = case
-    say(f"attention {case} {dtype}")
-    b = Batch(torch, heads, kv_heads, dim, new, lens, page, dtype, seed=sum(lens), tail=2, head=1)
+    say(f"attention {case} {dtype} {cols}")
+    b = Batch(torch, heads, kv_heads, dim, new, lens, page, dtype, seed=sum(lens), tail=2, head=1, cols=cols * 16 // page)
     for weights in (None, b.weights):
         got_w = None if weights is None else weights.clone()
         out, lse = b.run(weights=got_w, window=window, sinks=sinks)
         assert b.kv.get_status() == OK
         b.check(out, lse, b.reference(window=window, sinks=sinks, weights=weights), got_w)
+
+
+# heads, kv heads, dim, new tokens, lengths, page, extra columns: few queries; tiles of 32; of 256, in parts or not
+SHAPES = [(8, 2, 64, [1, 1, 2], [40, 300, 7], 16, 0), (8, 2, 128, [30, 1], [200, 77], 16, 0),
+          (8, 2, 128, [60, 20], [700, 30], 16, 5000), (8, 8, 64, [300], [1200], 24, 5000)]
+IDS = [f"{s[0]}x{s[2]}-{s[6]}" for s in SHAPES]
+
+
+def batch(torch, shape, **how):
+    heads, kv_heads, dim, new, lens, page, cols = shape
+    return Batch(torch, heads, kv_heads, dim, new, lens, page, cols=cols, **how)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+@pytest.mark.parametrize("scale,q_std", [(0.0, 1.0), (-0.3, 1.0), (0.5, 8.0), (1e-3, 0.1)])
+def test_scales(torch, scale, q_std, shape):
+    """Flat, reversed and nearly one-hot softmaxes."""
+    say(f"attention scale {scale} {shape}")
+    b = batch(torch, shape, seed=3, q_std=q_std)
+    w = b.weights.clone()
+    out, lse = b.run(scale=scale, weights=w)
+    b.check(out, lse, b.reference(scale=scale, weights=b.weights), w)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+@pytest.mark.parametrize("up", [1.0, -1.0])
+def test_rising_scores(torch, up, shape):
+    """The running maximum moves at every step, by far more than the type's range of exp."""
+    say(f"attention rising {up} {shape}")
+    b = batch(torch, shape, seed=4)
+    for s, L in zip(b.slots, b.lens):
+        for j in range(L):
+            b.pool[0, 0, int(b.tables[s, j // b.page]), j % b.page, :, 0] = up * (60.0 * j / max(L, 1) - 30)
+    b.q[:, :, 0] = 40.0
+    w = b.weights.clone()
+    out, lse = b.run(scale=0.125, weights=w)
+    b.check(out, lse, b.reference(scale=0.125, weights=b.weights), w)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+@pytest.mark.parametrize("dtype,q_value,unit", [
+    ("bfloat16", 2.0 ** 10, 2.0 ** 12), ("bfloat16", 2.0 ** 20, 2.0 ** 20), ("bfloat16", 2.0 ** 50, 2.0 ** 60),
+    ("float16", 2.0 ** 10, 2.0 ** 8), ("float16", 2.0 ** 15, 2.0 ** 12)])
+def test_scores_of_any_size(torch, dtype, q_value, unit, shape):
+    """Scores of up to 2^118, far past where one step of a float is more than the range of exp: the highest
+    tokens, and as many as tie, share the query.  (The scores are exact in 32 bits, so that ds is 0.)"""
+    say(f"attention scores {dtype} {q_value} {unit} {shape}")
+    b = batch(torch, shape, seed=31, dtype=dtype)
+    keys = torch.randint(-7, 8, b.pool.shape[2:5], generator=torch.Generator(device="cuda").manual_seed(32), device="cuda")
+    keep = torch.isfinite(b.pool[0, 0])   # (what lies behind the lengths stays NaN and infinity)
+    b.pool[0, 0] = torch.where(keep, (keys[..., None] * unit).to(b.pool.dtype), b.pool[0, 0])
+    b.q[:] = q_value
+    w = b.weights.clone()
+    out, lse = b.run(scale=0.125, weights=w)
+    assert b.kv.get_status() == OK
+    ref = list(b.reference(scale=0.125, weights=b.weights))
+    n = max(b.lens) + 32
+    ref[3] = torch.zeros_like(ref[3])
+    ref[5] = b.reference(scale=0.0, weights=b.weights)[5] + n * 2.0 ** -23 * ref[4]   # (every p at most 1)
+    b.check(out, lse, ref, w)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (9, 2)])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_what_a_query_does_not_see_stays_out(torch, value, window, sinks, shape):
+    """K and V of some tokens are not finite: queries before them, and those whose window has passed them, are as ever."""
+    say(f"attention not finite {value} {window} {shape}")
+    b = batch(torch, shape, seed=5)
+    clean = b.run(window=window, sinks=sinks)
+    w0 = b.weights.clone()
+    b.run(window=window, sinks=sinks, weights=w0)
+    bad = {}
+    for i, (s, L, n) in enumerate(zip(b.slots, b.lens, b.new)):
+        bad[i] = [L - n // 2 - 1] if n > 1 else ([int(L) // 2] if window and L > 40 else [])
+        for j in bad[i]:
+            for plane in (0, 1):
+                b.pool[0, plane, int(b.tables[s, j // b.page]), j % b.page, :, 3] = value
+    w = b.weights.clone()
+    out, lse = b.run(window=window, sinks=sinks, weights=w)
+    assert b.kv.get_status() == OK
+    for i, (s0, L, n, slot) in enumerate(zip(b.starts, b.lens, b.new, b.slots)):
+        for t in range(n):
+            p = L - n + t
+            sees = any(j <= p and (not window or j > p - window or j < sinks) for j in bad[i])
+            if not sees:   # (a tile that holds such a value takes its products in another order)
+                for got, want in ((out, clean[0]), (lse, clean[1])):
+                    g, c = got[s0 + t].double(), want[s0 + t].double()
+                    assert bool(((g - c).abs() <= 2.0 ** -7 * (c.abs() + 1)).all())
+        # tokens that only such queries see have their weights as ever
+        if bad[i] and not window:
+            first = L - n
+            assert bool((w[slot, :, L:] == w0[slot, :, L:]).all())
+            late = bad[i][0] + 1
+            assert not bool(torch.isnan(out[s0:s0 + max(0, bad[i][0] - first)]).any())
+
+
+def test_infinite_values_that_are_seen(torch):
+    """V with infinity and NaN: the dimension that has it, of the queries that see it, and no other."""
+    for shape in SHAPES:
+        say(f"attention infinite values {shape}")
+        b = batch(torch, shape, seed=6)
+        s, L, n = int(b.slots[0]), int(b.lens[0]), int(b.new[0])
+        j = L - max(n // 2, 1)
+        b.pool[0, 1, int(b.tables[s, j // b.page]), j % b.page, :, 5] = math.inf
+        out, lse = b.run()
+        ref = b.reference()
+        b.check(out, lse, ref)
+        seen = out[int(b.starts[0]) + n - 1]
+        assert bool(torch.isinf(seen[:, 5]).all()) and bool(torch.isfinite(seen[:, :5]).all())
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_nan_in_a_query_stays_there(torch, shape):
+    b = batch(torch, shape, seed=7)
+    want, want_lse = b.run()
+    at = int(b.starts[1]) - 1 if len(b.new) > 1 else 3
+    b.q[at, 1, 2] = math.nan
+    out, lse = b.run()
+    ok = torch.ones(out.shape[:2], dtype=torch.bool, device="cuda")
+    ok[at, 1] = False
+    assert bool(torch.isnan(out[at, 1]).all()) and torch.equal(out[ok], want[ok]) and torch.equal(lse[ok], want_lse[ok])
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_strides_and_layouts(torch, shape):
+    """Queries and outputs inside wider tensors, weights of a layer inside all layers', tables and another layer of the pool."""
+    from paper_2609_09800_amd import hbf
+    say(f"attention layouts {shape}")
+    b = batch(torch, shape, seed=8)
+    w = b.weights.clone()
+    want, want_lse = b.run(weights=w)
+    T, H, D = b.q.shape
+    two = torch.zeros((2, *b.pool.shape[1:]), dtype=b.pool.dtype, device="cuda")
+    two[1] = b.pool[0]
+    tables = torch.full((b.tables.shape[0], b.tables.shape[1] + 3), -1, dtype=torch.int32, device="cuda")
+    tables[:, :-3] = b.dev["tables"]
+    kv = hbf.KvPages(two, refs=b.dev["refs"], tables=tables[:, :-3], lens=b.dev["lens"])
+    wide = torch.full((T, 3, H, D + 8), 5.0, dtype=b.q.dtype, device="cuda")
+    wide[:, 1, :, :D] = b.q
+    out = torch.full((T, H, 2, D), 5.0, dtype=b.q.dtype, device="cuda")
+    all_w = torch.full((b.weights.shape[0], 3, b.weights.shape[1], b.weights.shape[2] + 5), 5.0, device="cuda")
+    all_w[:, 1, :, :-5] = b.weights
+    lse = torch.empty_like(want_lse)
+    assert kv.attention(1, wide[:, 1, :, :D], out[:, :, 1], b.dev["slots"], b.dev["starts"], lse=lse, weights=all_w[:, 1]) == OK
+    assert torch.equal(out[:, :, 1], want) and torch.equal(lse, want_lse) and torch.equal(all_w[:, 1, :, :-5], w)
+    assert bool((out[:, :, 0] == 5.0).all()) and bool((all_w[:, ::2] == 5.0).all()) and bool((all_w[..., -5:] == 5.0).all())
+    # without lse; nothing to do
+    o2 = torch.empty_like(b.q)
+    assert kv.attention(1, b.q, o2, b.dev["slots"], b.dev["starts"]) == OK and torch.equal(o2, want)
+    assert kv.attention(1, b.q, o2, b.dev["slots"][:0], b.dev["starts"][:1]) == OK and torch.equal(o2, want)
+    assert kv.attention(1, b.q[:0], o2[:0], b.dev["slots"], torch.zeros_like(b.dev["starts"])) == OK
+    assert kv.get_status() == OK
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_repeats_bit_for_bit_from_any_scratch(torch, shape):
+    b = batch(torch, shape, seed=9)
+    runs = []
+    for fill in (0, 255, 255):
+        if b.kv._attn_ws._t is not None:
+            b.kv._attn_ws._t.fill_(fill)
+        w = b.weights.clone()
+        runs.append((*b.run(weights=w), w))
+        assert not bool(b.kv._chunk_ctl.any())
+    for r in runs[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(r, runs[0]))
+    # without control words nothing is cut into parts
+    b.kv._chunk_at = None
+    w = b.weights.clone()
+    out, lse = b.run(weights=w)
+    b.check(out, lse, b.reference(weights=b.weights), w)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_rows_of_one_slot(torch, shape):
+    """A slot that several rows name: each result as alone, its weights the sum of all."""
+    heads, kv_heads, dim, new, lens, page, cols = shape
+    say(f"attention rows of one slot {shape}")
+    L = max(lens)
+    b = Batch(torch, heads, kv_heads, dim, [new[0], 3, new[0]], [L, 50, L], page, cols=cols, seed=10, slots=[2, 0, 2])
+    w = b.weights.clone()
+    out, lse = b.run(weights=w)
+    b.check(out, lse, b.reference(weights=b.weights), w)
+
+
+def test_many_rows(torch):
+    """More rows than are searched at a time, and than a workgroup has threads; rows without tokens among them."""
+    rng = np.random.default_rng(11)
+    for rows, top, cols in ((70, 3, 0), (4200, 2, 0), (600, 40, 3000)):
+        say(f"attention {rows} rows")
+        new = rng.integers(0, top, rows)
+        lens = np.maximum(new, rng.integers(0, 9, rows))
+        b = Batch(torch, 2, 1, 64, new, lens, 8, seed=rows, cols=cols)
+        w = b.weights[:, :, :64].contiguous()   # (no token lies behind)
+        got = w.clone()
+        out, lse = b.run(weights=got)
+        assert b.kv.get_status() == OK
+        b.check(out, lse, b.reference(weights=w), got)
+
+
+def test_offsets_past_32_bits(torch):
+    """Pages behind 2^32 bytes of a 9 GiB pool."""
+    from paper_2609_09800_amd import hbf
+    for new, lens in (([1, 1], [100, 1500]), ([40, 9], [300, 1100])):
+        b = Batch(torch, 8, 4, 64, new, lens, 1024, seed=12, cols=100)
+        want = b.run()
+        pages = 9000
+        pool = torch.zeros((1, 2, pages, 1024, 4, 64), dtype=torch.bfloat16, device="cuda")
+        moved = pages - b.pool.shape[2]
+        pool[:, :, moved:] = b.pool
+        tables = torch.where(b.dev["tables"] >= 0, b.dev["tables"] + moved, -1).int()
+        kv = hbf.KvPages(pool, refs=torch.ones(pages, dtype=torch.int32, device="cuda"), tables=tables, lens=b.dev["lens"])
+        out = torch.empty_like(b.q)
+        w, w2 = b.weights.clone(), b.weights.clone()
+        assert kv.attention(0, b.q, out, b.dev["slots"], b.dev["starts"], weights=w) == OK
+        b.run(weights=w2)
+        assert torch.equal(out, want[0]) and torch.equal(w, w2)
+        del pool, kv
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+@pytest.mark.parametrize("what", ["long", "negative", "weights", "slot", "slot_low", "page", "page_low"])
+def test_bad_entries_fail_closed(torch, what, shape):
+    """A slot, length or page out of range: that row is NaN, the others are right."""
+    say(f"attention bad {what} {shape}")
+    heads, kv_heads, dim, new, lens, page, cols = shape
+    b = Batch(torch, heads, kv_heads, dim, [new[0], new[0], 2], [lens[0], lens[0] + 30, 20], page, cols=cols, seed=13)
+    want, want_lse = b.run()
+    s = int(b.slots[1])
+    weights = b.weights.clone()
+    if what == "long":
+        b.dev["lens"][s] = b.tables.shape[1] * page + 1
+    elif what == "negative":
+        b.dev["lens"][s] = -1
+    elif what == "weights":
+        weights = weights[:, :, :lens[0] + 29].contiguous()
+    elif what == "slot":
+        b.dev["slots"][1] = b.tables.shape[0]
+    elif what == "slot_low":
+        b.dev["slots"][1] = -1
+    elif what == "page":
+        b.dev["tables"][s, 0] = b.pool.shape[2]
+    else:
+        b.dev["tables"][s, 0] = -1
+    w = weights.clone()
+    out, lse = b.run(weights=w)
+    assert b.kv.get_status() == EINVAL and b.kv.get_status() == OK
+    rows = slice(int(b.starts[1]), int(b.starts[2]))
+    keep = torch.ones(len(out), dtype=torch.bool, device="cuda")
+    keep[rows] = False
+    assert bool(torch.isnan(out[rows]).all()) and bool(torch.isnan(lse[rows]).all())
+    assert torch.equal(out[keep], want[keep]) and torch.equal(lse[keep], want_lse[keep])
+    assert torch.equal(w[s], weights[s])
+
+
+def test_bad_starts(torch):
+    """Starts that decrease or leave the queries: an error, and nothing outside the tensors is touched."""
+    for shape in SHAPES:
+        b = batch(torch, shape, seed=14)
+        for change in ((1, -5), (1, 10 ** 9), (len(b.new), len(b.q) + 1), (0, int(b.starts[1]) + 1)):
+            say(f"attention bad starts {change} {shape}")
+            b.dev["starts"].copy_(torch.from_numpy(b.starts))
+            b.dev["starts"][change[0]] = change[1]
+            b.run(weights=b.weights.clone())
+            assert b.kv.get_status() == EINVAL
+            assert not bool(b.kv._chunk_ctl.any())
+
+
+def test_refusals(torch):
+    from paper_2609_09800_amd import hbf
+    b = batch(torch, SHAPES[0], seed=15)
+    out, lse = b.run()
+    sl, st, q, w = b.dev["slots"], b.dev["starts"], b.q, b.weights
+    for args, how in (((1, q, out, sl, st), {}), ((0, q.float(), out, sl, st), {}), ((0, q, out[:3], sl, st), {}),
+                      ((0, q, out, sl, st[:-1]), {}), ((0, q, out, sl.long(), st), {}), ((0, q, out, sl, st.long()), {}),
+                      ((0, q.cpu(), out, sl, st), {}), ((0, q, out[:1].expand(len(q), -1, -1), sl, st), {}),
+                      ((0, q[..., :32], out[..., :32], sl, st), {}), ((0, q, out, sl, st), dict(lse=lse[:, :3])),
+                      ((0, q, out, sl, st), dict(weights=w[:-1])), ((0, q, out, sl, st), dict(weights=w.double())),
+                      ((0, q, out, sl, st), dict(weights=w[:, :1])), ((0, q, out, sl, st), dict(weights=w[:1].expand(len(w), -1, -1))),
+                      ((0, q, out, sl, st), dict(weights=w[..., ::2]))):
+        with pytest.raises(hbf.HbfError):
+            b.kv.attention(*args, **how)
+    with pytest.raises(hbf.HbfError):
+        hbf.KvPages(b.pool).attention(0, q, out, sl, st)
+    assert b.kv.attention(0, q[:, :7], out[:, :7], sl, st) == EINVAL     # 7 heads over 2
+    for how in (dict(window=-1), dict(sinks=-1), dict(scale=math.nan), dict(scale=math.inf)):
+        assert b.kv.attention(0, q, out, sl, st, **how) == EINVAL
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=IDS)
+def test_another_stream_and_graph(torch, shape):
+    say(f"attention graph {shape}")
+    b = batch(torch, shape, seed=16)
+    want, want_lse = b.run()
+    out = torch.empty_like(b.q)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    assert b.kv.attention(0, b.q, out, b.dev["slots"], b.dev["starts"], stream=s) == OK
+    s.synchronize()
+    assert torch.equal(out, want)
+    q, out, lse = b.q.clone(), torch.empty_like(b.q), torch.empty_like(want_lse)
+    w = torch.zeros_like(b.weights)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        assert b.kv.attention(0, b.q, out, b.dev["slots"], b.dev["starts"], lse=lse, weights=w) == OK
+    lens = b.dev["lens"].clone()
+    for i in range(4):   # other queries and lengths than were captured
+        b.q.copy_(q * (i + 1) / 2)
+        b.dev["lens"].copy_((lens - i).clamp(min=0))
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        w.fill_(0.5)
+        g.replay()
+        torch.cuda.synchronize()
+        w2 = torch.full_like(w, 0.5)
+        eager, eager_lse = b.run(weights=w2)
+        rows = slice(int(b.starts[0]), int(b.starts[-1]))
+        assert torch.equal(out[rows], eager[rows]) and torch.equal(lse[rows], eager_lse[rows]) and torch.equal(w, w2)
