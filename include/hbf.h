@@ -663,7 +663,8 @@ typedef struct {
   const float *dev_weights;   /* layer l, slot s, head h at l * layer_stride + s * slot_stride + h * head_stride */
   int64_t layer_stride, slot_stride, head_stride; /* in elements, >= 0 */
   int32_t weights_tokens;     /* what a row of weights holds */
-  float *dev_weights_out;     /* as dev_weights, rows of listed slots up to their old length; NULL: in place */
+  float *dev_weights_out;     /* as dev_weights and not overlapping it, rows of listed slots up to their old length;
+                                 NULL or dev_weights: in place */
   int32_t *dev_kept;          /* [planes / 2][n][kv_heads][max_keep] */
   int32_t max_keep;           /* 0 .. 2^24; layers * n * kv_heads * max_keep <= 2^40 */
 } hbf_eviction;

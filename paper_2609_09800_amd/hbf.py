@@ -969,7 +969,7 @@ class KvPages:
         those of the largest weights between.  weights: float32 [layers, slots,
         kv_heads, tokens] (as attention's, for each layer; all but the tokens
         may be strided) follow their tokens, in place or to weights_out (shaped
-        and strided alike).  kept: int32 [layers, n, kv_heads, max_keep],
+        and strided alike, not overlapping).  kept: int32 [layers, n, kv_heads, max_keep],
         max_keep at least the largest keep, receives each place's token's old
         position, -1 behind them."""
         d = self._desc()
