@@ -520,7 +520,8 @@ struct Many {
   char *lds;
   uint32_t lds0;
   int lane, w, col, hf;
-  int page = 0, pos;
+  int page = 0;
+  int from, last;   // the query sees x < a.ch.sinks and from <= x, both below last
   bool bad = false, odd = false;
   int64_t at;       // bytes to the row of this lane's token of the group
   u32x4 qv[KS], p[2], kk[KS], vv[DT][2];
@@ -534,7 +535,9 @@ struct Many {
   __device__ __forceinline__ void load_queries() {
     const Query qq = query_of(a, t, w * 32 + col);
     const bool none = qq.head < 0;
-    pos = none ? t.view.p1 : qq.pos;
+    const int pos = none ? t.view.p1 : qq.pos;
+    last = (int)min((int64_t)pos + 1 - t.view.lo + t.view.first, (int64_t)t.x1);
+    from = a.ch.window ? (int)max((int64_t)pos + 1 - a.ch.window - t.view.lo + t.view.first, (int64_t)0) : 0;
     const char *from = (const char *)a.ch.dev_q + 2 * (none ? 0 : qq.token * a.ch.q_row_stride + qq.head * a.ch.q_head_stride);
 #pragma unroll
     for (int k = 0; k < KS; k++) {
@@ -619,12 +622,16 @@ struct Many {
   }
   // Scores of the tokens from x on that their query does not see, or that are none.
   __device__ __forceinline__ void mask(f32x16 &s, uint32_t x) const {
+    const uint32_t keep = (below(last - (int)x) & (~below(from - (int)x) | below(a.ch.sinks - (int)min(x, (uint32_t)INT32_MAX)))) >> 4 * hf;
 #pragma unroll
     for (int i = 0; i < 16; i++) {
-      const uint32_t xx = x + (i / 4) * 8 + hf * 4 + i % 4;
-      s[i] = (xx < t.x1) & sees(a, pos, (int)t.view.token(xx)) ? s[i] : -INFINITY;
+      const float v = s[i];
+      const uint32_t k = (uint32_t)__builtin_amdgcn_sbfe((int)keep, i / 4 * 8 + i % 4, 1);
+      s[i] = __uint_as_float((__float_as_uint(v) & k) | (0xff800000u & ~k));
     }
   }
+  // Bits 0 .. n - 1 of 32.
+  static __device__ __forceinline__ uint32_t below(int n) { return (uint32_t)((uint64_t(1) << min(max(n, 0), 32)) - 1); }
   // A tile that is not whole: whether its V holds what is not finite (0 * infinity would reach the sums).
   __device__ __forceinline__ void look(int tile) {
     const char *vt = lds + tile % RING * 2 * TILE_BYTES + TILE_BYTES;
@@ -703,10 +710,10 @@ struct Many {
   __device__ __forceinline__ void run() {
     const int n = (int)((t.x1 - t.x0 + MANY_TILE - 1) / MANY_TILE);
     find(0);
+    load_queries();  // (on their way beside the page ids)
     place(0);
     find(GROUP);
     for (int i = 0; i < min(n, RING - 1); i++) stage(i);
-    load_queries();
     nothing_pending();
     f32x16 sa, sb;
     arrived(min(n, RING - 1) - 1);
@@ -736,15 +743,18 @@ __device__ __forceinline__ bool many(const Args &a, const Tile &t, char *lds) {
   Many<T, D> z(a, t, lds);
   constexpr int DT = D / 32;
   z.run();
-  if (__syncthreads_or(z.odd)) return true;
-  const bool any_bad = __syncthreads_or(z.bad);
+  bool any_bad = false;
+  if (__syncthreads_or(z.odd || z.bad)) {
+    if (__syncthreads_or(z.odd)) return true;
+    any_bad = __syncthreads_or(z.bad);
+  }
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
   const int i = z.w * 32 + z.col;
   const Query qq = query_of(a, t, i);
   const float fix = z.to_maximum(), l = across_halves(z.l, SUM_OP);
-  if (qq.head < 0) return false;
   auto four = [&](int d, int g) { return f32x4{z.o[d][g * 4], z.o[d][g * 4 + 1], z.o[d][g * 4 + 2], z.o[d][g * 4 + 3]}; };
   if (t.parts > 1) {
+    if (qq.head < 0) return false;
     const int64_t at = part_at(a, t, t.split, i);
 #pragma unroll
     for (int d = 0; d < DT; d++)
@@ -752,12 +762,28 @@ __device__ __forceinline__ bool many(const Args &a, const Tile &t, char *lds) {
       for (int g = 0; g < 4; g++) hand_over((f32x4 *)(a.part + at * D + d * 32 + g * 8 + z.hf * 4), four(d, g) * fix);
     if (z.hf == 0) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(z.m, l * fix));
   } else {
+    if (z.hf == 0 && qq.head >= 0) write_sums<T>(a, qq, z.m, l * fix, any_bad);
+    // by way of LDS, of which every wave is done with its own eighth's tiles: a lane holds parts of a row, and a
+    // store of 8 bytes a row takes as long as one of all of it
     const float f = one_over(qq, l, any_bad);
+    char *mine = lds + z.w * 32 * D * 2;
 #pragma unroll
     for (int d = 0; d < DT; d++)
 #pragma unroll
-      for (int g = 0; g < 4; g++) write_out<T>(a, qq, d * 32 + g * 8 + z.hf * 4, four(d, g) * f);
-    if (z.hf == 0) write_sums<T>(a, qq, z.m, l * fix, any_bad);
+      for (int g = 0; g < 4; g++) {
+        const f32x4 v = four(d, g) * f;
+        *(u32x2 *)(mine + k_at<D>(z.col, d * 4 + g) + z.hf * 8) = u32x2{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])};
+      }
+    wave_lds_fence();
+    constexpr int LANES = D / 8;
+#pragma unroll
+    for (int j = 0; j < 32; j += 64 / LANES) {
+      const int row = j + z.lane / LANES, piece = z.lane % LANES;
+      const u32x4 v = *(const u32x4 *)(mine + k_at<D>(row, piece));
+      const Query to = query_of(a, t, z.w * 32 + row);
+      if (to.head >= 0)
+        *(u32x4 *)((typename T::elem *)a.ch.dev_out + to.token * a.ch.out_row_stride + to.head * a.ch.out_head_stride + piece * 8) = v;
+    }
   }
   return false;
 }
@@ -921,7 +947,7 @@ __global__ __launch_bounds__(THREADS, 3) void k_weigh(Args a, int blocks) {
         for (int i = 0; i < 4; i++) {
           const uint32_t j = x + u * 16 + kg * 4 + i;
           const float p = __builtin_amdgcn_exp2f((s[u][i] - z.ml.x) * a.c) * z.ml.y;
-          sum[u][i] += (z.ml.y != 0.f) & (j < x1) & sees(a, z.pos, (int)j) ? p : 0.f;
+          sum[u][i] += ((z.ml.y != 0.f) & (j < x1) & sees(a, z.pos, (int)j)) ? p : 0.f;
         }
     };
     for (int i = i0; i <= last; i++) {

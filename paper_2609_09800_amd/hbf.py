@@ -583,6 +583,14 @@ def _strided(t, what, dtypes, dim, inner=1):
     return t
 
 
+def _heads(t, dtype):
+    """[rows, heads, head_dim] as a kernel takes it, the strides of two dimensions in elements of 2 bytes (_strided says what is wrong)."""
+    if isinstance(t, _Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 3:
+        rows, heads, inner = t.stride()
+        return inner == 1 and not (rows | heads) & 7
+    return False
+
+
 def _writable(t, what):
     """An output whose elements must not share memory (an expanded tensor's do)."""
     if not t.is_contiguous() and any(t.stride(d) == 0 and t.shape[d] > 1 for d in range(t.dim())):
@@ -878,7 +886,7 @@ class KvPages:
         if positions is not None:
             _ints(positions, "positions", n)
         for t, what in ((q, "q"), (k, "k"), (v, "v"), (q_out, "q_out")):
-            if not _is(t, dtype) or t.dim() != 3:
+            if not _heads(t, dtype):
                 _strided(t, what, (dtype,), 3)
         _writable(q_out, "q_out")
         heads, dim, kv_shape = q.shape[1], self.head_dim, (n, self.kv_heads, self.head_dim)
@@ -919,10 +927,11 @@ class KvPages:
         dtype = self.pool.dtype
         if not 0 <= layer < self.layers:
             raise HbfError(HBF_EINVAL, f"layer {layer}, the pool has {self.layers}")
-        if not _is(q, dtype) or q.dim() != 3:
+        if not _heads(q, dtype):
             _strided(q, "q", (dtype,), 3)
-        if not _is(out, dtype):
-            _writable(_strided(out, "out", (dtype,), 3), "out")
+        if not _heads(out, dtype):
+            _strided(out, "out", (dtype,), 3)
+        _writable(out, "out")
         shape = q.shape
         tokens, heads, dim = shape
         if dim != self.head_dim or out.shape != shape:
