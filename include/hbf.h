@@ -629,7 +629,7 @@ typedef struct {
 } hbf_chunk;
 #define HBF_CHUNK_CTL_WORDS 2048u
 
-/* Device scratch of a call, in bytes (only sizes are looked at). */
+/* Device scratch of a call, in bytes (sizes are looked at, and whether dev_weights and dev_ctl are given). */
 int hbf_kv_chunk_workspace_bytes(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch, size_t *bytes);
 
 /* The tables and lengths are the cache's; its counts, pool and workspace are

@@ -39,6 +39,8 @@ constexpr int RING = 4;        // staged tiles
 constexpr int MANY_Q = 256;    // queries of a tile there
 constexpr int MANY_WAVES = MANY_Q / 32, MANY_THREADS = 64 * MANY_WAVES;
 
+constexpr int64_t SCORES_BYTES = 512 << 20;  // most that scores are kept in
+
 constexpr float LARGE = 1 << 22;  // of a score, times c: beyond, its rounding shows in exp2
 
 struct Args {
@@ -61,6 +63,9 @@ struct Args {
   float2 *part_ml;    // [slots][kv_heads][splits][tile_q] maximum (of q.k, its sign the scale's) and sum
   float2 *query_ml;   // [tokens][heads] the same of each query, 1 / sum; with weights only
   float *part_w;      // [WEIGH_GROUPS][512] sums of a split's queries
+  float *scores;      // [tokens][heads][score_tokens] of few queries with weights, along a tile's axis; or null
+  int64_t score_tokens;
+  bool keep_scores;
   int32_t *status;
 };
 
@@ -431,6 +436,16 @@ __device__ __forceinline__ void few(const Args &a, const Tile &t, int i0, char *
             for (int q = 0; q < QT; q++)
               if (xx >= x1 || !sees(a, pos[q], token)) s[q][u][i] = -INFINITY;
           }
+      if (a.scores) {  // (a lane's columns of the tile, of its queries)
+#pragma unroll
+        for (int q = 0; q < QT; q++) {
+          const Query qq = query_of(a, t, i0 + q * 16 + col);
+          if (qq.head < 0) continue;
+          float *to = a.scores + ((int64_t)qq.token * a.ch.heads + qq.head) * a.score_tokens + x + kg * 4;
+          *(f32x4 *)to = s[q][0];
+          *(f32x4 *)(to + 16) = s[q][1];
+        }
+      }
       softmax_step<T, QT, 2, DT>(s, a.c, m, l, o);
       u32x4 p[QT][1];
 #pragma unroll
@@ -852,6 +867,73 @@ __global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chu
 
 // ------------------------------------------------------------ weights
 
+// The last row that names row i0's slot, or -1 where i0 is not the first; for a workgroup, by way of `after` in LDS.
+__device__ __forceinline__ int last_of_slot(const Args &a, int i0, int slot, int *after) {
+  if (threadIdx.x == 0) *after = i0;
+  bool before = false;
+  int last = i0;
+  for (int j = threadIdx.x; j < a.ch.rows; j += THREADS)
+    if (a.ch.dev_slots[j] == slot) {
+      before |= j < i0;
+      last = max(last, j);
+    }
+  if (__syncthreads_or(before)) return -1;
+  if (last > i0) atomicMax(after, last);
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(*after);
+}
+
+// What a row's queries gave each token, from the scores that attention left: a
+// thread a token.  A slot's rows are taken by the first of them, one after
+// another, and their queries in order.
+__global__ __launch_bounds__(THREADS) void k_weigh_scores(Args a, int blocks) {
+  constexpr int AHEAD = 8;  // queries whose scores are on their way together
+  __shared__ int after;
+  int b = blockIdx.x;
+  const int head = b % a.layer.kv_heads;
+  b /= a.layer.kv_heads;
+  const int i0 = b % a.ch.rows, block = b / a.ch.rows;
+  const int slot = a.ch.dev_slots[i0];
+  const Row first = get_row(a, i0);
+  if (!first.ok || block * THREADS >= first.len) return;
+  const int last = last_of_slot(a, i0, slot, &after);
+  if (last < 0) return;
+  float *out = a.ch.dev_weights + slot * a.ch.weights_slot_stride + head * a.ch.weights_head_stride;
+  for (int64_t j0 = (int64_t)block * THREADS; j0 < first.len; j0 += (int64_t)blocks * THREADS) {
+    const uint32_t j = (uint32_t)j0 + threadIdx.x;
+    const bool there = j < (uint32_t)first.len;
+    const float old = there ? out[j] : 0.f;
+    float sum = 0.f;
+    for (int i = i0; i <= last; i++) {
+      if (i > i0 && a.ch.dev_slots[i] != slot) continue;
+      const Row r = i == i0 ? first : get_row(a, i);
+      for (int q0 = 0; q0 < r.n * a.group; q0 += a.tile_q) {
+        const int q1 = min(q0 + a.tile_q, r.n * a.group);
+        const View v = view_of(a, r, q0, q1);
+        const uint32_t x = j < v.first ? j : j - v.lo + v.first;
+        const bool has = there && (j < v.first || j >= v.lo) && x < v.total;
+        if (!__any(has)) continue;
+        const float *from = a.scores + x;
+        for (int q = q0; q < q1; q += AHEAD) {
+          float s[AHEAD];
+          float2 ml[AHEAD];
+#pragma unroll
+          for (int k = 0; k < AHEAD; k++) {
+            const int qq = min(q + k, q1 - 1), tok = token_of(a, qq);
+            const int64_t at = (int64_t)(r.start + tok) * a.ch.heads + head * a.group + qq - tok * a.group;
+            ml[k] = a.query_ml[at];
+            s[k] = has ? from[at * a.score_tokens] : 0.f;
+          }
+#pragma unroll
+          for (int k = 0; k < AHEAD; k++)
+            sum += has && q + k < q1 && ml[k].y != 0.f ? __builtin_amdgcn_exp2f((s[k] - ml[k].x) * a.c) * ml[k].y : 0.f;
+        }
+      }
+    }
+    if (there && sum != 0.f) out[j] = old + sum;  // (NaN too; a token that nobody sees has 0)
+  }
+}
+
 // What a row's queries gave each token: a wave takes 32 tokens at a time, through LDS of
 // its own, the next ones on their way, and meets 16 queries at a time; a token's
 // sum over the lanes that hold its scores is taken once.  A slot's rows are taken
@@ -866,19 +948,8 @@ __global__ __launch_bounds__(THREADS, 3) void k_weigh(Args a, int blocks) {
   const int head = b % a.layer.kv_heads;
   b /= a.layer.kv_heads;
   const int i0 = b % a.ch.rows, block = b / a.ch.rows;
-  const int slot = a.ch.dev_slots[i0];
-  if (threadIdx.x == 0) after = i0;
-  bool before = false;
-  int last = i0;
-  for (int j = threadIdx.x; j < a.ch.rows; j += THREADS)
-    if (a.ch.dev_slots[j] == slot) {
-      before |= j < i0;
-      last = max(last, j);
-    }
-  if (__syncthreads_or(before)) return;
-  if (last > i0) atomicMax(&after, last);
-  __syncthreads();
-  last = __builtin_amdgcn_readfirstlane(after);
+  const int slot = a.ch.dev_slots[i0], last = last_of_slot(a, i0, slot, &after);
+  if (last < 0) return;
   const Row first = get_row(a, i0);
   if (!first.ok) return;
   const uint32_t len = (uint32_t)first.len, step = (uint32_t)blocks * WAVES * NT;
@@ -1268,6 +1339,13 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   a.part_steps = a.tile_q == MANY_Q ? 4 : 2;
   const int64_t steps = longest / ((a.tile_q == MANY_Q ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
   a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(steps, (a.tile_q == MANY_Q ? 256 : groups < 128 ? 512 : 1024) / groups));
+  // Weights of few queries: from the scores that attention leaves, where those of a tile, written and read, are no
+  // more bytes than K, which is read again else (64 rows of one token behind 4,096: 146 us, else 173; 32 queries
+  // a row and head of 64 values, which go the other way: 99 us, else 90), and within SCORES_BYTES.
+  const int64_t held = std::min<int64_t>(longest, ch.weights_tokens);
+  a.score_tokens = (held + WAVES * FEW_TILE - 1) / (WAVES * FEW_TILE) * (WAVES * FEW_TILE);
+  a.keep_scores = ch.dev_weights && a.tile_q * 4 <= layer.head_dim &&
+                  ch.tokens * (int64_t)ch.heads * a.score_tokens * 4 <= SCORES_BYTES;
   return a;
 }
 
@@ -1286,6 +1364,7 @@ size_t carve(Args &a, char *ws) {
   }
   if (a.ch.dev_weights) {
     a.query_ml = (float2 *)take((size_t)a.ch.tokens * a.ch.heads * 8);
+    if (a.keep_scores) a.scores = (float *)take((size_t)a.ch.tokens * a.ch.heads * a.score_tokens * 4);
     if (a.tile_q == MANY_Q && a.ch.dev_ctl) a.part_w = (float *)take((size_t)WEIGH_GROUPS * BLOCK * 4);
   }
   return std::max(o, size_t(256));
@@ -1302,6 +1381,11 @@ hipError_t run(const Args &a, hipStream_t s) {
     const int64_t longest = std::min<int64_t>((int64_t)a.kv.table_cols * a.kv.page_tokens, a.ch.weights_tokens);
     if (a.tile_q == MANY_Q && a.ch.rows <= WEIGH_ROWS) {
       k_weigh_many<T, D><<<WEIGH_GROUPS, MANY_THREADS, 0, s>>>(a);
+      return hipGetLastError();
+    }
+    if (a.keep_scores) {
+      const int64_t each = std::max<int64_t>(1, std::min<int64_t>(longest / THREADS + 1, 8192 / groups));
+      k_weigh_scores<<<(uint32_t)(groups * each), THREADS, 0, s>>>(a, (int)each);
       return hipGetLastError();
     }
     const int64_t most = longest / (WAVES * FEW_TILE) + 1;

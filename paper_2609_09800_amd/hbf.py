@@ -953,7 +953,7 @@ class KvPages:
                     int(sinks), out.data_ptr(), os[0] if tokens > 1 else 0, os[1] if heads > 1 else 0,
                     0 if lse is None else lse.data_ptr(), 0 if weights is None else weights.data_ptr(), *ws,
                     min(held, (1 << 31) - 1), self._chunk_at or 0)
-        sizes = (tokens, rows, heads, weights is None)
+        sizes = (tokens, rows, heads, None if weights is None else held)
         if sizes != self._chunk_sizes:
             b = ctypes.c_size_t()
             rc = self._lib.hbf_kv_chunk_workspace_bytes(d, kv, at, ctypes.byref(b))

@@ -405,6 +405,19 @@ def test_many_rows(torch):
         b.check(out, lse, b.reference(weights=w), got)
 
 
+@pytest.mark.parametrize("heads,kv_heads,dim,new", [(8, 2, 64, [1, 1, 2]), (8, 2, 128, [14, 1])])
+def test_weights_beside_tables_of_millions_of_tokens(torch, heads, kv_heads, dim, new):
+    """Scores of all that the tables could hold would take more scratch than is given to them."""
+    say(f"attention wide tables {heads} {dim}")
+    for cols, dtype in ((20, "float16"), (9000, "bfloat16")):
+        b = Batch(torch, heads, kv_heads, dim, new, [70, 900, 30][:len(new)], 1024, dtype=dtype, seed=17, cols=cols)
+        w = b.weights.clone()
+        out, lse = b.run(weights=w, window=200, sinks=5)
+        b.check(out, lse, b.reference(window=200, sinks=5, weights=b.weights), w)
+        need = b.q.shape[0] * heads * b.weights.shape[-1] * 4
+        assert (need > 512 << 20) == (b.kv._attn_ws._t.numel() < need), "the scratch is what the scores say"
+
+
 def test_offsets_past_32_bits(torch):
     """Pages behind 2^32 bytes of a 9 GiB pool."""
     from paper_2609_09800_amd import hbf
