@@ -309,10 +309,11 @@ __device__ __forceinline__ int64_t part_at(const Args &a, const Tile &t, int spl
 }
 
 // The tile's last workgroup joins its parts: D / 4 lanes a query, R queries at
-// a time, U parts of each asked for at once.
-template <typename T, int D>
+// a time, U parts of each asked for at once (a trip to memory each: of two queries 8, where there are more, 16 of
+// one; one row of 8 queries in 79 parts 28.3 -> 22.5 us a call).
+template <typename T, int D, int R, int U>
 __device__ void join(const Args &a, const Tile &t) {
-  constexpr int LANES = D / 4, R = 2, U = 8;
+  constexpr int LANES = D / 4;
   const int AT_ONCE = blockDim.x / LANES;
   const int d0 = threadIdx.x % LANES * 4, mine = threadIdx.x / LANES;
   for (int i0 = mine; i0 < t.q1 - t.q0; i0 += AT_ONCE * R) {
@@ -359,7 +360,8 @@ __device__ void end_part(const Args &a, const Tile &t) {
   stores_done();
   if (!last_of(a.ch.dev_ctl + t.place * a.layer.kv_heads + t.head, (uint32_t)t.parts)) return;
   see_handed();
-  join<T, D>(a, t);
+  if (t.parts <= 8) join<T, D, 2, 8>(a, t);
+  else join<T, D, 1, 16>(a, t);
 }
 
 // ------------------------------------------------------------ few queries
@@ -851,7 +853,11 @@ __global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chu
     }
     return;
   }
-  const uint32_t most = (steps + a.part_steps - 1) / a.part_steps, parts = min(most, (uint32_t)a.splits);
+  uint32_t most = (steps + a.part_steps - 1) / a.part_steps;
+  // (a part's steps and the trips that its join takes: as many of one as of the other, about; one row of 20,000 tokens
+  // 22.5 -> 18.7 us)
+  if (QT) most = min(most, (uint32_t)(3.5f * __builtin_sqrtf((float)steps)) + 1);
+  const uint32_t parts = min(most, (uint32_t)a.splits);
   const uint32_t each = (steps + parts - 1) / parts;
   t.parts = (int)((steps + each - 1) / each);
   if (t.split >= t.parts) return;
@@ -1334,9 +1340,10 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   a.tile_q = 1 << a.tile_shift;
   a.slots = (int)(queries >> a.tile_shift) + ch.rows;
   // Parts, so that a card's worth of workgroups have work if all rows are long, twice that where rows of different
-  // lengths have to be packed; a tile takes as many as its length gives work for.
+  // lengths have to be packed; a tile takes as many as its length gives work for.  Where the tiles alone are a card's
+  // worth, a part has 8 steps at least (64 rows of 500 tokens 24.1 -> 19.1 us, of 1,500 47.3 -> 48.5).
   const int64_t groups = (int64_t)a.slots * layer.kv_heads;
-  a.part_steps = a.tile_q == MANY_Q ? 4 : 2;
+  a.part_steps = a.tile_q == MANY_Q ? 4 : groups >= 256 ? 8 : 2;
   const int64_t steps = longest / ((a.tile_q == MANY_Q ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
   a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(steps, (a.tile_q == MANY_Q ? 256 : groups < 128 ? 512 : 1024) / groups));
   // Weights of few queries: from the scores that attention leaves, where those of a tile, written and read, are no
