@@ -23,6 +23,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <numeric>
 
 #include "hbf_attn_tile.h"
 #include "hbf_kv_rows.h"
@@ -55,9 +56,10 @@ struct Args {
   uint32_t window;    // of positions, or all of them
   uint32_t page_mul;  // token / page_tokens = token * page_mul >> page_shift, for tokens below 2^31
   int page_shift;
-  int tile_q, tile_shift;  // queries per tile, 16, 32 or MANY_Q, and its logarithm
+  int tile_q, tile_shift;  // queries per tile, 16 or MANY_Q, and its logarithm
   int slots;          // places for tiles: tokens * group / tile_q + rows
   int splits;         // most parts of a tile
+  uint32_t spread;    // tiles of few queries: workgroup b takes place and head b * spread % their number
   int part_steps;     // least steps of a part
   float *part;        // [slots][kv_heads][splits][tile_q][head_dim] sums of p v
   float2 *part_ml;    // [slots][kv_heads][splits][tile_q] maximum (of q.k, its sign the scale's) and sum
@@ -263,35 +265,31 @@ __device__ __forceinline__ void write_sums(const Args &a, Query q, float m, floa
   if (a.query_ml) a.query_ml[at] = bad || none ? make_float2(0.f, 0.f) : make_float2(m, 1.f / sum);
 }
 
-// A step's products with V one by one, in 32 bits: a value that a query does not see
-// must not meet its 0.  p: the lane's probabilities as they are multiplied otherwise;
-// pos: its queries' positions; at: U * 512 bytes of LDS of the wave's own.
-template <typename T, int D, int QT, int U>
+// The products of a step's 32 tokens with V one by one, in 32 bits: a value that a
+// query does not see must not meet its 0.  p: the lane's probabilities as they are
+// multiplied otherwise; pos: its query's position; at: 1 KiB of LDS of the wave's own.
+template <typename T, int D>
 __device__ __forceinline__ void products_one_by_one(const Args &a, const View &v, const char *vt, uint32_t x, uint32_t x1,
-                                                    const u32x4 (&p)[QT][U / 2], const int (&pos)[QT],
-                                                    f32x4 (&o)[QT][D / 16], char *at) {
+                                                    u32x4 p, int pos, f32x4 (&o)[D / 16], char *at) {
   typedef typename T::elem e4 __attribute__((ext_vector_type(4)));
   const int lane = threadIdx.x & 63, col = lane & 15, kg = lane >> 4;
 #pragma unroll
-  for (int q = 0; q < QT; q++) {
-#pragma unroll
-    for (int u = 0; u < U; u++)  // [tokens / 4][16 queries][4 tokens]
-      *(u32x2 *)(at + ((u * 4 + kg) * 16 + col) * 8) = u32x2{p[q][u / 2][u % 2 * 2], p[q][u / 2][u % 2 * 2 + 1]};
-    wave_lds_fence();
+  for (int u = 0; u < 2; u++)  // [tokens / 4][16 queries][4 tokens]
+    *(u32x2 *)(at + ((u * 4 + kg) * 16 + col) * 8) = u32x2{p[u * 2], p[u * 2 + 1]};
+  wave_lds_fence();
 #pragma unroll 1
-    for (int t = 0; t < U * 16 && x + t < x1; t++) {
-      if (!sees(a, pos[q], (int)v.token(x + t))) continue;
-      const float w = (float)*(const typename T::elem *)(at + ((t >> 2) * 16 + col) * 8 + (t & 3) * 2);
+  for (int t = 0; t < FEW_TILE && x + t < x1; t++) {
+    if (!sees(a, pos, (int)v.token(x + t))) continue;
+    const float w = (float)*(const typename T::elem *)(at + ((t >> 2) * 16 + col) * 8 + (t & 3) * 2);
 #pragma unroll
-      for (int d = 0; d < D / 16; d++) {
-        const int n = d * 16 + kg * 4;
-        const e4 e = *(const e4 *)(vt + v_at<D>(t, n / 8) + (n % 8) * 2);
+    for (int d = 0; d < D / 16; d++) {
+      const int n = d * 16 + kg * 4;
+      const e4 e = *(const e4 *)(vt + v_at<D>(t, n / 8) + (n % 8) * 2);
 #pragma unroll
-        for (int k = 0; k < 4; k++) o[q][d][k] = fmaf(w, (float)e[k], o[q][d][k]);
-      }
+      for (int k = 0; k < 4; k++) o[d][k] = fmaf(w, (float)e[k], o[d][k]);
     }
-    wave_lds_fence();
   }
+  wave_lds_fence();
 }
 // Whether 16 bytes hold a value that is not finite.
 template <typename T>
@@ -366,30 +364,23 @@ __device__ void end_part(const Args &a, const Tile &t) {
 
 // ------------------------------------------------------------ few queries
 
-// 16 QT queries of a tile, from i0 on, one per column: each of W waves takes 32 tokens
+// 16 queries of a tile, from i0 on, one per column: each of W waves takes 32 tokens
 // at a time through LDS of its own, the next ones' loads in flight; the waves
 // meet once, at the end.
-template <typename T, int D, int QT, int W>
+template <typename T, int D, int W>
 __device__ __forceinline__ void few(const Args &a, const Tile &t, int i0, char *lds) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   constexpr int KS = D / 32, DT = D / 16;
-  u32x4 qv[QT][KS];
-  int pos[QT];
+  u32x4 qv[KS];
+  const Query mine = query_of(a, t, i0 + col);
+  const int pos = mine.head < 0 ? t.view.p1 : mine.pos;
+  load_query<T, D>(a, mine, kg, qv);
+  float *scores = a.scores && mine.head >= 0  // the lane's part of its query's
+                      ? a.scores + ((int64_t)mine.token * a.ch.heads + mine.head) * a.score_tokens + kg * 4 : nullptr;
+  f32x4 o[1][DT];
+  float m[1] = {-INFINITY}, l[1] = {0.f};
 #pragma unroll
-  for (int q = 0; q < QT; q++) {
-    const Query qq = query_of(a, t, i0 + q * 16 + col);
-    pos[q] = qq.head < 0 ? t.view.p1 : qq.pos;
-    load_query<T, D>(a, qq, kg, qv[q]);
-  }
-  f32x4 o[QT][DT];
-  float m[QT], l[QT];
-#pragma unroll
-  for (int q = 0; q < QT; q++) {
-    m[q] = -INFINITY;
-    l[q] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DT; d++) o[q][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int d = 0; d < DT; d++) o[0][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   char *kt = lds + w * FEW_TILE * D * 4, *vt = kt + FEW_TILE * D * 2;
   const int32_t *pages = t.row.pages;
   const uint32_t x1 = t.x1;
@@ -415,17 +406,12 @@ __device__ __forceinline__ void few(const Args &a, const Tile &t, int i0, char *
         st.load(a, t.view, x + STEP, x1, t.head);
         st.find(a, t.view, pages, x + 2 * STEP, x1);
       }
-      f32x4 s[QT][2];
+      f32x4 s[1][2];
 #pragma unroll
       for (int u = 0; u < 2; u++) {
+        s[0][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 0; q < QT; q++) s[q][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KS; k++) {
-          const u32x4 kk = *(const u32x4 *)(kt + k_at<D>(u * 16 + col, k * 4 + kg));
-#pragma unroll
-          for (int q = 0; q < QT; q++) s[q][u] = T::mfma(kk, qv[q][k], s[q][u]);
-        }
+        for (int k = 0; k < KS; k++) s[0][u] = T::mfma(*(const u32x4 *)(kt + k_at<D>(u * 16 + col, k * 4 + kg)), qv[k], s[0][u]);
       }
       if (!whole)
 #pragma unroll
@@ -433,81 +419,63 @@ __device__ __forceinline__ void few(const Args &a, const Tile &t, int i0, char *
 #pragma unroll
           for (int i = 0; i < 4; i++) {
             const uint32_t xx = x + u * 16 + kg * 4 + i;
-            const int token = (int)t.view.token(xx);
-#pragma unroll
-            for (int q = 0; q < QT; q++)
-              if (xx >= x1 || !sees(a, pos[q], token)) s[q][u][i] = -INFINITY;
+            if (xx >= x1 || !sees(a, pos, (int)t.view.token(xx))) s[0][u][i] = -INFINITY;
           }
-      if (a.scores) {  // (a lane's columns of the tile, of its queries)
-#pragma unroll
-        for (int q = 0; q < QT; q++) {
-          const Query qq = query_of(a, t, i0 + q * 16 + col);
-          if (qq.head < 0) continue;
-          float *to = a.scores + ((int64_t)qq.token * a.ch.heads + qq.head) * a.score_tokens + x + kg * 4;
-          *(f32x4 *)to = s[q][0];
-          *(f32x4 *)(to + 16) = s[q][1];
-        }
+      if (scores) {
+        *(f32x4 *)(scores + x) = s[0][0];
+        *(f32x4 *)(scores + x + 16) = s[0][1];
       }
-      softmax_step<T, QT, 2, DT>(s, a.c, m, l, o);
-      u32x4 p[QT][1];
-#pragma unroll
-      for (int q = 0; q < QT; q++) p[q][0] = p_operand<T>(s[q][0], s[q][1]);
+      softmax_step<T, 1, 2, DT>(s, a.c, m, l, o);
+      const u32x4 p = p_operand<T>(s[0][0], s[0][1]);
       if (odd) {  // (in the wave's own K, which is done with)
-        products_one_by_one<T, D, QT, 2>(a, t.view, vt, x, x1, p, pos, o, kt);
+        products_one_by_one<T, D>(a, t.view, vt, x, x1, p, pos, o[0], kt);
       } else {
 #pragma unroll
-        for (int d = 0; d < DT; d++) {
-          const u32x4 v = v_operand<D>(vt, kg * 4, 16 + kg * 4, d, lane);
-#pragma unroll
-          for (int q = 0; q < QT; q++) o[q][d] = T::mfma(v, p[q][0], o[q][d]);
-        }
+        for (int d = 0; d < DT; d++) o[0][d] = T::mfma(v_operand<D>(vt, kg * 4, 16 + kg * 4, d, lane), p, o[0][d]);
       }
       wave_lds_fence();
       if (!more) break;
       x += STEP;
     }
   }
-  // the waves' parts become one: 16 queries at a time through LDS
+  // the waves' parts become one, through LDS
   constexpr int RS = D + 4;  // a query's row, padded against bank conflicts
   float *ro = (float *)lds;  // [W][16][RS], then the maxima and sums
   float2 *rml = (float2 *)(lds + W * 16 * RS * 4);
   const bool any_bad = __syncthreads_or(st.bad);
   if (any_bad && threadIdx.x == 0 && a.status) *a.status = HBF_EINVAL;
+  const float lq = across_rows(l[0], SUM_OP);
+  if (kg == 0) rml[w * 16 + col] = make_float2(m[0], lq);
 #pragma unroll
-  for (int q = 0; q < QT; q++) {
-    const float lq = across_rows(l[q], SUM_OP);
-    if (kg == 0) rml[w * 16 + col] = make_float2(m[q], lq);
+  for (int d = 0; d < DT; d++) *(f32x4 *)(ro + (w * 16 + col) * RS + d * 16 + kg * 4) = o[0][d];
+  __syncthreads();
+  constexpr int PER = W * 64 / 16;  // threads per query
+  const int n = threadIdx.x / PER, d0 = threadIdx.x % PER * 4;
+  const Query qq = query_of(a, t, i0 + n);
+  if (qq.head >= 0) {
+    float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int d = 0; d < DT; d++) *(f32x4 *)(ro + (w * 16 + col) * RS + d * 16 + kg * 4) = o[q][d];
-    __syncthreads();
-    constexpr int PER = W * 64 / 16;  // threads per query
-    const int n = threadIdx.x / PER, d0 = threadIdx.x % PER * 4;
-    const Query qq = query_of(a, t, i0 + q * 16 + n);
-    if (qq.head >= 0) {
-      float mx = -INFINITY, sum = 0.f;
+    for (int i = 0; i < W; i++) mx = fmaxf(mx, rml[i * 16 + n].x);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float f[W];
 #pragma unroll
-      for (int i = 0; i < W; i++) mx = fmaxf(mx, rml[i * 16 + n].x);
-      const float ref = mx == -INFINITY ? 0.f : mx;
-      float f[W];
-#pragma unroll
-      for (int i = 0; i < W; i++) {
-        f[i] = __builtin_amdgcn_exp2f((rml[i * 16 + n].x - ref) * a.c);
-        sum += f[i] * rml[i * 16 + n].y;
-      }
-      const int64_t at = t.parts > 1 ? part_at(a, t, t.split, i0 + q * 16 + n) : 0;
-#pragma unroll
-      for (int d = d0; d < D; d += PER * 4) {
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < W; i++) v += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
-        if (t.parts > 1) hand_over((f32x4 *)(a.part + at * D + d), v);
-        else write_out<T>(a, qq, d, v * one_over(qq, sum, any_bad));
-      }
-      if (d0 == 0 && t.parts == 1) write_sums<T>(a, qq, mx, sum, any_bad);
-      if (d0 == 0 && t.parts > 1) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum));
+    for (int i = 0; i < W; i++) {
+      f[i] = __builtin_amdgcn_exp2f((rml[i * 16 + n].x - ref) * a.c);
+      sum += f[i] * rml[i * 16 + n].y;
     }
-    __syncthreads();
+    const int64_t at = t.parts > 1 ? part_at(a, t, t.split, i0 + n) : 0;
+#pragma unroll
+    for (int d = d0; d < D; d += PER * 4) {
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < W; i++) v += f[i] * *(const f32x4 *)(ro + (i * 16 + n) * RS + d);
+      if (t.parts > 1) hand_over((f32x4 *)(a.part + at * D + d), v);
+      else write_out<T>(a, qq, d, v * one_over(qq, sum, any_bad));
+    }
+    if (d0 == 0 && t.parts == 1) write_sums<T>(a, qq, mx, sum, any_bad);
+    if (d0 == 0 && t.parts > 1) hand_over(a.part_ml + at, any_bad ? make_float2(NAN, NAN) : make_float2(mx, sum));
   }
+  __syncthreads();
 }
 
 // ------------------------------------------------------------ many queries
@@ -809,15 +777,15 @@ template <int D, int W>
 constexpr int few_bytes() {  // K and V of each wave; or the waves' join
   return W * FEW_TILE * D * 4 > W * 16 * ((D + 4) * 4 + 8) ? W * FEW_TILE * D * 4 : W * 16 * ((D + 4) * 4 + 8);
 }
-template <int D, int QT>
+template <int D, bool MANY>
 constexpr int lds_bytes() {
-  return QT ? few_bytes<D, WAVES>() : std::max(RING * 2 * MANY_TILE * D * 2, few_bytes<D, MANY_WAVES>());
+  return !MANY ? few_bytes<D, WAVES>() : std::max(RING * 2 * MANY_TILE * D * 2, few_bytes<D, MANY_WAVES>());
 }
 
-// Tiles of 16 QT queries, or of MANY_Q (QT = 0).
-template <typename T, int D, int QT>
-__global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chunk(Args a) {
-  __shared__ __align__(16) char lds[lds_bytes<D, QT>()];
+// Tiles of 16 queries, or of MANY_Q.
+template <typename T, int D, bool MANY>
+__global__ __launch_bounds__(MANY ? MANY_THREADS : THREADS, MANY ? 1 : 2) void k_chunk(Args a) {
+  __shared__ __align__(16) char lds[lds_bytes<D, MANY>()];
   const int kv_heads = a.layer.kv_heads;
   uint32_t b = blockIdx.x;
   if (b == 0) {  // starts that decrease or leave the queries
@@ -829,10 +797,12 @@ __global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chu
     if (bad && a.status) *a.status = HBF_EINVAL;
   }
   Tile t;
+  const uint32_t groups = (uint32_t)a.slots * kv_heads;
+  t.split = b / groups;
+  b -= t.split * groups;
+  if (!MANY) b = (uint32_t)((uint64_t)b * a.spread % groups);
+  t.place = a.slots - 1 - (int)(b / kv_heads);  // the longest first
   t.head = b % kv_heads;
-  b /= kv_heads;
-  t.place = a.slots - 1 - (int)(b % a.slots);  // the longest first
-  t.split = b / a.slots;
   const int i = find_row(a, t.place);
   t.row = get_row(a, i);
   const int64_t q0 = (int64_t)(t.place - first_tile(a, i, t.row.start)) * a.tile_q, n = (int64_t)t.row.n * a.group;
@@ -840,7 +810,7 @@ __global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chu
   t.q0 = (int)q0;
   t.q1 = (int)min(n, q0 + a.tile_q);
   t.view = view_of(a, t.row, t.q0, t.q1);
-  constexpr uint32_t step = QT ? WAVES * FEW_TILE : MANY_TILE;
+  constexpr uint32_t step = MANY ? MANY_TILE : WAVES * FEW_TILE;
   const uint32_t steps = t.row.ok ? (t.view.total + step - 1) / step : 0;
   if (steps == 0) {  // nothing is seen, or the row is in error
     if (t.split) return;
@@ -856,17 +826,17 @@ __global__ __launch_bounds__(QT ? THREADS : MANY_THREADS, QT ? 2 : 1) void k_chu
   uint32_t most = (steps + a.part_steps - 1) / a.part_steps;
   // (a part's steps and the trips that its join takes: as many of one as of the other, about; one row of 20,000 tokens
   // 22.5 -> 18.7 us)
-  if (QT) most = min(most, (uint32_t)(3.5f * __builtin_sqrtf((float)steps)) + 1);
+  if (!MANY) most = min(most, (uint32_t)(3.5f * __builtin_sqrtf((float)steps)) + 1);
   const uint32_t parts = min(most, (uint32_t)a.splits);
   const uint32_t each = (steps + parts - 1) / parts;
   t.parts = (int)((steps + each - 1) / each);
   if (t.split >= t.parts) return;
   t.x0 = (uint32_t)t.split * each * step;
   t.x1 = min(t.view.total, t.x0 + each * step);
-  if constexpr (QT) {
-    few<T, D, QT, WAVES>(a, t, 0, lds);
+  if constexpr (!MANY) {
+    few<T, D, WAVES>(a, t, 0, lds);
   } else if (many<T, D>(a, t, lds)) {
-    for (int i = 0; i < t.q1 - t.q0; i += 16) few<T, D, 1, MANY_WAVES>(a, t, i, lds);
+    for (int i = 0; i < t.q1 - t.q0; i += 16) few<T, D, MANY_WAVES>(a, t, i, lds);
   }
   if (t.parts > 1) end_part<T, D>(a, t);
 }
@@ -1334,25 +1304,38 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   const int64_t queries = (int64_t)ch.tokens * a.group;
   const int64_t rows = std::max(ch.rows, 1);
   const int64_t longest = (int64_t)kv.table_cols * kv.page_tokens;
-  // Small calls of many queries: their tiles of 256, in parts of 256 tokens, leave most of the card idle.
-  const bool idle = ((queries >> 8) + ch.rows) * layer.kv_heads * (longest / 256 + 1) < 256;
-  a.tile_shift = queries <= 16 * rows ? 4 : queries <= 32 * rows || idle ? 5 : 8;
+  // Tiles of 256 queries or of 16.  Those of 256 read K and V a sixteenth as often, but take 15 us to begin and end, and
+  // to join their parts: for calls of more than 16 queries a row, of at least 450,000 tokens met by tiles of 16 (16 rows
+  // of 64 queries a KV head behind 600 / 2,000 tokens, in tiles of 16 and of 256: 18 and 37 us / 54 and 47), whose
+  // tiles of 256, in parts of 1,024 tokens, take half of the card at least (one row of 2,048 queries behind 2,000: 36
+  // and 68; four of 256 behind 4,096: 59 and 71, behind 8,192: 102 and 79).  As a rule a row is no longer than 16,384,
+  // however wide its table is.
+  const int64_t likely = std::min<int64_t>(longest, 16384);
+  const bool many = queries > 16 * rows && (queries >> 4) * layer.kv_heads * likely >= 450000 &&
+                    std::max(rows, queries >> 8) * layer.kv_heads * (likely / 1024 + 1) >= 128;
+  a.tile_shift = many ? 8 : 4;
   a.tile_q = 1 << a.tile_shift;
   a.slots = (int)(queries >> a.tile_shift) + ch.rows;
   // Parts, so that a card's worth of workgroups have work if all rows are long, twice that where rows of different
   // lengths have to be packed; a tile takes as many as its length gives work for.  Where the tiles alone are a card's
   // worth, a part has 8 steps at least (64 rows of 500 tokens 24.1 -> 19.1 us, of 1,500 47.3 -> 48.5).
   const int64_t groups = (int64_t)a.slots * layer.kv_heads;
-  a.part_steps = a.tile_q == MANY_Q ? 4 : groups >= 256 ? 8 : 2;
-  const int64_t steps = longest / ((a.tile_q == MANY_Q ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
-  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(steps, (a.tile_q == MANY_Q ? 256 : groups < 128 ? 512 : 1024) / groups));
-  // Weights of few queries: from the scores that attention leaves, where those of a tile, written and read, are no
-  // more bytes than K, which is read again else (64 rows of one token behind 4,096: 146 us, else 173; 32 queries
-  // a row and head of 64 values, which go the other way: 99 us, else 90), and within SCORES_BYTES.
+  // Rows of one tile each: places that no row needs may come at a fixed distance, and in the places' order they would
+  // leave some of the XCDs, which take workgroups by turns, idle (64 rows of 16 queries behind 2,048 tokens 91 -> 77
+  // us).  A row's tiles stay side by side, as they read the same (one row of 2,048 queries 36 us, spread 54).
+  a.spread = 1;
+  if (queries <= 16 * rows)
+    for (a.spread = (uint32_t)(groups * 0.618) | 1; std::gcd((uint64_t)a.spread, (uint64_t)groups) != 1; a.spread += 2) {
+    }
+  a.part_steps = many ? 16 : groups >= 256 ? 8 : 2;
+  const int64_t steps = longest / ((many ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
+  const int64_t card = many ? 256 : groups < 128 ? 512 : 1024;
+  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min(steps, card / groups));
+  // Weights of tiles of 16: from the scores that attention leaves (64 rows of 8 queries behind 4,096 tokens: 146 us,
+  // from K again 173), where they take no more than SCORES_BYTES.
   const int64_t held = std::min<int64_t>(longest, ch.weights_tokens);
   a.score_tokens = (held + WAVES * FEW_TILE - 1) / (WAVES * FEW_TILE) * (WAVES * FEW_TILE);
-  a.keep_scores = ch.dev_weights && a.tile_q * 4 <= layer.head_dim &&
-                  ch.tokens * (int64_t)ch.heads * a.score_tokens * 4 <= SCORES_BYTES;
+  a.keep_scores = ch.dev_weights && !many && ch.tokens * (int64_t)ch.heads * a.score_tokens * 4 <= SCORES_BYTES;
   return a;
 }
 
@@ -1380,9 +1363,8 @@ size_t carve(Args &a, char *ws) {
 template <typename T, int D>
 hipError_t run(const Args &a, hipStream_t s) {
   const uint32_t blocks = (uint32_t)((int64_t)a.slots * a.layer.kv_heads * a.splits);
-  if (a.tile_q == 16) k_chunk<T, D, 1><<<blocks, THREADS, 0, s>>>(a);
-  else if (a.tile_q == 32) k_chunk<T, D, 2><<<blocks, THREADS, 0, s>>>(a);
-  else k_chunk<T, D, 0><<<blocks, MANY_THREADS, 0, s>>>(a);
+  if (a.tile_q == MANY_Q) k_chunk<T, D, true><<<blocks, MANY_THREADS, 0, s>>>(a);
+  else k_chunk<T, D, false><<<blocks, THREADS, 0, s>>>(a);
   if (a.ch.dev_weights) {
     const int64_t groups = (int64_t)a.ch.rows * a.layer.kv_heads;
     const int64_t longest = std::min<int64_t>((int64_t)a.kv.table_cols * a.kv.page_tokens, a.ch.weights_tokens);
