@@ -191,24 +191,44 @@ CASES = [
 
 
 
-# Tables that could hold far more: calls of many queries are then cut into tiles of 256, and else, so small, of 32.
-@pytest.mark.parametrize("cols", [0, 5000])
+# In tables that could hold 19,200 tokens more: such calls are cut into tiles of 256 queries.
+WIDE_CASES = [
+    (12, 4, 64, [130, 0, 3, 24, 25], [130, 9, 99, 24, 500], 24, 0, 0),
+    (32, 8, 128, [70], [70], 16, 0, 0),
+    (64, 8, 128, [50, 1, 1], [600, 2000, 3], 16, 0, 0),
+    (64, 8, 128, [33], [2000], 1, 0, 0),
+    (8, 8, 64, [200], [333], 64, 0, 0),
+    (24, 8, 128, [19, 5], [4, 5], 256, 0, 0),       # more new tokens than there are
+    (32, 8, 128, [100, 30], [1000, 45], 16, 64, 4),
+    (8, 8, 64, [150], [150], 16, 1, 0),
+    (8, 8, 64, [150], [700], 16, 1, 1),
+    (64, 8, 128, [40], [900], 7, 17, 200),
+    (64, 8, 64, [300], [301], 24, 128, 33),
+    (32, 8, 128, [64], [2000], 16, 5000, 4),
+    (32, 8, 64, [30], [400], 16, 2 ** 31 - 1, 2 ** 31 - 1),
+    (64, 8, 128, [64], [5000], 16, 0, 0),           # in parts
+]
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
-@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
-def test_against_64_bits(torch, case, dtype, cols):
+@pytest.mark.parametrize("case,cols", [(c, 0) for c in CASES] + [(c, 19200) for c in WIDE_CASES],
+                         ids=lambda c: "-".join(map(str, c)).replace(" ", "") if isinstance(c, tuple) else str(c))
+def test_against_64_bits(torch, case, cols, dtype):
     heads, kv_heads, dim, new, lens, page, window, sinks = case
     say(f"attention {case} {dtype} {cols}")
-    b = Batch(torch, heads, kv_heads, dim, new, lens, page, dtype, seed=sum(lens), tail=2, head=1, cols=cols * 16 // page)
+    b = Batch(torch, heads, kv_heads, dim, new, lens, page, dtype, seed=sum(lens), tail=2, head=1, cols=cols // page)
     for weights in (None, b.weights):
         got_w = None if weights is None else weights.clone()
         out, lse = b.run(weights=got_w, window=window, sinks=sinks)
         assert b.kv.get_status() == OK
         b.check(out, lse, b.reference(window=window, sinks=sinks, weights=weights), got_w)
+    scores = b.q.shape[0] * heads * b.weights.shape[-1] * 4   # bytes that tiles of 16 would leave
+    assert not cols or scores > 512 << 20 or b.kv._chunk_bytes < scores, "tiles of 256"
 
 
-# heads, kv heads, dim, new tokens, lengths, page, extra columns: few queries; tiles of 32; of 256, in parts or not
+# heads, kv heads, dim, new tokens, lengths, page, extra columns: tiles of 16, one a row or more; of 256, in parts
 SHAPES = [(8, 2, 64, [1, 1, 2], [40, 300, 7], 16, 0), (8, 2, 128, [30, 1], [200, 77], 16, 0),
-          (8, 2, 128, [60, 20], [700, 30], 16, 5000), (8, 8, 64, [300], [1200], 24, 5000)]
+          (16, 4, 128, [60, 20], [2100, 30], 16, 1200), (8, 8, 64, [300], [1200], 24, 800)]
 IDS = [f"{s[0]}x{s[2]}-{s[6]}" for s in SHAPES]
 
 
@@ -393,7 +413,7 @@ def test_rows_of_one_slot(torch, shape):
 def test_many_rows(torch):
     """More rows than are searched at a time, and than a workgroup has threads; rows without tokens among them."""
     rng = np.random.default_rng(11)
-    for rows, top, cols in ((70, 3, 0), (4200, 2, 0), (600, 40, 3000)):
+    for rows, top, cols in ((70, 3, 0), (4200, 2, 0), (600, 40, 3000), (300, 60, 3000)):
         say(f"attention {rows} rows")
         new = rng.integers(0, top, rows)
         lens = np.maximum(new, rng.integers(0, 9, rows))
@@ -415,7 +435,7 @@ def test_weights_beside_tables_of_millions_of_tokens(torch, heads, kv_heads, dim
         out, lse = b.run(weights=w, window=200, sinks=5)
         b.check(out, lse, b.reference(window=200, sinks=5, weights=b.weights), w)
         need = b.q.shape[0] * heads * b.weights.shape[-1] * 4
-        assert (need > 512 << 20) == (b.kv._attn_ws._t.numel() < need), "the scratch is what the scores say"
+        assert (need > 512 << 20) == (b.kv._chunk_bytes < need), "the scratch is what the scores say"
 
 
 def test_offsets_past_32_bits(torch):
