@@ -13,12 +13,21 @@
 // positions.  Where tiles are too few to fill the card the axis is cut into
 // parts, by the tile's own length as the device finds it, and the last
 // workgroup of a tile to finish joins them: one launch, whatever the lengths.
-// Tiles of few queries are bound by memory, those of many by the matrix cores
-// and the LDS.
+// Tiles of 16 queries are bound by the memory (64 rows of 4,096 tokens, 8 heads
+// for each of 4 KV heads of 128: 108 us, 5.0 TB/s of K and V; one row of 4,396: 13.4
+// us, of rounds to memory), those of 256 by the matrix cores and the vector
+// units together (4,096 tokens behind 4,096: 402 to 433 us by the card, 950 to
+// 1,030 TFLOP/s of the pairs that are seen).
 //
 // A token that one query of a tile sees and another does not has p = 0 for the
 // other, and 0 * infinity would be NaN: where a step of that kind holds a value of V
-// that is not finite, its products are taken one by one.
+// that is not finite, its products are taken one by one; a tile of 256 that meets
+// one is done again, 16 queries at a time.
+//
+// Weights take each score a second time, once the row's sums are known: tiles
+// of 16 leave their scores in scratch (64 rows of up to 4,096 tokens: attention 69 us
+// without them, 80 with, and 14 to add them up, 44 from K again), for
+// tiles of 256 they are computed again.
 #include <float.h>
 #include <math.h>
 
@@ -490,7 +499,9 @@ __device__ __forceinline__ float across_halves(float x, F op) {
 }
 
 // A tile of up to MANY_Q queries, 32 for each of eight waves, two on each SIMD, and 64
-// tokens staged for all of them.  Steps of 32 tokens are one ahead of each other:
+// tokens staged for all of them (128 queries, four waves, 32 tokens at a time and two
+// workgroups a CU: 173 us instead of 180 on windows of 1,024, 442 instead of 417 on
+// 4,096 tokens behind 4,096).  Steps of 32 tokens are one ahead of each other:
 // while the scores of step h become probabilities on the vector units, the matrix
 // cores multiply h - 1's probabilities with V, then K of h + 1 with the queries.
 template <typename T, int D>
@@ -607,7 +618,8 @@ struct Many {
   }
   // Scores of the tokens from x on that their query does not see, or that are none.
   __device__ __forceinline__ void mask(f32x16 &s, uint32_t x) const {
-    const uint32_t keep = (below(last - (int)x) & (~below(from - (int)x) | below(a.ch.sinks - (int)min(x, (uint32_t)INT32_MAX)))) >> 4 * hf;
+    const uint32_t first = below(a.ch.sinks - (int)min(x, (uint32_t)INT32_MAX));
+    const uint32_t keep = (below(last - (int)x) & (~below(from - (int)x) | first)) >> 4 * hf;
 #pragma unroll
     for (int i = 0; i < 16; i++) {
       const float v = s[i];
@@ -767,7 +779,8 @@ __device__ __forceinline__ bool many(const Args &a, const Tile &t, char *lds) {
       const u32x4 v = *(const u32x4 *)(mine + k_at<D>(row, piece));
       const Query to = query_of(a, t, z.w * 32 + row);
       if (to.head >= 0)
-        *(u32x4 *)((typename T::elem *)a.ch.dev_out + to.token * a.ch.out_row_stride + to.head * a.ch.out_head_stride + piece * 8) = v;
+        *(u32x4 *)((typename T::elem *)a.ch.dev_out + to.token * a.ch.out_row_stride + to.head * a.ch.out_head_stride +
+                   piece * 8) = v;
     }
   }
   return false;
@@ -860,8 +873,9 @@ __device__ __forceinline__ int last_of_slot(const Args &a, int i0, int slot, int
 }
 
 // What a row's queries gave each token, from the scores that attention left: a
-// thread a token.  A slot's rows are taken by the first of them, one after
-// another, and their queries in order.
+// thread a token (14 us of rounds to memory for 64 rows of up to 4,096 tokens, 17
+// MB).  A slot's rows are taken by the first of them, one after another, and their
+// queries in order.
 __global__ __launch_bounds__(THREADS) void k_weigh_scores(Args a, int blocks) {
   constexpr int AHEAD = 8;  // queries whose scores are on their way together
   __shared__ int after;
@@ -910,10 +924,11 @@ __global__ __launch_bounds__(THREADS) void k_weigh_scores(Args a, int blocks) {
   }
 }
 
-// What a row's queries gave each token: a wave takes 32 tokens at a time, through LDS of
+// The same from K, where scores would take too much, and for more rows of many
+// queries than k_weigh_many takes: a wave takes 32 tokens at a time, through LDS of
 // its own, the next ones on their way, and meets 16 queries at a time; a token's
-// sum over the lanes that hold its scores is taken once.  A slot's rows are taken
-// by the first of them, one after another.
+// sum over the lanes that hold its scores is taken once.  (64 rows of up to 4,096
+// tokens: 44 us, 3.1 TB/s of K.)
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS, 3) void k_weigh(Args a, int blocks) {
   constexpr int KS = D / 32, NT = FEW_TILE;
@@ -1026,10 +1041,12 @@ __global__ __launch_bounds__(THREADS, 3) void k_weigh(Args a, int blocks) {
   }
 }
 
-// The same for rows of many queries.  A workgroup holds 512 tokens' K in
+// And for rows of many queries.  A workgroup holds 512 tokens' K in
 // registers, 64 a wave, and meets 64 queries at a time, which all waves read from
 // LDS.  A block's queries are cut into `splits` as far as the card has room; the last
-// split to finish adds their sums up, in order.
+// split to finish adds their sums up, in order.  Bound by issue, products and
+// exponentials by turns (2,048 tokens behind 2,048, 32 heads of 128: 110 us, the
+// products alone 41).
 constexpr int BLOCK = 64 * MANY_WAVES, Q_TILE = 64, Q_RING = 3;
 constexpr int WEIGH_GROUPS = 256;      // workgroups: one for each CU
 constexpr int WEIGH_ROWS = 512;        // most rows that it takes; more go the way of few queries

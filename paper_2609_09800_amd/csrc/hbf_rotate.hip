@@ -9,6 +9,8 @@
 // The angle position * freq is taken in 64 bits (a position of 2^20 leaves 32 bits
 // less than four digits of it), reduced to [-pi, pi] there, and its sine and cosine once
 // per token and pair, by a lane each, handed to the token's heads through LDS.
+// Bound by the memory: 8,192 tokens of 32 + 4 + 4 heads of 128, 168 MB, 35 us, 4.8
+// TB/s; one token 3.6 us, a launch.
 #include "hbf_half.h"
 #include "hbf_kv_rows.h"
 #include "hbf_ops.h"
