@@ -68,6 +68,7 @@ struct Args {
   int tile_q, tile_shift;  // queries per tile, 16 or MANY_Q, and its logarithm
   int slots;          // places for tiles: tokens * group / tile_q + rows
   int splits;         // most parts of a tile
+  bool one_tile;      // a row's queries are one tile of 16, as a rule
   uint32_t spread;    // tiles of few queries: workgroup b takes place and head b * spread % their number
   int part_steps;     // least steps of a part
   float *part;        // [slots][kv_heads][splits][tile_q][head_dim] sums of p v
@@ -187,7 +188,7 @@ __device__ __forceinline__ int64_t from_lane(int64_t v, int lane) {
   return (int64_t)((uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32 | (uint32_t)__shfl((int)v, lane));
 }
 
-template <int D, int NT, bool V = true>
+template <int D, int NT, bool V, bool ONCE>
 struct Stage : Places<D, NT> {
   using P = Places<D, NT>;
   u32x4 k[P::PASSES], v[P::PASSES];
@@ -198,9 +199,15 @@ struct Stage : Places<D, NT> {
 #pragma unroll
     for (int j = 0; j < P::PASSES; j++) {
       const int64_t mine = from_lane(at, j * P::AT_ONCE + lane / P::LANES) + lane % P::LANES * 16;
-      // (past the caches' order: one tile holds all of a row's queries as a rule, and nobody else reads them)
-      k[j] = __builtin_nontemporal_load((const u32x4 *)((const char *)a.layer.dev_k + mine));
-      if (V) v[j] = __builtin_nontemporal_load((const u32x4 *)((const char *)a.layer.dev_v + mine));
+      const u32x4 *kp = (const u32x4 *)((const char *)a.layer.dev_k + mine);
+      const u32x4 *vp = (const u32x4 *)((const char *)a.layer.dev_v + mine);
+      if (ONCE) {  // past the caches' order, as nobody else reads them (64 rows of 4,096 tokens 122 -> 110 us)
+        k[j] = __builtin_nontemporal_load(kp);
+        if (V) v[j] = __builtin_nontemporal_load(vp);
+      } else {  // a row's tiles find them there (4 rows of 32 tokens behind 4,096: 52 us, 59 the other way)
+        k[j] = *kp;
+        if (V) v[j] = *vp;
+      }
     }
   }
   // To tiles of K and V.  What lies behind the last token may be anything: 0 * NaN
@@ -376,7 +383,7 @@ __device__ void end_part(const Args &a, const Tile &t) {
 // 16 queries of a tile, from i0 on, one per column: each of W waves takes 32 tokens
 // at a time through LDS of its own, the next ones' loads in flight; the waves
 // meet once, at the end.
-template <typename T, int D, int W>
+template <typename T, int D, int W, bool ONCE>
 __device__ __forceinline__ void few(const Args &a, const Tile &t, int i0, char *lds) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 15, kg = lane >> 4;
   constexpr int KS = D / 32, DT = D / 16;
@@ -394,7 +401,7 @@ __device__ __forceinline__ void few(const Args &a, const Tile &t, int i0, char *
   const int32_t *pages = t.row.pages;
   const uint32_t x1 = t.x1;
   uint32_t x = t.x0 + w * FEW_TILE;
-  Stage<D, FEW_TILE> st;
+  Stage<D, FEW_TILE, true, ONCE> st;
   constexpr uint32_t STEP = W * FEW_TILE;
   if (x < x1) {
     st.find(a, t.view, pages, x, x1);
@@ -795,8 +802,8 @@ constexpr int lds_bytes() {
   return !MANY ? few_bytes<D, WAVES>() : std::max(RING * 2 * MANY_TILE * D * 2, few_bytes<D, MANY_WAVES>());
 }
 
-// Tiles of 16 queries, or of MANY_Q.
-template <typename T, int D, bool MANY>
+// Tiles of 16 queries (ONCE: one a row, as a rule), or of MANY_Q.
+template <typename T, int D, bool MANY, bool ONCE>
 __global__ __launch_bounds__(MANY ? MANY_THREADS : THREADS, MANY ? 1 : 2) void k_chunk(Args a) {
   __shared__ __align__(16) char lds[lds_bytes<D, MANY>()];
   const int kv_heads = a.layer.kv_heads;
@@ -847,9 +854,9 @@ __global__ __launch_bounds__(MANY ? MANY_THREADS : THREADS, MANY ? 1 : 2) void k
   t.x0 = (uint32_t)t.split * each * step;
   t.x1 = min(t.view.total, t.x0 + each * step);
   if constexpr (!MANY) {
-    few<T, D, WAVES>(a, t, 0, lds);
+    few<T, D, WAVES, ONCE>(a, t, 0, lds);
   } else if (many<T, D>(a, t, lds)) {
-    for (int i = 0; i < t.q1 - t.q0; i += 16) few<T, D, MANY_WAVES>(a, t, i, lds);
+    for (int i = 0; i < t.q1 - t.q0; i += 16) few<T, D, MANY_WAVES, false>(a, t, i, lds);
   }
   if (t.parts > 1) end_part<T, D>(a, t);
 }
@@ -976,7 +983,7 @@ __global__ __launch_bounds__(THREADS, 3) void k_weigh(Args a, int blocks) {
   Queries mine = load(own, 0);
   uint32_t x = ((uint32_t)block * WAVES + w) * NT;
   if (x >= len) return;  // (a whole wave; no barrier follows)
-  Stage<D, NT, false> st;
+  Stage<D, NT, false, true> st;
   st.find(a, all, first.pages, x, len);
   st.load(a, all, x, len, head);
   st.find(a, all, first.pages, min(x + step, len - 1), len);
@@ -1325,7 +1332,7 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   // to join their parts: for calls of more than 16 queries a row, of at least 450,000 tokens met by tiles of 16 (16 rows
   // of 64 queries a KV head behind 600 / 2,000 tokens, in tiles of 16 and of 256: 18 and 37 us / 54 and 47), whose
   // tiles of 256, in parts of 1,024 tokens, take half of the card at least (one row of 2,048 queries behind 2,000: 36
-  // and 68; four of 256 behind 4,096: 59 and 71, behind 8,192: 102 and 79).  As a rule a row is no longer than 16,384,
+  // and 68; four of 256 behind 4,096: 51 and 71, behind 8,192: 102 and 79).  As a rule a row is no longer than 16,384,
   // however wide its table is.
   const int64_t likely = std::min<int64_t>(longest, 16384);
   const bool many = queries > 16 * rows && (queries >> 4) * layer.kv_heads * likely >= 450000 &&
@@ -1340,8 +1347,9 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   // Rows of one tile each: places that no row needs may come at a fixed distance, and in the places' order they would
   // leave some of the XCDs, which take workgroups by turns, idle (64 rows of 16 queries behind 2,048 tokens 91 -> 77
   // us).  A row's tiles stay side by side, as they read the same (one row of 2,048 queries 36 us, spread 54).
+  a.one_tile = queries <= 16 * rows;
   a.spread = 1;
-  if (queries <= 16 * rows)
+  if (a.one_tile)
     for (a.spread = (uint32_t)(groups * 0.618) | 1; std::gcd((uint64_t)a.spread, (uint64_t)groups) != 1; a.spread += 2) {
     }
   a.part_steps = many ? 16 : groups >= 256 ? 8 : 2;
@@ -1380,8 +1388,9 @@ size_t carve(Args &a, char *ws) {
 template <typename T, int D>
 hipError_t run(const Args &a, hipStream_t s) {
   const uint32_t blocks = (uint32_t)((int64_t)a.slots * a.layer.kv_heads * a.splits);
-  if (a.tile_q == MANY_Q) k_chunk<T, D, true><<<blocks, MANY_THREADS, 0, s>>>(a);
-  else k_chunk<T, D, false><<<blocks, THREADS, 0, s>>>(a);
+  if (a.tile_q == MANY_Q) k_chunk<T, D, true, false><<<blocks, MANY_THREADS, 0, s>>>(a);
+  else if (a.one_tile) k_chunk<T, D, false, true><<<blocks, THREADS, 0, s>>>(a);
+  else k_chunk<T, D, false, false><<<blocks, THREADS, 0, s>>>(a);
   if (a.ch.dev_weights) {
     const int64_t groups = (int64_t)a.ch.rows * a.layer.kv_heads;
     const int64_t longest = std::min<int64_t>((int64_t)a.kv.table_cols * a.kv.page_tokens, a.ch.weights_tokens);
