@@ -1329,11 +1329,11 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   const int64_t rows = std::max(ch.rows, 1);
   const int64_t longest = (int64_t)kv.table_cols * kv.page_tokens;
   // Tiles of 256 queries or of 16.  Those of 256 read K and V a sixteenth as often, but take 15 us to begin and end, and
-  // to join their parts: for calls of more than 16 queries a row, of at least 450,000 tokens met by tiles of 16 (16 rows
-  // of 64 queries a KV head behind 600 / 2,000 tokens, in tiles of 16 and of 256: 18 and 37 us / 54 and 47), whose
-  // tiles of 256, in parts of 1,024 tokens, take half of the card at least (one row of 2,048 queries behind 2,000: 36
-  // and 68; four of 256 behind 4,096: 51 and 71, behind 8,192: 102 and 79).  As a rule a row is no longer than 16,384,
-  // however wide its table is.
+  // more to join their parts: for calls of more than 16 queries a row and KV head, of at least 450,000 tokens met by
+  // tiles of 16 (4 rows of 128 queries in 1,000 tokens, 4 KV heads, in tiles of 16 and of 256: 17 and 36 us; 16 of 64
+  // in 2,000: 54 and 47), whose tiles of 256, in parts of 1,024 tokens, take half of the card at least (one row of
+  // 2,048 queries in 2,000: 36 and 68; four of 256 in 4,096: 51 and 71, in 8,192: 102 and 79).  As a rule a row is no
+  // longer than 16,384, however wide its table is.
   const int64_t likely = std::min<int64_t>(longest, 16384);
   const bool many = queries > 16 * rows && (queries >> 4) * layer.kv_heads * likely >= 450000 &&
                     std::max(rows, queries >> 8) * layer.kv_heads * (likely / 1024 + 1) >= 128;
