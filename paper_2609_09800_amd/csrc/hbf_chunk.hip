@@ -26,8 +26,8 @@
 //
 // Weights take each score a second time, once the row's sums are known: tiles
 // of 16 leave their scores in scratch (64 rows of up to 4,096 tokens: attention 69 us
-// without them, 80 with, and 14 to add them up, 44 from K again), for
-// tiles of 256 they are computed again.
+// without them, 80 with, and 14 to add them up, 44 from K again), for rows of many
+// queries they are computed again.
 #include <float.h>
 #include <math.h>
 
@@ -50,6 +50,7 @@ constexpr int MANY_Q = 256;    // queries of a tile there
 constexpr int MANY_WAVES = MANY_Q / 32, MANY_THREADS = 64 * MANY_WAVES;
 
 constexpr int64_t SCORES_BYTES = 512 << 20;  // most that scores are kept in
+constexpr int SCORES_QUERIES = 256;          // and the queries of a row and KV head whose are, as a rule
 
 constexpr float LARGE = 1 << 22;  // of a score, times c: beyond, its rounding shows in exp2
 
@@ -880,54 +881,66 @@ __device__ __forceinline__ int last_of_slot(const Args &a, int i0, int slot, int
 }
 
 // What a row's queries gave each token, from the scores that attention left: a
-// thread a token (14 us of rounds to memory for 64 rows of up to 4,096 tokens, 17
-// MB).  A slot's rows are taken by the first of them, one after another, and their
-// queries in order.
+// thread a token, with W = 4 a thread of each wave, whose queries are every fourth
+// 8 (14 us of rounds to memory for 64 rows of up to 4,096 tokens, 17 MB).  A slot's
+// rows are taken by the first of them, one after another, and their queries in
+// order.
+template <int W>
 __global__ __launch_bounds__(THREADS) void k_weigh_scores(Args a, int blocks) {
-  constexpr int AHEAD = 8;  // queries whose scores are on their way together
+  constexpr int AHEAD = 8;  // queries whose scores are on their way together; of one tile
+  constexpr int TOKENS = THREADS / W;
   __shared__ int after;
+  __shared__ float part[W][TOKENS];
+  const int w = W == 1 ? 0 : threadIdx.x / TOKENS, mine = threadIdx.x % TOKENS;
   int b = blockIdx.x;
   const int head = b % a.layer.kv_heads;
   b /= a.layer.kv_heads;
   const int i0 = b % a.ch.rows, block = b / a.ch.rows;
   const int slot = a.ch.dev_slots[i0];
   const Row first = get_row(a, i0);
-  if (!first.ok || block * THREADS >= first.len) return;
+  if (!first.ok || block * TOKENS >= first.len) return;
   const int last = last_of_slot(a, i0, slot, &after);
   if (last < 0) return;
   float *out = a.ch.dev_weights + slot * a.ch.weights_slot_stride + head * a.ch.weights_head_stride;
-  for (int64_t j0 = (int64_t)block * THREADS; j0 < first.len; j0 += (int64_t)blocks * THREADS) {
-    const uint32_t j = (uint32_t)j0 + threadIdx.x;
+  for (int64_t j0 = (int64_t)block * TOKENS; j0 < first.len; j0 += (int64_t)blocks * TOKENS) {
+    const uint32_t j = (uint32_t)j0 + mine;
     const bool there = j < (uint32_t)first.len;
-    const float old = there ? out[j] : 0.f;
+    const float old = there && w == 0 ? out[j] : 0.f;
     float sum = 0.f;
     for (int i = i0; i <= last; i++) {
       if (i > i0 && a.ch.dev_slots[i] != slot) continue;
       const Row r = i == i0 ? first : get_row(a, i);
-      for (int q0 = 0; q0 < r.n * a.group; q0 += a.tile_q) {
-        const int q1 = min(q0 + a.tile_q, r.n * a.group);
-        const View v = view_of(a, r, q0, q1);
+      const int n = r.n * a.group;
+      for (int q = w * AHEAD; q < n; q += W * AHEAD) {
+        const int q0 = q & ~(a.tile_q - 1);  // its tile, whose axis the scores lie along
+        const View v = view_of(a, r, q0, min(q0 + a.tile_q, n));
         const uint32_t x = j < v.first ? j : j - v.lo + v.first;
         const bool has = there && (j < v.first || j >= v.lo) && x < v.total;
         if (!__any(has)) continue;
         const float *from = a.scores + x;
-        for (int q = q0; q < q1; q += AHEAD) {
-          float s[AHEAD];
-          float2 ml[AHEAD];
+        float s[AHEAD];
+        float2 ml[AHEAD];
 #pragma unroll
-          for (int k = 0; k < AHEAD; k++) {
-            const int qq = min(q + k, q1 - 1), tok = token_of(a, qq);
-            const int64_t at = (int64_t)(r.start + tok) * a.ch.heads + head * a.group + qq - tok * a.group;
-            ml[k] = a.query_ml[at];
-            s[k] = has ? from[at * a.score_tokens] : 0.f;
-          }
-#pragma unroll
-          for (int k = 0; k < AHEAD; k++)
-            sum += has && q + k < q1 && ml[k].y != 0.f ? __builtin_amdgcn_exp2f((s[k] - ml[k].x) * a.c) * ml[k].y : 0.f;
+        for (int k = 0; k < AHEAD; k++) {
+          const int qq = min(q + k, n - 1), tok = token_of(a, qq);
+          const int64_t at = (int64_t)(r.start + tok) * a.ch.heads + head * a.group + qq - tok * a.group;
+          ml[k] = a.query_ml[at];
+          s[k] = has ? from[at * a.score_tokens] : 0.f;
         }
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++)
+          sum += has && q + k < n && ml[k].y != 0.f ? __builtin_amdgcn_exp2f((s[k] - ml[k].x) * a.c) * ml[k].y : 0.f;
       }
     }
-    if (there && sum != 0.f) out[j] = old + sum;  // (NaN too; a token that nobody sees has 0)
+    if (W > 1) {
+      part[w][mine] = sum;
+      __syncthreads();
+      sum = 0.f;
+      if (w == 0)
+        for (int k = 0; k < W; k++) sum += part[k][mine];
+      __syncthreads();
+    }
+    if (w == 0 && there && sum != 0.f) out[j] = old + sum;  // (NaN too; a token that nobody sees has 0)
   }
 }
 
@@ -1356,11 +1369,13 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   const int64_t steps = longest / ((many ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
   const int64_t card = many ? 256 : groups < 128 ? 512 : 1024;
   a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min(steps, card / groups));
-  // Weights of tiles of 16: from the scores that attention leaves (64 rows of 8 queries behind 4,096 tokens: 146 us,
-  // from K again 173), where they take no more than SCORES_BYTES.
+  // Weights of tiles of 16: from the scores that attention leaves, where they take no more than SCORES_BYTES (64 rows of
+  // 8 queries behind 4,096 tokens: 146 us, from K again 173) and are not many for each token (one row of 256 queries
+  // behind 4,096: 35, from K by k_weigh_many 39; of 1,024 behind 1,000, the other way: 134 and 42).
   const int64_t held = std::min<int64_t>(longest, ch.weights_tokens);
   a.score_tokens = (held + WAVES * FEW_TILE - 1) / (WAVES * FEW_TILE) * (WAVES * FEW_TILE);
-  a.keep_scores = ch.dev_weights && !many && ch.tokens * (int64_t)ch.heads * a.score_tokens * 4 <= SCORES_BYTES;
+  a.keep_scores = ch.dev_weights && !many && queries <= SCORES_QUERIES * rows &&
+                  ch.tokens * (int64_t)ch.heads * a.score_tokens * 4 <= SCORES_BYTES;
   return a;
 }
 
@@ -1380,7 +1395,7 @@ size_t carve(Args &a, char *ws) {
   if (a.ch.dev_weights) {
     a.query_ml = (float2 *)take((size_t)a.ch.tokens * a.ch.heads * 8);
     if (a.keep_scores) a.scores = (float *)take((size_t)a.ch.tokens * a.ch.heads * a.score_tokens * 4);
-    if (a.tile_q == MANY_Q && a.ch.dev_ctl) a.part_w = (float *)take((size_t)WEIGH_GROUPS * BLOCK * 4);
+    if (!a.keep_scores && !a.one_tile && a.ch.dev_ctl) a.part_w = (float *)take((size_t)WEIGH_GROUPS * BLOCK * 4);
   }
   return std::max(o, size_t(256));
 }
@@ -1394,13 +1409,14 @@ hipError_t run(const Args &a, hipStream_t s) {
   if (a.ch.dev_weights) {
     const int64_t groups = (int64_t)a.ch.rows * a.layer.kv_heads;
     const int64_t longest = std::min<int64_t>((int64_t)a.kv.table_cols * a.kv.page_tokens, a.ch.weights_tokens);
-    if (a.tile_q == MANY_Q && a.ch.rows <= WEIGH_ROWS) {
-      k_weigh_many<T, D><<<WEIGH_GROUPS, MANY_THREADS, 0, s>>>(a);
+    if (a.keep_scores) {
+      const int64_t each = std::max<int64_t>(1, std::min<int64_t>(longest / (a.one_tile ? THREADS : 64) + 1, 8192 / groups));
+      if (a.one_tile) k_weigh_scores<1><<<(uint32_t)(groups * each), THREADS, 0, s>>>(a, (int)each);
+      else k_weigh_scores<WAVES><<<(uint32_t)(groups * each), THREADS, 0, s>>>(a, (int)each);
       return hipGetLastError();
     }
-    if (a.keep_scores) {
-      const int64_t each = std::max<int64_t>(1, std::min<int64_t>(longest / THREADS + 1, 8192 / groups));
-      k_weigh_scores<<<(uint32_t)(groups * each), THREADS, 0, s>>>(a, (int)each);
+    if (!a.one_tile && a.ch.rows <= WEIGH_ROWS) {
+      k_weigh_many<T, D><<<WEIGH_GROUPS, MANY_THREADS, 0, s>>>(a);
       return hipGetLastError();
     }
     const int64_t most = longest / (WAVES * FEW_TILE) + 1;
