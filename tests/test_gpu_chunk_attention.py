@@ -557,3 +557,35 @@ def test_another_stream_and_graph(torch, shape):
         eager, eager_lse = b.run(weights=w2)
         rows = slice(int(b.starts[0]), int(b.starts[-1]))
         assert torch.equal(out[rows], eager[rows]) and torch.equal(lse[rows], eager_lse[rows]) and torch.equal(w, w2)
+
+
+def test_largest_calls(torch):
+    """As many rows, tokens, heads of a group and tokens of a page as a call takes.  Where a query sees its own
+    token alone the result is that token's V, whose weight grows by one a query head."""
+    from paper_2609_09800_amd import hbf
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    # rows, new tokens of each, heads, kv heads, page, window
+    for rows, new, heads, kv_heads, page, window in ((65535, 1, 2, 1, 1, 0), (1, 1 << 20, 16, 2, 16, 1), (3, 5, 1024, 1, 65536, 1),
+                                                     (2, 1, 1024, 1024, 4, 0), (512, 2048, 1, 1, 256, 1), (5000, 200, 1, 1, 8, 1)):
+        say(f"attention largest {rows} {new} {heads}/{kv_heads} {page}")
+        held = -(-new // page)
+        pool = torch.randn((1, 2, rows * held, page, kv_heads, 64), generator=gen, device="cuda").bfloat16()
+        tables = torch.arange(rows * held, **i32).view(rows, held).flip(0).contiguous()
+        kv = hbf.KvPages(pool, refs=torch.ones(rows * held, **i32), tables=tables, lens=torch.full((rows,), new, **i32))
+        q = torch.randn((rows * new, heads, 64), generator=gen, device="cuda").bfloat16()
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+        w = torch.zeros((rows, kv_heads, new), device="cuda")
+        slots, starts = torch.arange(rows, **i32), torch.arange(0, rows * new + 1, new, **i32)
+        assert kv.attention(0, q, out, slots, starts, lse=lse, weights=w, window=window) == OK
+        assert kv.get_status() == OK
+        v = pool[0, 1][tables.long()].flatten(1, 2)[:, :new].flatten(0, 1)   # [rows * new, kv heads, 64]
+        want = v.repeat_interleave(heads // kv_heads, 1)
+        # the bounds above for one token: sum p |v| is |v|, and |q k| at most the product of both norms
+        k = pool[0, 0][tables.long()].flatten(1, 2)[:, :new].flatten(0, 1)
+        ds = (64 + 8) * 2.0 ** -23 * float(q.float().norm(dim=-1).max() * k.float().norm(dim=-1).max()) / 8
+        bound = 2 * U["bfloat16"] + 2 * ds + 17 * 2.0 ** -23
+        assert bool(((out.float() - want.float()).abs() <= bound * want.float().abs()).all())
+        n = heads // kv_heads
+        assert bool(((w - n).abs() <= n * (4 * ds + 34 * 2.0 ** -23) + (n + 4) * 2.0 ** -24 * n).all())
+        del pool, q, out, want, v, k, kv

@@ -302,3 +302,32 @@ def test_another_stream_and_graph(torch):
         for n in ("weights", "tables", "refs", "lens", "pool"):
             assert torch.equal(c.dev[n], d.dev[n]), n
         assert c.kv.get_status() == OK
+
+
+def test_largest_lists(torch):
+    """65,535 slots of one layer; and more choices a launch than the moves have workgroups for."""
+    for slots, heads, layers, L, keep, recent in ((65535, 1, 1, 3, 2, 1), (600, 16, 4, 40, 24, 8)):
+        say(f"evict largest {slots} {heads} {layers}")
+        from paper_2609_09800_amd import hbf
+        i32 = dict(dtype=torch.int32, device="cuda")
+        held = -(-L // 8)
+        gen = torch.Generator(device="cuda").manual_seed(9)
+        pool = torch.randn((layers, 2, slots * held, 8, heads, 64), generator=gen, device="cuda").bfloat16()
+        tables, lens = torch.arange(slots * held, **i32).view(slots, held).flip(0).contiguous(), torch.full((slots,), L, **i32)
+        old, was = pool.clone(), tables.clone()
+        kv = hbf.KvPages(pool, refs=torch.ones(slots * held, **i32), tables=tables, lens=lens)
+        w = torch.rand((layers, slots, heads, L), generator=gen, device="cuda")
+        w0 = w.clone()
+        kept = torch.empty((layers, slots, heads, keep), **i32)
+        assert kv.evict(torch.arange(slots, **i32), torch.full((slots,), keep, **i32), w, kept, recent=recent) == OK
+        assert kv.get_status() == OK and bool((lens == keep).all())
+        # the heaviest of those before the last ones, which stay the last
+        m = keep - recent
+        best = w0[..., :L - recent].topk(m, -1).indices.sort(-1).values
+        assert torch.equal(kept[..., :m].sort(-1).values.long(), best)
+        assert torch.equal(kept[..., m:].long(), torch.arange(L - recent, L, device="cuda").expand(*kept.shape[:3], -1))
+        rows = lambda p, n: p[:, :, was.long()].flatten(3, 4)[:, :, :, :n]     # [layers, 2, slots, n, heads, 64]
+        at = kept.long().permute(0, 1, 3, 2)[:, None, :, :, :, None].expand(-1, 2, -1, -1, -1, 64)
+        assert torch.equal(rows(pool, keep), rows(old, L).gather(3, at))
+        assert torch.equal(w[..., :keep], w0.gather(-1, kept.long())) and not bool(w[..., keep:].any())
+        del pool, old, kv

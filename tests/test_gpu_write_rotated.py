@@ -298,3 +298,25 @@ def test_another_stream_and_graph(torch):
             c.pool.zero_()
             assert c.call(want) == OK
             assert torch.equal(out, want) and torch.equal(got, c.pool)
+
+
+def test_largest_calls(torch):
+    """2^20 tokens, and 1,024 heads of each kind; without norms, turned by nothing: copies."""
+    from paper_2609_09800_amd import hbf
+    i32 = dict(dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    for n, heads, kv_heads, page in ((1 << 20, 2, 1, 16), (5, 1024, 1024, 4)):
+        say(f"write_rotated largest {n} {heads}/{kv_heads}")
+        held = -(-n // page)
+        pool = torch.zeros((1, 2, held, page, kv_heads, 64), dtype=torch.float16, device="cuda")
+        tables = torch.arange(held, **i32).flip(0).view(1, held).contiguous()
+        kv = hbf.KvPages(pool, refs=torch.ones(held, **i32), tables=tables, lens=torch.full((1,), n, **i32))
+        q, k, v = (torch.randn((n, h, 64), generator=gen, device="cuda").half() for h in (heads, kv_heads, kv_heads))
+        out = torch.empty_like(q)
+        freqs = torch.zeros(32, dtype=torch.float64, device="cuda")
+        slots = torch.zeros(n, **i32)
+        assert kv.write_rotated(0, q, k, v, slots, torch.arange(n, **i32), freqs, out) == OK and kv.get_status() == OK
+        assert torch.equal(out, q)
+        for plane, x in ((0, k), (1, v)):
+            assert torch.equal(pool[0, plane][tables[0].long()].flatten(0, 1)[:n], x)
+        del pool, q, k, v, out, kv
