@@ -205,7 +205,7 @@ struct Stage : Places<D, NT> {
       if (ONCE) {  // past the caches' order, as nobody else reads them (64 rows of 4,096 tokens 122 -> 110 us)
         k[j] = __builtin_nontemporal_load(kp);
         if (V) v[j] = __builtin_nontemporal_load(vp);
-      } else {  // a row's tiles find them there (4 rows of 32 tokens behind 4,096: 52 us, 59 the other way)
+      } else {  // a row's tiles find them there (4 rows of 32 tokens in 4,096: 51 us, 59 the other way)
         k[j] = *kp;
         if (V) v[j] = *vp;
       }
@@ -846,7 +846,7 @@ __global__ __launch_bounds__(MANY ? MANY_THREADS : THREADS, MANY ? 1 : 2) void k
   }
   uint32_t most = (steps + a.part_steps - 1) / a.part_steps;
   // (a part's steps and the trips that its join takes: as many of one as of the other, about; one row of 20,000 tokens
-  // 22.5 -> 18.7 us)
+  // 22.5 -> 19 us)
   if (!MANY) most = min(most, (uint32_t)(3.5f * __builtin_sqrtf((float)steps)) + 1);
   const uint32_t parts = min(most, (uint32_t)a.splits);
   const uint32_t each = (steps + parts - 1) / parts;
@@ -1345,7 +1345,7 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   // more to join their parts: for calls of more than 16 queries a row and KV head, of at least 450,000 tokens met by
   // tiles of 16 (4 rows of 128 queries in 1,000 tokens, 4 KV heads, in tiles of 16 and of 256: 17 and 36 us; 16 of 64
   // in 2,000: 54 and 47), whose tiles of 256, in parts of 1,024 tokens, take half of the card at least (one row of
-  // 2,048 queries in 2,000: 36 and 68; four of 256 in 4,096: 51 and 71, in 8,192: 102 and 79).  As a rule a row is no
+  // 2,048 queries in 2,000: 36 and 68; four of 256 in 4,096: 45 and 71, in 8,192: 102 and 79).  As a rule a row is no
   // longer than 16,384, however wide its table is.
   const int64_t likely = std::min<int64_t>(longest, 16384);
   const bool many = queries > 16 * rows && (queries >> 4) * layer.kv_heads * likely >= 450000 &&
@@ -1353,9 +1353,10 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   a.tile_shift = many ? 8 : 4;
   a.tile_q = 1 << a.tile_shift;
   a.slots = (int)(queries >> a.tile_shift) + ch.rows;
-  // Parts, so that a card's worth of workgroups have work if all rows are long, twice that where rows of different
-  // lengths have to be packed; a tile takes as many as its length gives work for.  Where the tiles alone are a card's
-  // worth, a part has 8 steps at least (64 rows of 500 tokens 24.1 -> 19.1 us, of 1,500 47.3 -> 48.5).
+  // Parts, so that the workgroups of all rows, if they are long, have room at once, two on a CU where the tiles are
+  // many (8 rows behind 16,000 tokens, 32 tiles: in 160 workgroups 52 us, in 256 65; 24 behind 10,000, 96 tiles: in 480
+  // 86, in 672 101); a tile takes as many as its length gives work for.  Where the tiles alone are a card's worth, a
+  // part has 8 steps at least (64 rows of 500 tokens 24.1 -> 19.1 us, of 1,500 47.3 -> 48.5).
   const int64_t groups = (int64_t)a.slots * layer.kv_heads;
   // Rows of one tile each: places that no row needs may come at a fixed distance, and in the places' order they would
   // leave some of the XCDs, which take workgroups by turns, idle (64 rows of 16 queries behind 2,048 tokens 91 -> 77
@@ -1365,10 +1366,11 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   if (a.one_tile)
     for (a.spread = (uint32_t)(groups * 0.618) | 1; std::gcd((uint64_t)a.spread, (uint64_t)groups) != 1; a.spread += 2) {
     }
-  a.part_steps = many ? 16 : groups >= 256 ? 8 : 2;
+  const int64_t tiles = std::max(rows, queries >> a.tile_shift) * layer.kv_heads;  // that there are, as a rule
+  a.part_steps = many ? 16 : tiles >= 256 ? 8 : 2;
   const int64_t steps = longest / ((many ? MANY_TILE : WAVES * FEW_TILE) * a.part_steps) + 1;
-  const int64_t card = many ? 256 : groups < 128 ? 512 : 1024;
-  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min(steps, card / groups));
+  const int64_t parts = many || tiles < 64 ? 256 / groups : 512 / tiles;
+  a.splits = groups > (int64_t)HBF_CHUNK_CTL_WORDS || !ch.dev_ctl ? 1 : (int)std::max<int64_t>(1, std::min(steps, parts));
   // Weights of tiles of 16: from the scores that attention leaves, where they take no more than SCORES_BYTES (64 rows of
   // 8 queries behind 4,096 tokens: 146 us, from K again 173) and are not many for each token (one row of 256 queries
   // behind 4,096: 35, from K by k_weigh_many 39; of 1,024 behind 1,000, the other way: 134 and 42).
