@@ -1357,7 +1357,7 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   // many (8 rows behind 16,000 tokens, 32 tiles: in 160 workgroups 52 us, in 256 65; 24 behind 10,000, 96 tiles: in 480
   // 86, in 672 101); a tile takes as many as its length gives work for.  Where the tiles alone are a card's worth, a
   // part has 8 steps at least (64 rows of 500 tokens 24.1 -> 19.1 us, of 1,500 47.3 -> 48.5).
-  const int64_t groups = (int64_t)a.slots * layer.kv_heads;
+  const int64_t groups = std::max<int64_t>((int64_t)a.slots * layer.kv_heads, 1);  // (0 without rows)
   // Rows of one tile each: places that no row needs may come at a fixed distance, and in the places' order they would
   // leave some of the XCDs, which take workgroups by turns, idle (64 rows of 16 queries behind 2,048 tokens 91 -> 77
   // us).  A row's tiles stay side by side, as they read the same (one row of 2,048 queries 36 us, spread 54).

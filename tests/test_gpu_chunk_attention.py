@@ -376,6 +376,8 @@ def test_strides_and_layouts(torch, shape):
     assert kv.attention(1, b.q, o2, b.dev["slots"], b.dev["starts"]) == OK and torch.equal(o2, want)
     assert kv.attention(1, b.q, o2, b.dev["slots"][:0], b.dev["starts"][:1]) == OK and torch.equal(o2, want)
     assert kv.attention(1, b.q[:0], o2[:0], b.dev["slots"], torch.zeros_like(b.dev["starts"])) == OK
+    assert kv.attention(1, b.q[:0], o2[:0], b.dev["slots"][:0], b.dev["starts"][:1], weights=all_w[:, 1]) == OK
+    assert kv.attention(1, b.q[:1], o2[:1], b.dev["slots"][:0], b.dev["starts"][:1]) == OK
     assert kv.get_status() == OK
 
 

@@ -70,6 +70,17 @@ def test_attention_refuses(lib):
     assert lib.hbf_kv_chunk_workspace_bytes(ctypes.byref(c), ctypes.byref(l), ctypes.byref(h), None) == EINVAL
 
 
+@pytest.mark.parametrize("rows,tokens,heads", [(0, 0, 8), (0, 1, 2), (0, 20, 8), (3, 0, 8), (1, 1, 2)])
+def test_scratch_of_calls_with_little_or_nothing_to_do(lib, rows, tokens, heads):
+    for more in (dict(), dict(dev_ctl=AT), dict(dev_ctl=AT, dev_weights=AT, weights_tokens=0),
+                 dict(dev_weights=AT, weights_tokens=2 ** 31 - 1)):
+        b, c, l, h = ctypes.c_size_t(), cache(), layer(), chunk(rows=rows, tokens=tokens, heads=heads, **more)
+        assert lib.hbf_kv_chunk_workspace_bytes(ctypes.byref(c), ctypes.byref(l), ctypes.byref(h), ctypes.byref(b)) == OK
+        assert b.value >= 256
+        if not rows or not tokens:
+            assert call_chunk(lib, c, l, h) == OK
+
+
 def test_write_rotated_refuses(lib):
     def call(kv={}, at=0, **kw):
         d = dict(dev_q=AT, dev_k=AT, dev_v=AT, q_row_stride=512, q_head_stride=64, k_row_stride=128, k_head_stride=64,
