@@ -172,7 +172,8 @@ hipError_t launch_kv_write_rotated(const hbf_kv &kv, int layer, const hbf_new_to
   a.v_pages = a.k_pages + kv.plane_stride;
   const int at_once = 64 / (nt.head_dim / 16);
   a.groups = (nt.heads + 2 * nt.kv_heads + at_once - 1) / at_once;
-  // Few tokens: a wave for each group of heads, so that they wait side by side.
+  // Few tokens: a wave for each group of heads, so that they wait side by side (5 groups a token; 256 tokens 4.2 us, by
+  // a wave a token 6.9; 1,638 10.1 and 10.1; 8,192 38.9 and 30.2, in a graph).
   a.per_wave = (int64_t)nt.n * a.groups <= 8192 ? 1 : a.groups;
   a.waves = (a.groups + a.per_wave - 1) / a.per_wave;
   return nt.dtype == HBF_BF16 ? run<Bf16>(a, s) : run<Fp16>(a, s);
