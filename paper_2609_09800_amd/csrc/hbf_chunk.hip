@@ -703,7 +703,7 @@ struct Many {
     if (!whole) mask(sn, t.x0 + next * MANY_TILE + HALF - first);
     maximum<true>(sn);
   }
-  // Waits until at most `tiles` (0 .. 2) of the staged tiles are on their way.
+  // Waits until at most `tiles` (0 .. 2) of the staged tiles are on their way, in every wave.
   __device__ __forceinline__ void arrived(int tiles) {
     constexpr int N = 2 * PASSES;
     if (tiles <= 0) loads_left<0>();
@@ -730,8 +730,8 @@ struct Many {
     maximum<false>(sa);
     for (int i = 0; i < n; i++) {
       step(sa, sb, i, 0, true, now);
-      // the next tile is there, and one more goes where all are done with
-      arrived(n - 2 - i);
+      // the next tile is there, the one behind it may be on its way, and one more goes where all are done with
+      arrived(min(n - 2 - i, 1));
       if (i + RING - 1 < n) stage(i + RING - 1);
       const bool more = i + 1 < n;
       now = more && whole(i + 1);
