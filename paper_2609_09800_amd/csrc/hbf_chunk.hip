@@ -920,16 +920,18 @@ __global__ __launch_bounds__(THREADS) void k_weigh_scores(Args a, int blocks) {
         const float *from = a.scores + x;
         float s[AHEAD];
         float2 ml[AHEAD];
+        bool seen[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; k++) {
           const int qq = min(q + k, n - 1), tok = token_of(a, qq);
           const int64_t at = (int64_t)(r.start + tok) * a.ch.heads + head * a.group + qq - tok * a.group;
           ml[k] = a.query_ml[at];
           s[k] = has ? from[at * a.score_tokens] : 0.f;
+          seen[k] = has & (q + k < n) & sees(a, r.len - r.n + tok, (int)j);
         }
 #pragma unroll
-        for (int k = 0; k < AHEAD; k++)
-          sum += has && q + k < n && ml[k].y != 0.f ? __builtin_amdgcn_exp2f((s[k] - ml[k].x) * a.c) * ml[k].y : 0.f;
+        for (int k = 0; k < AHEAD; k++)  // (not seen: the score is -infinity, but the query's sums may be NaN)
+          sum += seen[k] && ml[k].y != 0.f ? __builtin_amdgcn_exp2f((s[k] - ml[k].x) * a.c) * ml[k].y : 0.f;
       }
     }
     if (W > 1) {
