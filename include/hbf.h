@@ -611,7 +611,7 @@ typedef struct {
   const void *dev_q;          /* [tokens][heads][head_dim], 16-byte aligned, strides in elements, multiples of 8 */
   int64_t q_row_stride, q_head_stride;
   int32_t tokens;             /* 0 .. 2^20, tokens * heads <= 2^24 */
-  int32_t rows;               /* 0 .. 65535 */
+  int32_t rows;               /* 0 .. 65535, rows * kv_heads + tokens * heads / 16 < 2^24 */
   int32_t heads;              /* a multiple of kv_heads, up to 1024 */
   float scale;                /* finite */
   const int32_t *dev_slots;   /* [rows] */

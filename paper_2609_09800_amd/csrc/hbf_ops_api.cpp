@@ -75,6 +75,8 @@ int check_chunk(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch
   if (ch->tokens < 0 || ch->tokens > 1 << 20 || ch->rows < 0 || ch->rows > 65535 || ch->heads < layer->kv_heads ||
       ch->heads > 1024 || ch->heads % layer->kv_heads || (int64_t)ch->tokens * ch->heads > 1 << 24)
     return HBF_EINVAL;
+  // a workgroup of 256 threads for each row's and KV head's 16 queries, all in one launch, which has fewer than 2^32 threads
+  if ((int64_t)ch->rows * layer->kv_heads * 16 + (int64_t)ch->tokens * ch->heads >= 1 << 28) return HBF_EINVAL;
   if (!isfinite(ch->scale) || ch->window < 0 || ch->sinks < 0) return HBF_EINVAL;
   if (ch->q_row_stride % 8 || ch->q_head_stride % 8 || ch->out_row_stride % 8 || ch->out_head_stride % 8)
     return HBF_EINVAL;

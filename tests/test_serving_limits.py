@@ -1,0 +1,21 @@
+"""Serving from a cache of pages, calls at and past the largest sizes, on the host (no GPU)."""
+import ctypes
+
+import pytest
+
+from test_serving_host import AT, EINVAL, OK, cache, call_chunk, chunk, layer, lib  # noqa: F401
+
+
+@pytest.mark.parametrize("rows,kv_heads,tokens,heads,rc", [
+    (65535, 257, 1, 257, EINVAL), (65535, 1024, 1, 1024, EINVAL), (65535, 256, 16, 256, EINVAL), (62000, 256, 1 << 15, 512, EINVAL),
+    (65535, 256, 14, 256, OK), (61439, 256, 1 << 15, 512, OK), (65535, 1, 1 << 20, 16, OK), (15000, 1024, 1, 1024, OK)])
+def test_attention_refuses_more_workgroups_than_a_launch_takes(lib, rows, kv_heads, tokens, heads, rc):   # noqa: F811
+    """A tile of 16 queries and a KV head a workgroup of 256 threads: one launch has fewer than 2^32 threads."""
+    b, c, l = ctypes.c_size_t(), cache(), layer(kv_heads=kv_heads)
+    for weights in (None, AT):
+        h = chunk(rows=rows, tokens=tokens, heads=heads, dev_weights=weights, weights_tokens=64)
+        assert lib.hbf_kv_chunk_workspace_bytes(ctypes.byref(c), ctypes.byref(l), ctypes.byref(h), ctypes.byref(b)) == rc
+        if rc != OK:
+            assert call_chunk(lib, c, l, h) == rc
+        else:   # every workgroup that such a call starts
+            assert (rows + (tokens * (heads // kv_heads) >> 4)) * kv_heads * 256 < 1 << 32
