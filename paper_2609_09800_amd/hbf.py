@@ -991,10 +991,14 @@ class KvPages:
             _dev(kept, "kept", _I32)
             raise HbfError(HBF_EINVAL, f"kept: shape {tuple(kept.shape)}, expected "
                                        f"[{self.layers}, {n}, {self.kv_heads}, max_keep]")
-        ev = hbf_eviction(slots.data_ptr(), keep.data_ptr(), n, self.kv_heads, int(sinks), int(recent),
+        sinks, recent, max_keep = int(sinks), int(recent), kept.shape[3]
+        for value, what in ((n, "slots"), (sinks, "sinks"), (recent, "recent"), (max_keep, "max_keep")):
+            if not -(1 << 31) <= value < 1 << 31:   # (ctypes would cut it)
+                raise HbfError(HBF_EINVAL, f"{what} {value}: expected what fits 32 bits")
+        ev = hbf_eviction(slots.data_ptr(), keep.data_ptr(), n, self.kv_heads, sinks, recent,
                           weights.data_ptr(), _stride(weights, 0), _stride(weights, 1), _stride(weights, 2),
                           min(weights.shape[3], (1 << 31) - 1), None if weights_out is None else weights_out.data_ptr(),
-                          kept.data_ptr(), kept.shape[3])
+                          kept.data_ptr(), max_keep)
         return self._lib.hbf_kv_evict(d, ev, self._on(stream))
 
     def _layer(self, layer):

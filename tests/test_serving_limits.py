@@ -3,7 +3,9 @@ import ctypes
 
 import pytest
 
-from test_serving_host import AT, EINVAL, OK, cache, call_chunk, chunk, layer, lib  # noqa: F401
+from paper_2609_09800_amd import hbf
+from test_scratch_streams import Block, notes  # noqa: F401
+from test_serving_host import AT, EINVAL, OK, cache, call_chunk, chunk, layer, lib, objects  # noqa: F401
 
 
 @pytest.mark.parametrize("rows,kv_heads,tokens,heads,rc", [
@@ -19,3 +21,14 @@ def test_attention_refuses_more_workgroups_than_a_launch_takes(lib, rows, kv_hea
             assert call_chunk(lib, c, l, h) == rc
         else:   # every workgroup that such a call starts
             assert (rows + (tokens * (heads // kv_heads) >> 4)) * kv_heads * 256 < 1 << 32
+
+
+@pytest.mark.parametrize("what,value", [("sinks", 2 ** 32), ("recent", 2 ** 32 + 8), ("recent", 2 ** 31), ("sinks", -2 ** 32),
+                                        ("max_keep", 2 ** 32)])
+def test_evict_refuses_numbers_that_do_not_fit(notes, what, value):   # noqa: F811
+    """(Cut to 32 bits they would be other numbers, 0 and 8 among them.)"""
+    kv = objects(notes)
+    slots, keep, w, kept = (Block(notes, s, d) for s, d in (((3,), "int32"), ((3,), "int32"), ((2, 8, 1, 64), "float32"), ((2, 3, 1, value if what == "max_keep" else 40), "int32")))
+    with pytest.raises(hbf.HbfError, match=f"{what}.*fit"):
+        kv.evict(slots, keep, w, kept, **({} if what == "max_keep" else {what: value}))
+    assert not notes.calls
