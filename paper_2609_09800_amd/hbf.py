@@ -901,14 +901,17 @@ class KvPages:
         qs, ks, vs, os = q.stride(), k.stride(), v.stride(), q_out.stride()
         row = n > 1
         nt = self._new_args
-        _pack_new_tokens(nt, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), qs[0] if row else 0,
-                         qs[1] if heads > 1 else 0, ks[0] if row else 0, ks[1] if self.kv_heads > 1 else 0,
-                         vs[0] if row else 0, vs[1] if self.kv_heads > 1 else 0, q_out.data_ptr(),
-                         os[0] if row else 0, os[1] if heads > 1 else 0, n, heads, self.kv_heads, dim,
-                         HBF_BF16 if dtype is torch.bfloat16 else HBF_FP16, HBF_ROT_PAIRS if interleaved else 0,
-                         0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
-                         eps, freqs.numel(), freqs.data_ptr(), slots.data_ptr(), pos.data_ptr(),
-                         0 if positions is None else positions.data_ptr())
+        try:
+            _pack_new_tokens(nt, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), qs[0] if row else 0,
+                             qs[1] if heads > 1 else 0, ks[0] if row else 0, ks[1] if self.kv_heads > 1 else 0,
+                             vs[0] if row else 0, vs[1] if self.kv_heads > 1 else 0, q_out.data_ptr(),
+                             os[0] if row else 0, os[1] if heads > 1 else 0, n, heads, self.kv_heads, dim,
+                             HBF_BF16 if dtype is torch.bfloat16 else HBF_FP16, HBF_ROT_PAIRS if interleaved else 0,
+                             0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(),
+                             eps, freqs.numel(), freqs.data_ptr(), slots.data_ptr(), pos.data_ptr(),
+                             0 if positions is None else positions.data_ptr())
+        except (struct.error, OverflowError):
+            raise HbfError(HBF_EINVAL, f"{n} tokens, {freqs.numel()} freqs, eps {eps}: expected what fits 32 bits") from None
         return self._lib.hbf_kv_write_rotated(d, layer, nt, self._on(stream))
 
     def attention(self, layer, q, out, slots, starts, lse=None, weights=None, scale=None, window=0, sinks=0,
@@ -948,11 +951,15 @@ class KvPages:
         kv = self._layer(layer)
         qs, os = q.stride(), out.stride()
         at = self._chunk_args
-        _pack_chunk(at, 0, q.data_ptr(), qs[0] if tokens > 1 else 0, qs[1] if heads > 1 else 0, tokens, rows, heads,
-                    dim ** -0.5 if scale is None else scale, slots.data_ptr(), starts.data_ptr(), int(window),
-                    int(sinks), out.data_ptr(), os[0] if tokens > 1 else 0, os[1] if heads > 1 else 0,
-                    0 if lse is None else lse.data_ptr(), 0 if weights is None else weights.data_ptr(), *ws,
-                    min(held, (1 << 31) - 1), self._chunk_at or 0)
+        try:
+            _pack_chunk(at, 0, q.data_ptr(), qs[0] if tokens > 1 else 0, qs[1] if heads > 1 else 0, tokens, rows, heads,
+                        dim ** -0.5 if scale is None else scale, slots.data_ptr(), starts.data_ptr(), int(window),
+                        int(sinks), out.data_ptr(), os[0] if tokens > 1 else 0, os[1] if heads > 1 else 0,
+                        0 if lse is None else lse.data_ptr(), 0 if weights is None else weights.data_ptr(), *ws,
+                        min(held, (1 << 31) - 1), self._chunk_at or 0)
+        except (struct.error, OverflowError):
+            raise HbfError(HBF_EINVAL, f"{tokens} tokens, {rows} rows, window {window}, sinks {sinks}, scale {scale}: "
+                                       "expected what fits 32 bits") from None
         sizes = (tokens, rows, heads, None if weights is None else held)
         if sizes != self._chunk_sizes:
             b = ctypes.c_size_t()

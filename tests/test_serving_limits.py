@@ -23,6 +23,28 @@ def test_attention_refuses_more_workgroups_than_a_launch_takes(lib, rows, kv_hea
             assert (rows + (tokens * (heads // kv_heads) >> 4)) * kv_heads * 256 < 1 << 32
 
 
+@pytest.mark.parametrize("how", [dict(window=2 ** 31), dict(window=2 ** 32 + 5), dict(sinks=2 ** 31), dict(sinks=-2 ** 31 - 1), dict(window=10 ** 30)])
+def test_attention_refuses_numbers_that_do_not_fit(notes, how):   # noqa: F811
+    kv = objects(notes)
+    q, out, slots, starts = (Block(notes, s, d) for s, d in (((9, 4, 64), "bf16"), ((9, 4, 64), "bf16"), ((3,), "int32"), ((4,), "int32")))
+    with pytest.raises(hbf.HbfError, match=f"{next(iter(how))}.*fit"):
+        kv.attention(0, q, out, slots, starts, **how)
+    assert not notes.calls
+    for ok in (dict(window=2 ** 31 - 1, sinks=2 ** 31 - 1), dict(window=-2 ** 31), dict(scale=1e39)):   # (the library looks at these)
+        assert kv.attention(0, q, out, slots, starts, **ok) == OK
+
+
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32 + 3])
+def test_write_rotated_refuses_numbers_that_do_not_fit(notes, monkeypatch, n):   # noqa: F811
+    monkeypatch.setattr(hbf.torch, "float64", "float64", raising=False)
+    kv = objects(notes)
+    k, v, slots, pos, freqs = (Block(notes, s, d) for s, d in (((n, 1, 64), "bf16"), ((n, 1, 64), "bf16"), ((n,), "int32"), ((n,), "int32"), ((32,), "float64")))
+    q, out = Block(notes, (n, 4, 64), "bf16"), Block(notes, (n, 4, 64), "bf16")
+    with pytest.raises(hbf.HbfError, match="tokens.*fit"):
+        kv.write_rotated(0, q, k, v, slots, pos, freqs, out)
+    assert not notes.calls
+
+
 @pytest.mark.parametrize("what,value", [("sinks", 2 ** 32), ("recent", 2 ** 32 + 8), ("recent", 2 ** 31), ("sinks", -2 ** 32),
                                         ("max_keep", 2 ** 32)])
 def test_evict_refuses_numbers_that_do_not_fit(notes, what, value):   # noqa: F811
