@@ -622,7 +622,7 @@ typedef struct {
   float *dev_lse;             /* [tokens][heads], or NULL */
   float *dev_weights;         /* slot s, KV head h at s * weights_slot_stride + h * weights_head_stride; or NULL */
   int64_t weights_slot_stride, weights_head_stride;  /* in elements, >= 0 */
-  int32_t weights_tokens;     /* what a row of weights holds */
+  int32_t weights_tokens;     /* what a row of weights holds; rows do not overlap */
   uint32_t *dev_ctl;          /* HBF_CHUNK_CTL_WORDS words, zero before the first call and kept by the calls from then on;
                                  calls that share them must be ordered on one stream.  NULL: few long rows are not cut
                                  into parts */

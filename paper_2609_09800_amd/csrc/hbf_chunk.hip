@@ -1240,7 +1240,8 @@ __global__ __launch_bounds__(MANY_THREADS, 1) void k_weigh_many(Args a) {
   static_assert(WEIGH_ROWS == MANY_THREADS, "a row a thread");
   const int kv_heads = a.layer.kv_heads;
   // The blocks of rows whose slot no row before names.
-  int units, splits = 1;
+  uint32_t units;
+  int splits = 1;
   {
     const int i = threadIdx.x;
     int mine = 0;
@@ -1255,10 +1256,10 @@ __global__ __launch_bounds__(MANY_THREADS, 1) void k_weigh_many(Args a) {
     uint32_t total;
     row_blocks[i] = (int)block_scan<MANY_THREADS>((uint32_t)mine, &total, scan);
     __syncthreads();
-    units = (int)min((uint64_t)total * kv_heads, (uint64_t)INT32_MAX / 64);
-    if (a.part_w) splits = max(1, min((int)gridDim.x / max(units, 1), 64));
+    units = total * kv_heads;  // (below 2^32: the weights of as many blocks take more memory than the card has)
+    if (a.part_w) splits = max(1, min((int)(gridDim.x / max(units, 1u)), 64));
   }
-  for (int u = blockIdx.x; u < units * splits; u += gridDim.x) {
+  for (uint32_t u = blockIdx.x; u < units * splits; u += gridDim.x) {
     const int split = u / units, unit = u - split * units, head = unit % kv_heads, b = unit / kv_heads;
     int i0 = 0;  // the last row whose first block is at most b
     for (int hi = a.ch.rows; hi - i0 > 1;) {

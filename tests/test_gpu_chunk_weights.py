@@ -41,3 +41,27 @@ def test_sums_that_are_not_finite_stay_with_what_the_query_sees(torch, way, wind
     assert bool(torch.isnan(got[seen]).all())
     err = (got.double() - want).abs()
     assert bool((err <= tol)[~seen].all()), "tokens that it does not see"
+
+
+def test_more_blocks_of_tokens_than_2_to_the_25(torch):   # noqa: F811
+    """512 rows of 32,769 tokens (the same pages) and 1,024 KV heads, 69 GB of weights: every new token, which sees
+    itself alone, has its 1."""
+    from paper_2609_09800_amd import hbf
+    rows, L, heads, dim, page, n = 512, 32769, 1024, 64, 16, 32
+    say(f"weights of {rows} x {L} x {heads}")
+    assert rows * -(-L // 512) * heads > 1 << 25
+    i32 = dict(dtype=torch.int32, device="cuda")
+    held = -(-L // page)
+    pool = torch.zeros((1, 2, held, page, heads, dim), dtype=torch.bfloat16, device="cuda")
+    kv = hbf.KvPages(pool, refs=torch.full((held,), rows, **i32), tables=torch.arange(held, **i32).repeat(rows, 1), lens=torch.full((rows,), L, **i32))
+    q = torch.ones((rows * n, heads, dim), dtype=torch.bfloat16, device="cuda")
+    out, w = torch.empty_like(q), torch.zeros((rows, heads, L), device="cuda")
+    slots, starts = torch.arange(rows, **i32), torch.arange(0, rows * n + 1, n, **i32)
+    assert kv.attention(0, q, out, slots, starts, weights=w, window=1) == OK and kv.get_status() == OK
+    for at in range(0, rows, 64):
+        new = w[at:at + 64, :, L - n:]
+        assert bool((new == 1.0).all()), f"rows from {at}: {int((new != 1.0).sum())} without their weight"
+        new.zero_()
+        assert not bool(w[at:at + 64].any())
+    del pool, kv, q, out, w, new
+    torch.cuda.empty_cache()
