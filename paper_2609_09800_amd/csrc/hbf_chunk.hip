@@ -1328,8 +1328,8 @@ Args plan(const hbf_kv &kv, const hbf_kv_layer &layer, const hbf_chunk &ch) {
   a.layer = layer;
   a.ch = ch;
   a.group = ch.heads / layer.kv_heads;
-  // (1e-30: as flat as 0 is, and -infinity times it stays that)
-  a.c = std::min(std::max(fabsf(ch.scale) * LOG2E, 1e-30f), FLT_MAX);
+  // (the least number that is not 0: as flat as 0 is, and -infinity times it stays that)
+  a.c = std::min(std::max(fabsf(ch.scale) * LOG2E, FLT_TRUE_MIN), FLT_MAX);
   a.flip = ch.scale < 0 ? 0x80008000u : 0;
   a.window = ch.window ? (uint32_t)ch.window : UINT32_MAX;
   // with M = ceil(2^k / d), k = 31 + ceil(log2 d): x * M / 2^k is at most x / 2^31 < 1 / d above x / d
