@@ -614,8 +614,8 @@ Args plan(const hbf_kv_layer &kv, const hbf_attention &at) {
   a.kv = kv;
   a.at = at;
   a.group = at.heads / kv.kv_heads;
-  // (1e-30: as flat as 0 is, and -infinity times it stays that)
-  a.c = std::min(std::max(fabsf(at.scale) * LOG2E, 1e-30f), FLT_MAX);
+  // (the least number that is not 0: as flat as 0 is, and -infinity times it stays that)
+  a.c = std::min(std::max(fabsf(at.scale) * LOG2E, FLT_TRUE_MIN), FLT_MAX);
   a.flip = at.scale < 0 ? 0x80008000u : 0;
   // with M = ceil(2^k / d), k = 31 + ceil(log2 d): token * M / 2^k is at most token / 2^31 < 1 / d above token / d
   while ((1 << a.page_shift) < kv.page_tokens) a.page_shift++;
