@@ -629,7 +629,10 @@ typedef struct {
 } hbf_chunk;
 #define HBF_CHUNK_CTL_WORDS 2048u
 
-/* Device scratch of a call, in bytes (sizes are looked at, and whether dev_weights and dev_ctl are given). */
+/* Device scratch of a call, in bytes (sizes are looked at, and whether dev_weights and dev_ctl are given).
+ * With dev_weights, a call of few queries may ask for 4 bytes for each of them and each token that a row of the table
+ * and of the weights has room for, whatever the lengths are, up to 512 MiB beside the rest; past that it asks for none
+ * of them and reads K a second time.  Where the host knows that sequences are shorter, weights_tokens may say so. */
 int hbf_kv_chunk_workspace_bytes(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch, size_t *bytes);
 
 /* The tables and lengths are the cache's; its counts, pool and workspace are
@@ -649,7 +652,10 @@ int hbf_kv_chunk_attention(const hbf_kv *kv, const hbf_kv_layer *layer, const hb
  * largest weights (ties: the lowest position; NaN counts as the lowest).  With
  * m = keep - recent, chosen tokens before m stay where they are, those from m
  * on move, in order, to the places that are free before it, in order: the fewest moves.
- * The last `recent` follow from m on, in their order.  The slot's length becomes
+ * The last `recent` follow from m on, in their order.  So places count, no
+ * longer the tokens' order: a window of hbf_kv_chunk that reaches past the last
+ * `recent` and what came behind them sees whichever of the middle lie there.
+ * The slot's length becomes
  * keep, its pages behind that lose one count and their entries become -1.
  * dev_kept[layer][i][head][j] receives the old position of the token that is at
  * j now, -1 from the new length on.  weights follow their tokens; behind the new

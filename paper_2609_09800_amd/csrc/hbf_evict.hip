@@ -6,15 +6,18 @@
 // are taken from the lowest position on.  The chosen tokens that already lie before the
 // new end of the middle stay, the others fill the places between them: fewer
 // bytes than closing ranks, and no place is both read and written, so that all
-// of it runs at once.  Only the last tokens, which stay in their order, move
-// over places that may have been read before: in a launch of their own, a
-// workgroup a plane, some tokens at a time from the front.
+// of it runs at once.  The last tokens, which stay in their order, move over
+// places that the others are read from, and over their own where fewer leave than
+// stay last: in a launch of their own, 32 KiB of a plane a workgroup, or where they
+// move over themselves a workgroup a plane, some tokens at a time from the front.
 // Launches: the check of every row beside the choice; the middle's moves; the
 // last tokens' and the weights behind them; tables, counts and lengths.  (48 layers,
 // 8 sequences of 1,100 to 2,200 tokens cut to 1,024, 4 heads of 128: 23 + 132 + 40 + 5 us,
-// the moves of single heads' 256 bytes at about 4.5 TB/s; a layer of 4 sequences of 600:
-// 11.6 + 6.5 + 6.3 + 2.5, each a few rounds to memory.  The last launch joined to the one
-// before by its last workgroup: 219 / 209 us and 34.3 / 33.7.)
+// the moves of single heads' 256 bytes at about 4.5 TB/s; the last 64 tokens' K and V,
+// 100 MB in two workgroups a plane, at half of a copy's rate, and beside them the weights,
+// which take 9 by themselves; a layer of 4 sequences of 600: 11.6 + 6.5 + 6.3 + 2.5, each a
+// few rounds to memory.  The last launch joined to the one before by its last workgroup:
+// 219 / 209 us and 34.3 / 33.7.)
 #include <algorithm>
 
 #include "hbf_half.h"

@@ -925,7 +925,13 @@ class KvPages:
         (not q itself); lse: float32 [tokens, heads] or None; weights: float32
         [slots, kv_heads, tokens] (slots and heads may be strided) or None:
         each cached token's grows by the probabilities that the row's queries
-        gave it.  What lies behind starts[rows] is left as it was."""
+        gave it.  What lies behind starts[rows] is left as it was.  The window
+        counts places: after evict, one that reaches past the last `recent` and
+        what came behind them sees whichever of the middle lie there.  With
+        weights, the object's scratch may hold a float for each query and each
+        token that both a table's row and weights have room for, up to 512 MiB
+        a call (and what it grew out of, less than that again): where sequences are known
+        to be shorter, pass weights[..., :n], n at least the longest length."""
         d = self._desc()
         dtype = self.pool.dtype
         if not 0 <= layer < self.layers:
@@ -987,7 +993,8 @@ class KvPages:
         may be strided) follow their tokens, in place or to weights_out (shaped
         and strided alike, not overlapping).  kept: int32 [layers, n, kv_heads, max_keep],
         max_keep at least the largest keep, receives each place's token's old
-        position, -1 behind them."""
+        position, -1 behind them.  The middle is in no order afterwards, and
+        attention's window counts places."""
         d = self._desc()
         n = _ints(slots, "slots")
         _ints(keep, "keep", n)
