@@ -961,7 +961,7 @@ class KvPages:
             _pack_chunk(at, 0, q.data_ptr(), qs[0] if tokens > 1 else 0, qs[1] if heads > 1 else 0, tokens, rows, heads,
                         dim ** -0.5 if scale is None else scale, slots.data_ptr(), starts.data_ptr(), int(window),
                         int(sinks), out.data_ptr(), os[0] if tokens > 1 else 0, os[1] if heads > 1 else 0,
-                        0 if lse is None else lse.data_ptr(), 0 if weights is None else weights.data_ptr(), *ws,
+                        0 if lse is None else lse.data_ptr(), 0 if weights is None else self._address(weights), *ws,
                         min(held, (1 << 31) - 1), self._chunk_at or 0)
         except (struct.error, OverflowError):
             raise HbfError(HBF_EINVAL, f"{tokens} tokens, {rows} rows, window {window}, sinks {sinks}, scale {scale}: "
@@ -984,6 +984,10 @@ class KvPages:
                 or tuple(t.shape[:-1]) != lead or (t.shape[-1] > 1 and t.stride(-1) != 1):
             raise HbfError(HBF_EINVAL, f"{what}: expected float32 {[*lead, 'tokens']} in GPU memory, tokens contiguous")
         _writable(t, what)
+
+    def _address(self, weights):
+        """Of weights that are given: those that hold no token have none of their own, and NULL says something else."""
+        return weights.data_ptr() or self.lens.data_ptr()
 
     def evict(self, slots, keep, weights, kept, sinks=0, recent=0, weights_out=None, stream=None):
         """Slot slots[i] is cut down to keep[i] tokens (int32 [n]), in every
@@ -1010,7 +1014,7 @@ class KvPages:
             if not -(1 << 31) <= value < 1 << 31:   # (ctypes would cut it)
                 raise HbfError(HBF_EINVAL, f"{what} {value}: expected what fits 32 bits")
         ev = hbf_eviction(slots.data_ptr(), keep.data_ptr(), n, self.kv_heads, sinks, recent,
-                          weights.data_ptr(), _stride(weights, 0), _stride(weights, 1), _stride(weights, 2),
+                          self._address(weights), _stride(weights, 0), _stride(weights, 1), _stride(weights, 2),
                           min(weights.shape[3], (1 << 31) - 1), None if weights_out is None else weights_out.data_ptr(),
                           kept.data_ptr(), max_keep)
         return self._lib.hbf_kv_evict(d, ev, self._on(stream))
