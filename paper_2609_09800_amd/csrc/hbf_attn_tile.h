@@ -93,6 +93,10 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[QT][U], float c, float (
   }
 }
 
+// A step's probabilities as the matrix cores take them with V: rounded to the
+// 16-bit type, each by half of a step relative to itself at most; the sum l keeps
+// them as they are.  (Errors against 64 bits, of the results' size: bfloat16 0.0019
+// to 0.0023, 0.0017 from the results' own rounding alone.)
 template <typename T>
 __device__ __forceinline__ u32x4 p_operand(f32x4 a, f32x4 b) {
   return u32x4{pack2<T>(a[0], a[1]), pack2<T>(a[2], a[3]), pack2<T>(b[0], b[1]), pack2<T>(b[2], b[3])};

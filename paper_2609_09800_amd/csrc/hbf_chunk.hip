@@ -1067,7 +1067,7 @@ __global__ __launch_bounds__(THREADS, 3) void k_weigh(Args a, int blocks) {
 // registers, 64 a wave, and meets 64 queries at a time, which all waves read from
 // LDS.  A block's queries are cut into `splits` as far as the card has room; the last
 // split to finish adds their sums up, in order.  Bound by issue, products and
-// exponentials by turns (2,048 tokens behind 2,048, 32 heads of 128: 110 us, the
+// exponentials by turns (2,048 tokens behind 2,048, 32 heads of 128: 108 us, the
 // products alone 41).
 constexpr int BLOCK = 64 * MANY_WAVES, Q_TILE = 64, Q_RING = 3;
 constexpr int WEIGH_GROUPS = 256;      // workgroups: one for each CU
