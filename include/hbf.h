@@ -630,9 +630,9 @@ typedef struct {
 #define HBF_CHUNK_CTL_WORDS 2048u
 
 /* Device scratch of a call, in bytes (sizes are looked at, and whether dev_weights and dev_ctl are given).
- * With dev_weights, a call of few queries may ask for 4 bytes for each of them and each token that a row of the table
- * and of the weights has room for, whatever the lengths are, up to 512 MiB beside the rest; past that it asks for none
- * of them and reads K a second time.  Where the host knows that sequences are shorter, weights_tokens may say so. */
+ * With dev_weights, a call of few queries may ask for 4 bytes for each query of each head and each token that a row of
+ * the table and of the weights has room for, whatever the lengths are, up to 512 MiB beside the rest; past that it asks
+ * for none of them and reads K a second time.  Where the host knows that sequences are shorter, weights_tokens may say so. */
 int hbf_kv_chunk_workspace_bytes(const hbf_kv *kv, const hbf_kv_layer *layer, const hbf_chunk *ch, size_t *bytes);
 
 /* The tables and lengths are the cache's; its counts, pool and workspace are

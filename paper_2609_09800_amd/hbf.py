@@ -928,10 +928,11 @@ class KvPages:
         gave it.  What lies behind starts[rows] is left as it was.  The window
         counts places: after evict, one that reaches past the last `recent` and
         what came behind them sees whichever of the middle lie there.  With
-        weights, the object's scratch may hold a float for each query and each
-        token that both a table's row and weights have room for, up to 512 MiB
-        a call (and what it grew out of, less than that again): where sequences are known
-        to be shorter, pass weights[..., :n], n at least the longest length."""
+        weights, the object's scratch may hold a float for each query of each
+        head and each token that both a table's row and weights have room for,
+        up to 512 MiB a call (and what it grew out of, less than that again):
+        where sequences are known to be shorter, pass weights[..., :n], n at
+        least the longest length."""
         d = self._desc()
         dtype = self.pool.dtype
         if not 0 <= layer < self.layers:
